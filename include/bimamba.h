@@ -287,6 +287,147 @@ size_t bimamba_workspace_bytes(const bimamba_desc* desc, int block_variant);
  * stride beyond 2^24 elements, which the answer does not know of: those take the parts).  Pure host code. */
 int bimamba_time_chunks(const bimamba_desc* desc);
 
+/* ---- What stands around the mixers of a denoiser: token table, layer norm, log probabilities, clipped gradients ----
+ *
+ * The calls below share the rules above (host validation, caller's memory and stream, nothing allocated or kept) and these:
+ * rows are (batch, token) pairs, batch * seqlen < 2^31; views read have any non-negative strides (0 repeats a row), rows of a
+ * view written must lie apart from each other and from everything read (BIMAMBA_ERR_ALIAS), but where a call allows the very
+ * same view; all sums, statistics and parameter gradients are fp32 or wider and formed in a fixed order: the same inputs give
+ * the same bits.  Activations need be aligned to their element only.  No call records a memset node. */
+
+/* Token ids [batch, seqlen] in device memory: id (b, t) at ptr + b*stride_batch + t*stride_token, 8-byte aligned. */
+typedef struct bimamba_tokens {
+    const int64_t* ptr;
+    int64_t stride_batch;
+    int64_t stride_token;
+} bimamba_tokens;
+
+/* Host struct.  vocab < 2^21, d_model <= 2^20; scale finite. */
+typedef struct bimamba_embed_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_embed_desc), checked */
+    int32_t batch;          /* >= 0 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t d_model;
+    int32_t vocab;
+    int32_t table_dtype;    /* bimamba_dtype of the table (the table's gradient is fp32 whatever it is) */
+    int32_t io_dtype;       /* bimamba_dtype of out and dout */
+    float scale;
+} bimamba_embed_desc;
+
+/* out[b, t, :] = scale * table[id(b, t), :], one rounding; table [vocab, d_model] contiguous.  An id outside [0, vocab) gives a
+ * row of zeros. */
+int bimamba_embed(const bimamba_embed_desc* desc, const bimamba_tokens* tokens, const void* table, const bimamba_tensor* out,
+                  void* hip_stream);
+
+/* dtable[v, :] = scale * sum of dout[b, t, :] over the places with id v; fp32 [vocab, d_model] contiguous, every row is written
+ * (rows of ids that do not occur: zeros).  Ids outside [0, vocab) count nowhere.
+ *   workspace   at least bimamba_embed_bwd_workspace_bytes(desc) bytes, 16-byte aligned. */
+int bimamba_embed_bwd(const bimamba_embed_desc* desc, const bimamba_tokens* tokens, const bimamba_tensor* dout, float* dtable,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t bimamba_embed_bwd_workspace_bytes(const bimamba_embed_desc* desc);
+
+/* Host struct.  eps > 0. */
+typedef struct bimamba_norm_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_norm_desc), checked */
+    int32_t batch;          /* >= 0, <= 65535 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t d_model;        /* <= 65536 */
+    int32_t io_dtype;       /* bimamba_dtype of x, y, dy, dx */
+    float eps;
+} bimamba_norm_desc;
+
+/* Layer norm of every row: y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps).
+ *   weight, bias    fp32, unit stride, or NULL (1 and 0).  weight_stride 0: one vector [d_model] for all rows; >= d_model: batch
+ *                   element b has its own at + b * weight_stride (AdaLN; both may be column slices of one projection output).
+ *   mean, rstd      fp32 [batch, seqlen] contiguous, or NULL (not wanted; the gradients take them). */
+int bimamba_layer_norm(const bimamba_norm_desc* desc, const bimamba_tensor* x, const float* weight, const float* bias,
+                       int64_t weight_stride, const bimamba_tensor* y, float* mean, float* rstd, void* hip_stream);
+
+/* Its gradients.  With xh = (x - mean) * rstd and g = dy * weight: dx = rstd * (g - mean(g) - xh * mean(g * xh));
+ * dweight = sum of dy * xh and dbias = sum of dy over the rows that share the vector: fp32 [batch, d_model] contiguous, or
+ * [d_model] with weight_stride 0; NULL: not wanted.
+ *   workspace   at least bimamba_layer_norm_bwd_workspace_bytes(desc, weight_stride != 0) bytes, 16-byte aligned; may be NULL if
+ *               neither dweight nor dbias is wanted. */
+int bimamba_layer_norm_bwd(const bimamba_norm_desc* desc, const bimamba_tensor* x, const float* weight, int64_t weight_stride,
+                           const float* mean, const float* rstd, const bimamba_tensor* dy, const bimamba_tensor* dx,
+                           float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t bimamba_layer_norm_bwd_workspace_bytes(const bimamba_norm_desc* desc, int per_batch);
+
+/* Host struct.  0 <= top_k <= 8, top_k <= vocab. */
+typedef struct bimamba_logits_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_logits_desc), checked */
+    int32_t batch;          /* >= 0 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t vocab;
+    int32_t io_dtype;       /* bimamba_dtype of the logits and their gradient */
+    int32_t top_k;          /* alternatives wanted per row */
+    int32_t targets_only;   /* 0 or 1: rows without a target are not read (training on masked places); all they get are zeros,
+                               and -1 for tokens */
+} bimamba_logits_desc;
+
+/* What is wanted of a call's rows, device pointers, contiguous; NULL: not wanted.
+ *   logp       fp32 [batch, seqlen]          log probability of the target; 0 without one (id outside [0, vocab))
+ *   lse        fp32 [batch, seqlen]          log of the sum of exp(logits)
+ *   entropy    fp32 [batch, seqlen]          -sum p log p
+ *   top_logp   fp32 [batch, seqlen, top_k]   the largest log probabilities, in descending order
+ *   top_token  int64 [batch, seqlen, top_k]  and their ids; of equal logits the lowest id comes first */
+typedef struct bimamba_scores {
+    float* logp;
+    float* lse;
+    float* entropy;
+    float* top_logp;
+    int64_t* top_token;
+} bimamba_scores;
+
+/*
+ * Log probabilities of given tokens under softmax(logits), with the entropy and the most probable tokens of every row.
+ *   logits   [batch, seqlen, vocab].  -inf (and the type's lowest value) are masks: probability 0.  A row of nothing but -inf has
+ *            lse -inf, logp -inf, entropy 0, alternatives 0, 1, ... with -inf.  A NaN or +inf makes a row's values NaN and its
+ *            alternatives -1.
+ *   targets  NULL: none (then out->logp must be NULL and targets_only 0).
+ *   workspace   at least bimamba_log_probs_workspace_bytes(desc) bytes, 16-byte aligned (may be NULL if 0).
+ */
+int bimamba_log_probs(const bimamba_logits_desc* desc, const bimamba_tensor* logits, const bimamba_tokens* targets,
+                      const bimamba_scores* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t bimamba_log_probs_workspace_bytes(const bimamba_logits_desc* desc);
+
+/* Gradient for the logits: dlogits_v = dlogp * (1[v = target] - p_v) - dentropy * p_v * (log p_v + entropy).
+ *   lse, entropy      what bimamba_log_probs gave (entropy: required with dentropy).
+ *   dlogp, dentropy   fp32 [batch, seqlen] contiguous; either may be NULL (0), dlogp is taken as 0 where there is no target.
+ *   dlogits           may be the very view of the logits (same pointer and strides): the gradient takes their place.
+ * Rows whose two gradients are 0, and rows of nothing but -inf, get zeros and are not read.  (desc's top_k and targets_only are
+ * not used.) */
+int bimamba_log_probs_bwd(const bimamba_logits_desc* desc, const bimamba_tensor* logits, const bimamba_tokens* targets,
+                          const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                          const bimamba_tensor* dlogits, void* hip_stream);
+
+/* One gradient tensor of a clipping call: count elements at `from`, contiguous; the scaled ones go to `to`, which is `from`
+ * itself or memory apart from every tensor. */
+typedef struct bimamba_grad {
+    const void* from;
+    void* to;
+    int64_t count;
+    int64_t first;          /* filled by bimamba_clip_layout */
+    int32_t dtype;          /* bimamba_dtype */
+    int32_t reserved;       /* 0 */
+} bimamba_grad;
+
+/* Fills `first` of a host table of n tensors.  BIMAMBA_OK or an error (a table that bimamba_clip_grads would refuse). */
+int bimamba_clip_layout(bimamba_grad* table, int n);
+
+/*
+ * Clipping by the global norm: norm = sqrt(sum of squares of all tensors), to = from * min(1, max_norm / norm).
+ *   table, table_dev   host array of n tensors that bimamba_clip_layout has filled, and a copy of it in device memory, 8-byte
+ *                      aligned, which stays until the work has run.
+ *   max_norm           >= 0; +inf: the norm alone, gradients as they are.
+ *   norm               fp32, one value on the device, or NULL.  Squares are summed in 64 bits, so they neither overflow nor vanish.
+ *   workspace          at least bimamba_clip_grads_workspace_bytes(table, n) bytes, 16-byte aligned.
+ * A norm that is not finite leaves the gradients as they are (`to` gets copies); the caller sees it in `norm` and skips the step.
+ */
+int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, float max_norm, float* norm, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+size_t bimamba_clip_grads_workspace_bytes(const bimamba_grad* table, int n);
+
 /* Benchmark diagnostics: arm a one-shot probe on the calling host thread.  The next bimamba_fwd or
  * bimamba_block_fwd made by this thread records ev_start immediately before and ev_stop immediately after its
  * scan-and-combine kernel (on the chunked matrix-core path: around its two launches, one per direction; never the

@@ -24,7 +24,10 @@ STATIC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = ("bimamba_fwd", "bimamba_block_fwd", "bimamba_block_fwd_static", "bimamba_block_stack", "bimamba_block_stack_form",
            "bimamba_block_stack_side_by_side", "bimamba_copy_inputs", "bimamba_bwd", "bimamba_workspace_bytes",
-           "bimamba_bwd_workspace_bytes", "bimamba_time_chunks", "bimamba_profile_next_call", "bimamba_status_string", "bimamba_version")
+           "bimamba_bwd_workspace_bytes", "bimamba_time_chunks", "bimamba_profile_next_call", "bimamba_status_string", "bimamba_version",
+           "bimamba_embed", "bimamba_embed_bwd", "bimamba_embed_bwd_workspace_bytes", "bimamba_layer_norm", "bimamba_layer_norm_bwd",
+           "bimamba_layer_norm_bwd_workspace_bytes", "bimamba_log_probs", "bimamba_log_probs_bwd", "bimamba_log_probs_workspace_bytes",
+           "bimamba_clip_layout", "bimamba_clip_grads", "bimamba_clip_grads_workspace_bytes")
 
 
 class Desc(C.Structure):
@@ -55,6 +58,33 @@ class InputGrads(C.Structure):
 
 class ParamGrads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("dconv_w", "dconv_b", "dA", "dD", "ddt_bias")]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_batch", C.c_int64), ("stride_token", C.c_int64)]
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "batch", "seqlen", "d_model", "vocab", "table_dtype", "io_dtype")] + [("scale", C.c_float)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("batch", "seqlen", "d_model", "io_dtype")] + [("eps", C.c_float)]
+
+
+class LogitsDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "batch", "seqlen", "vocab", "io_dtype", "top_k", "targets_only")]
+
+
+class Scores(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logp", "lse", "entropy", "top_logp", "top_token")]
+
+
+class Grad(C.Structure):
+    _fields_ = [("from_", C.c_void_p), ("to", C.c_void_p), ("count", C.c_int64), ("first", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class BimambaError(RuntimeError):
@@ -109,6 +139,22 @@ def lib():
         L.bimamba_version.restype = C.c_int
         L.bimamba_profile_next_call.restype = None
         L.bimamba_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
+        P, V, Z, I = C.POINTER, C.c_void_p, C.c_size_t, C.c_int
+        for name, res, args in (
+                ("bimamba_embed", I, [P(EmbedDesc), P(Tokens), V, P(Tensor), V]),
+                ("bimamba_embed_bwd", I, [P(EmbedDesc), P(Tokens), P(Tensor), V, V, Z, V]),
+                ("bimamba_embed_bwd_workspace_bytes", Z, [P(EmbedDesc)]),
+                ("bimamba_layer_norm", I, [P(NormDesc), P(Tensor), V, V, C.c_int64, P(Tensor), V, V, V]),
+                ("bimamba_layer_norm_bwd", I, [P(NormDesc), P(Tensor), V, C.c_int64, V, V, P(Tensor), P(Tensor), V, V, V, Z, V]),
+                ("bimamba_layer_norm_bwd_workspace_bytes", Z, [P(NormDesc), I]),
+                ("bimamba_log_probs", I, [P(LogitsDesc), P(Tensor), P(Tokens), P(Scores), V, Z, V]),
+                ("bimamba_log_probs_bwd", I, [P(LogitsDesc), P(Tensor), P(Tokens), V, V, V, V, P(Tensor), V]),
+                ("bimamba_log_probs_workspace_bytes", Z, [P(LogitsDesc)]),
+                ("bimamba_clip_layout", I, [P(Grad), I]),
+                ("bimamba_clip_grads", I, [P(Grad), I, V, C.c_float, V, V, Z, V]),
+                ("bimamba_clip_grads_workspace_bytes", Z, [P(Grad), I])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
         _lib = L
     return _lib
 
@@ -290,6 +336,199 @@ def bimamba_copy_inputs(desc, src, dst, stream=None, check=True):
     rc = lib().bimamba_copy_inputs(C.byref(desc), C.byref(src), C.byref(dst), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_copy_inputs")
+    return rc
+
+
+# ---- what stands around the mixers: token table, layer norm, log probabilities, clipped gradients ----
+#
+# These take the tensors themselves and check them against the descriptor: shape, type, unit stride along a row.  Tensors of a call are
+# on the current device, and the stream is the current one unless another is given.
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_TORCH = (torch.float32, torch.bfloat16)
+_NAMES = {"f32": F32, "bf16": BF16}
+
+
+def _rows(t, what, dtype, *shape):
+    """[batch, L, width] activations -> Tensor."""
+    assert t.dtype is dtype and tuple(t.shape) == shape and t.is_cuda, "%s: %s %s, wanted %s %s on the GPU" % (
+        what, t.dtype, tuple(t.shape), dtype, shape)
+    s = t.stride()
+    assert s[2] == 1 or shape[2] == 1 or t.numel() == 0, "%s: the channel dimension must be contiguous" % what
+    return Tensor(t.data_ptr(), s[0], s[1])
+
+
+def _ids(t, what, *shape):
+    assert t.dtype is torch.int64 and tuple(t.shape) == shape and t.is_cuda, "%s: %s %s, wanted torch.int64 %s on the GPU" % (
+        what, t.dtype, tuple(t.shape), shape)
+    s = t.stride()
+    return Tokens(t.data_ptr(), s[0], s[1])
+
+
+def _flat(t, what, *shape, dtype=torch.float32):
+    """Contiguous device array of a shape, or None -> pointer."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and tuple(t.shape) == shape and t.is_contiguous() and t.is_cuda, "%s: %s %s, wanted contiguous %s %s on the GPU" % (
+        what, t.dtype, tuple(t.shape), dtype, shape)
+    return t.data_ptr()
+
+
+def _vector(t, what, batch, d):
+    """A parameter vector [d], or [batch, d] with unit stride along a vector -> (pointer, stride between vectors)."""
+    if t is None:
+        return None, None
+    assert t.dtype is torch.float32 and t.is_cuda and tuple(t.shape) in ((d,), (batch, d)), "%s: %s %s, wanted float32 [%d] or [%d, %d] on the GPU" % (
+        what, t.dtype, tuple(t.shape), d, batch, d)
+    assert t.stride(-1) == 1 or d == 1 or t.numel() == 0, "%s: a vector must be contiguous" % what
+    if t.dim() == 1:
+        return t.data_ptr(), 0
+    stride = t.stride(0) if batch > 1 else d
+    assert stride >= d, "%s: vectors of batch elements must not overlap" % what
+    return t.data_ptr(), stride
+
+
+def _workspace(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def make_embed_desc(batch, seqlen, d_model, vocab, table="f32", io="bf16", scale=1.0):
+    return EmbedDesc(C.sizeof(EmbedDesc), batch, seqlen, d_model, vocab, _NAMES[table], _NAMES[io], scale)
+
+
+def bimamba_embed(desc, tokens, table, out, stream=None, check=True):
+    """Enqueue out[b, t] = scale * table[tokens[b, t]].  tokens: int64 [batch, L]; table [vocab, d_model] contiguous; out
+    [batch, L, d_model]."""
+    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
+    rc = lib().bimamba_embed(C.byref(desc), C.byref(_ids(tokens, "tokens", Bt, L)),
+                             _flat(table, "table", desc.vocab, D, dtype=_TORCH[desc.table_dtype]),
+                             C.byref(_rows(out, "out", _TORCH[desc.io_dtype], Bt, L, D)), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_embed")
+    return rc
+
+
+def bimamba_embed_bwd_workspace_bytes(desc):
+    return int(lib().bimamba_embed_bwd_workspace_bytes(C.byref(desc)))
+
+
+def bimamba_embed_bwd(desc, tokens, dout, dtable, workspace, stream=None, check=True):
+    """Enqueue the gradient of the table: dtable float32 [vocab, d_model] contiguous, overwritten."""
+    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
+    rc = lib().bimamba_embed_bwd(C.byref(desc), C.byref(_ids(tokens, "tokens", Bt, L)),
+                                 C.byref(_rows(dout, "dout", _TORCH[desc.io_dtype], Bt, L, D)),
+                                 _flat(dtable, "dtable", desc.vocab, D), *_workspace(workspace), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_embed_bwd")
+    return rc
+
+
+def make_norm_desc(batch, seqlen, d_model, io="bf16", eps=1e-5):
+    return NormDesc(C.sizeof(NormDesc), batch, seqlen, d_model, _NAMES[io], eps)
+
+
+def bimamba_layer_norm(desc, x, weight, bias, y, mean=None, rstd=None, stream=None, check=True):
+    """Enqueue the layer norm of every row.  weight, bias: float32 [d_model], or [batch, d_model] with a vector for each batch
+    element, or None; both of the same kind and row stride.  mean, rstd: float32 [batch, L] or None (bimamba_layer_norm_bwd takes them)."""
+    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
+    io = _TORCH[desc.io_dtype]
+    w, ws = _vector(weight, "weight", Bt, D)
+    b, bs = _vector(bias, "bias", Bt, D)
+    assert ws is None or bs is None or ws == bs, "weight and bias: not of the same kind and stride"
+    rc = lib().bimamba_layer_norm(C.byref(desc), C.byref(_rows(x, "x", io, Bt, L, D)), w, b, bs or 0 if ws is None else ws,
+                                  C.byref(_rows(y, "y", io, Bt, L, D)), _flat(mean, "mean", Bt, L), _flat(rstd, "rstd", Bt, L),
+                                  _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_layer_norm")
+    return rc
+
+
+def bimamba_layer_norm_bwd_workspace_bytes(desc, per_batch):
+    return int(lib().bimamba_layer_norm_bwd_workspace_bytes(C.byref(desc), int(per_batch)))
+
+
+def bimamba_layer_norm_bwd(desc, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, stream=None, check=True):
+    """Enqueue the gradients of bimamba_layer_norm.  dweight, dbias: float32 [d_model], or [batch, d_model] where each batch element
+    has a vector of its own (weight None: their shape says which), or None; overwritten."""
+    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
+    io = _TORCH[desc.io_dtype]
+    w, ws = _vector(weight, "weight", Bt, D)
+    if ws is None:
+        ws = D if any(g is not None and g.dim() == 2 for g in (dweight, dbias)) else 0
+    shape = (Bt, D) if ws else (D,)
+    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), C.byref(_rows(x, "x", io, Bt, L, D)), w, ws, _flat(mean, "mean", Bt, L),
+                                      _flat(rstd, "rstd", Bt, L), C.byref(_rows(dy, "dy", io, Bt, L, D)),
+                                      C.byref(_rows(dx, "dx", io, Bt, L, D)), _flat(dweight, "dweight", *shape),
+                                      _flat(dbias, "dbias", *shape), *_workspace(workspace), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_layer_norm_bwd")
+    return rc
+
+
+def make_logits_desc(batch, seqlen, vocab, io="bf16", top_k=0, targets_only=0):
+    return LogitsDesc(C.sizeof(LogitsDesc), batch, seqlen, vocab, _NAMES[io], top_k, targets_only)
+
+
+def bimamba_log_probs_workspace_bytes(desc):
+    return int(lib().bimamba_log_probs_workspace_bytes(C.byref(desc)))
+
+
+def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, check=True):
+    """Enqueue the log probabilities of targets (int64 [batch, L], or None) under softmax(logits).  out: dict of what is wanted:
+    logp, lse, entropy float32 [batch, L]; top_logp float32 and top_token int64 [batch, L, top_k]."""
+    Bt, L, k = desc.batch, desc.seqlen, desc.top_k
+    s = Scores(_flat(out.get("logp"), "logp", Bt, L), _flat(out.get("lse"), "lse", Bt, L), _flat(out.get("entropy"), "entropy", Bt, L),
+               _flat(out.get("top_logp"), "top_logp", Bt, L, k), _flat(out.get("top_token"), "top_token", Bt, L, k, dtype=torch.int64))
+    rc = lib().bimamba_log_probs(C.byref(desc), C.byref(_rows(logits, "logits", _TORCH[desc.io_dtype], Bt, L, desc.vocab)),
+                                 None if targets is None else C.byref(_ids(targets, "targets", Bt, L)), C.byref(s),
+                                 *_workspace(workspace), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_log_probs")
+    return rc
+
+
+def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
+    """Enqueue the gradient for the logits, given those of logp and of the entropy (float32 [batch, L]; either None).  dlogits may be
+    logits itself."""
+    Bt, L = desc.batch, desc.seqlen
+    io = _TORCH[desc.io_dtype]
+    rc = lib().bimamba_log_probs_bwd(C.byref(desc), C.byref(_rows(logits, "logits", io, Bt, L, desc.vocab)),
+                                     None if targets is None else C.byref(_ids(targets, "targets", Bt, L)), _flat(lse, "lse", Bt, L),
+                                     _flat(entropy, "entropy", Bt, L), _flat(dlogp, "dlogp", Bt, L), _flat(dentropy, "dentropy", Bt, L),
+                                     C.byref(_rows(dlogits, "dlogits", io, Bt, L, desc.vocab)), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_log_probs_bwd")
+    return rc
+
+
+class GradTable:
+    """The tensors of a clipping call, made once: where each gradient lies and where the scaled one goes (to None: in place).  Holds the
+    tensors and the table's copy on the device."""
+
+    def __init__(self, grads, to=None):
+        self.grads, self.to = list(grads), list(grads if to is None else to)
+        assert len(self.grads) == len(self.to)
+        for g, t in zip(self.grads, self.to):
+            assert g.dtype in _DTYPES and t.dtype is g.dtype and t.shape == g.shape, "a gradient and where it goes: one shape and type"
+            assert g.is_contiguous() and t.is_contiguous() and g.is_cuda and t.device == g.device, "gradients: contiguous, on one GPU"
+        self.n = len(self.grads)
+        self.host = (Grad * self.n)(*[Grad(g.data_ptr(), t.data_ptr(), g.numel(), 0, _DTYPES[g.dtype], 0) for g, t in zip(self.grads, self.to)])
+        rc = lib().bimamba_clip_layout(self.host, self.n)
+        if rc != 0:
+            raise BimambaError(rc, "bimamba_clip_layout")
+        self.dev = torch.frombuffer(bytearray(self.host), dtype=torch.uint8).to(self.grads[0].device) if self.n else None
+
+
+def bimamba_clip_grads_workspace_bytes(table):
+    return int(lib().bimamba_clip_grads_workspace_bytes(table.host, table.n))
+
+
+def bimamba_clip_grads(table, max_norm, norm, workspace, stream=None, check=True):
+    """Enqueue the norm of a GradTable's gradients (norm: float32 [1], or None) and their scaling to at most max_norm."""
+    rc = lib().bimamba_clip_grads(table.host, table.n, None if table.dev is None else table.dev.data_ptr(), max_norm,
+                                  _flat(norm, "norm", 1), *_workspace(workspace), _stream_ptr(stream))
+    if check and rc != 0:
+        raise BimambaError(rc, "bimamba_clip_grads")
     return rc
 
 

@@ -1,0 +1,196 @@
+// The norm of many gradient tensors, and the tensors scaled so that it is at most a given one.
+#include "model_ops.h"
+
+namespace bm {
+
+// All tensors are cut into pieces of 8192 elements, numbered through; a workgroup takes a run of them, finds the tensor of its first
+// one by binary search and steps on from there.  Two launches: the squares' sums, 64 bits each, one a workgroup; then every
+// workgroup adds up all of these in the same order, which gives it the norm, and scales its run.  The second launch walks backwards, so
+// that it starts with what the first has left in the caches.
+constexpr int kClipThreads = 256, kClipPiece = 8192;
+constexpr int kClipSteps = kClipPiece / (kClipThreads * kPiece);
+struct ClipArgs {
+    const bimamba_grad* table;
+    long long pieces, per_group;
+    int n;
+    float max_norm;
+    float* norm;
+    double* sums;
+};
+
+// Index of the last tensor that starts at or before a piece (empty ones start where the next does).
+__device__ __forceinline__ int tensor_of(const ClipArgs& a, long long piece)
+{
+    int lo = 0, hi = a.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.table[mid].first <= piece) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <typename IO>
+__device__ __forceinline__ double piece_squares(const typename IO::T* from, int n)
+{
+    double s = 0.0;
+    Piece<IO> p[kClipSteps];
+#pragma unroll
+    for (int k = 0; k < kClipSteps; k++) {
+        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
+        p[k] = load_piece_of<IO>(from, at, n, typename IO::T(0));
+    }
+#pragma unroll
+    for (int k = 0; k < kClipSteps; k++)
+#pragma unroll
+        for (int i = 0; i < kPiece; i++) {
+            const double v = p[k][i];
+            s += v * v;
+        }
+    return s;
+}
+template <typename IO>
+__device__ __forceinline__ void piece_scaled(const typename IO::T* from, typename IO::T* to, int n, float scale)
+{
+    Piece<IO> p[kClipSteps];
+#pragma unroll
+    for (int k = 0; k < kClipSteps; k++) {
+        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
+        if (at < n) p[k] = load_piece_of<IO>(from, at, n, typename IO::T(0));
+    }
+#pragma unroll
+    for (int k = 0; k < kClipSteps; k++) {
+        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
+        float f[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; i++) f[i] = scale == 1.0f ? p[k][i] : p[k][i] * scale;
+        if (at < n) store_piece_of<IO>(to, at, n, f);
+    }
+}
+
+// The sum over a workgroup, the same in all lanes.
+__device__ __forceinline__ double workgroup_sum(double v)
+{
+    __shared__ double part[kClipThreads / 64];
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipArgs a)
+{
+    const long long p0 = blockIdx.x * a.per_group, p1 = min(p0 + a.per_group, a.pieces);
+    double s = 0.0;
+    int i = p0 < p1 ? tensor_of(a, p0) : 0;
+    for (long long p = p0; p < p1; p++) {
+        while (i + 1 < a.n && a.table[i + 1].first <= p) i++;
+        const bimamba_grad g = a.table[i];
+        const long long at = (p - g.first) * kClipPiece;
+        const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
+        if (g.dtype == BIMAMBA_BF16) s += piece_squares<IoBF16>(static_cast<const unsigned short*>(g.from) + at, n);
+        else s += piece_squares<IoF32>(static_cast<const float*>(g.from) + at, n);
+    }
+    s = workgroup_sum(s);
+    if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(const ClipArgs a)
+{
+    double s = 0.0;
+    for (unsigned k = threadIdx.x; k < gridDim.x; k += kClipThreads) s += a.sums[k];
+    s = workgroup_sum(s);
+    const double norm = sqrt(s);
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+    // (a norm that is not finite in 32 bits compares false or is taken out here)
+    const float scale = isfinite((float)norm) && norm > (double)a.max_norm ? (float)((double)a.max_norm / norm) : 1.0f;
+    const unsigned group = gridDim.x - 1 - blockIdx.x;
+    const long long p0 = group * a.per_group, p1 = min(p0 + a.per_group, a.pieces);
+    if (p0 >= p1) return;
+    int i = tensor_of(a, p1 - 1);
+    for (long long p = p1 - 1; p >= p0; p--) {
+        while (i > 0 && a.table[i].first > p) i--;
+        const bimamba_grad g = a.table[i];
+        if (scale == 1.0f && g.from == g.to) continue;
+        const long long at = (p - g.first) * kClipPiece;
+        const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
+        if (g.dtype == BIMAMBA_BF16)
+            piece_scaled<IoBF16>(static_cast<const unsigned short*>(g.from) + at, static_cast<unsigned short*>(g.to) + at, n, scale);
+        else piece_scaled<IoF32>(static_cast<const float*>(g.from) + at, static_cast<float*>(g.to) + at, n, scale);
+    }
+}
+
+namespace {
+
+// Pieces of a table, or an error; `first` is checked against where the tensors before end, or filled.
+int clip_pieces(const bimamba_grad* table, bimamba_grad* fill, int n, long long* pieces)
+{
+    if (n < 0) return BIMAMBA_ERR_BAD_SHAPE;
+    if (n > 0 && !table) return BIMAMBA_ERR_NULL_POINTER;
+    long long p = 0;
+    for (int i = 0; i < n; i++) {
+        const bimamba_grad& g = table[i];
+        if (g.count < 0 || g.reserved != 0) return BIMAMBA_ERR_BAD_SHAPE;
+        if (!known_dtype(g.dtype) || g.count > 1ll << 40) return BIMAMBA_ERR_UNSUPPORTED;
+        const size_t elem = dtype_bytes(g.dtype);
+        if (g.count > 0) {
+            if (!g.from || !g.to) return BIMAMBA_ERR_NULL_POINTER;
+            if (!aligned_to(g.from, elem) || !aligned_to(g.to, elem)) return BIMAMBA_ERR_MISALIGNED;
+            if (g.from != g.to && meet(bytes_of(g.from, g.count, elem), bytes_of(g.to, g.count, elem))) return BIMAMBA_ERR_ALIAS;
+        }
+        if (fill) fill[i].first = p;
+        else if (g.first != p) return BIMAMBA_ERR_BAD_SHAPE;
+        p += (g.count + kClipPiece - 1) / kClipPiece;
+    }
+    *pieces = p;
+    return BIMAMBA_OK;
+}
+
+unsigned clip_groups(long long pieces)
+{
+    const long long most = 8ll * cu_count();   // what the chip holds at once
+    return (unsigned)(pieces < 1 ? 1 : pieces < most ? pieces : most);
+}
+
+}  // namespace
+}  // namespace bm
+
+using namespace bm;
+
+extern "C" {
+
+int bimamba_clip_layout(bimamba_grad* table, int n)
+{
+    long long pieces;
+    return clip_pieces(table, table, n, &pieces);
+}
+
+size_t bimamba_clip_grads_workspace_bytes(const bimamba_grad* table, int n)
+{
+    long long pieces;
+    return clip_pieces(table, nullptr, n, &pieces) ? 0 : clip_groups(pieces) * sizeof(double);
+}
+
+int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, float max_norm, float* norm, void* workspace,
+                       size_t workspace_bytes, void* hip_stream)
+{
+    long long pieces;
+    int rc = clip_pieces(table, nullptr, n, &pieces);
+    if (rc) return rc;
+    if (!(max_norm >= 0.0f)) return BIMAMBA_ERR_BAD_SHAPE;
+    if (n > 0 && !table_dev) return BIMAMBA_ERR_NULL_POINTER;
+    if (!aligned_to(table_dev, 8) || !aligned_to(norm, 4)) return BIMAMBA_ERR_MISALIGNED;
+    const unsigned groups = clip_groups(pieces);
+    if ((rc = check_workspace(workspace, workspace_bytes, groups * sizeof(double)))) return rc;
+    ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, (pieces + groups - 1) / groups, n, max_norm, norm,
+               static_cast<double*>(workspace)};
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    const Launches launches;
+    hipLaunchKernelGGL(clip_squares_kernel, dim3(groups), dim3(kClipThreads), 0, st, a);
+    hipLaunchKernelGGL(clip_scale_kernel, dim3(groups), dim3(kClipThreads), 0, st, a);
+    return launches.status();
+}
+
+}  // extern "C"

@@ -1,0 +1,464 @@
+// Log probabilities of given tokens, entropies and the most probable tokens of rows of logits, and their gradient.
+#include "model_ops.h"
+
+#include <cfloat>
+
+namespace bm {
+
+constexpr int kMaxTop = 8, kMaxSplits = 64;
+constexpr float kFarBelow = -1e4f;   // a difference of logits whose exponential is 0: stands for all that lie lower, -inf among them
+
+// One pass over a row.  A lane keeps of the logits x it has seen the largest (m), S = sum exp(x - m) and, for the entropy,
+// T = sum exp(x - m) (x - m); then lse = m + log S and H = log S - T / S, no value of which is large where the row is confident.  To a
+// larger maximum m' both move by r = exp(m - m'): S' = r S, T' = r (T + S (m - m')).  m starts at the lowest finite value, so a row of
+// nothing but -inf keeps S = 0, and a NaN or +inf makes S a NaN.
+struct Stats {
+    float m, s, t;
+};
+template <bool kEntropy>
+__device__ __forceinline__ void move_to(Stats& a, float m)
+{
+    const float d = a.m - m, r = fast_exp2(d * kLog2e);
+    if constexpr (kEntropy) a.t = r * (a.t + a.s * fmaxf(d, kFarBelow));
+    a.s *= r;
+    a.m = m;
+}
+
+// The order of the alternatives as whole numbers: a larger logit first, of equal ones (-0 and 0 among them) the lower id.  0: none.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key key_of(float v, unsigned id)
+{
+    const unsigned u = __float_as_uint(v + 0.0f), ordered = u & 0x80000000u ? ~u : u | 0x80000000u;
+    return (Key)ordered << 32 | ~id;
+}
+__device__ __forceinline__ float value_of(Key k)
+{
+    const unsigned o = (unsigned)(k >> 32);
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ unsigned id_of(Key k) { return ~(unsigned)k; }
+__device__ __forceinline__ Key wave_max_key(Key k)
+{
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2) {
+        const Key other = __shfl_xor(k, step);
+        if (other > k) k = other;
+    }
+    return k;
+}
+
+struct ScoresArgs {
+    RowView logits;
+    const int64_t* ids;   // or null
+    long long ids_sb, ids_st;
+    float *logp, *lse, *entropy, *top_logp;
+    int64_t* top_token;
+    Stats* part;          // [rows][splits], and the parts' own alternatives [rows][splits][top_k], where a row is split
+    Key* part_top;
+    unsigned rows, L;
+    int vocab, top_k, splits, per_split, targets_only;
+};
+
+__device__ __forceinline__ long long target_of(const ScoresArgs& a, unsigned b, unsigned t)
+{
+    if (!a.ids) return -1;
+    const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
+    return id >= 0 && id < a.vocab ? id : -1;
+}
+// A row that is not asked for.
+__device__ __forceinline__ void store_nothing(const ScoresArgs& a, unsigned row)
+{
+    if (a.logp) a.logp[row] = 0.0f;
+    if (a.lse) a.lse[row] = 0.0f;
+    if (a.entropy) a.entropy[row] = 0.0f;
+    for (int k = 0; k < a.top_k; k++) {
+        if (a.top_logp) a.top_logp[(long long)row * a.top_k + k] = 0.0f;
+        if (a.top_token) a.top_token[(long long)row * a.top_k + k] = -1;
+    }
+}
+__device__ __forceinline__ void store_stats(const ScoresArgs& a, unsigned row, const Stats& s, long long target, float x)
+{
+    const float log_s = logf(s.s);   // (-inf for a row of nothing but -inf)
+    if (a.logp) a.logp[row] = target < 0 ? 0.0f : s.s == 0.0f ? -INFINITY : (x - s.m) - log_s;
+    if (a.lse) a.lse[row] = s.m + log_s;
+    if (a.entropy) a.entropy[row] = s.s == 0.0f ? 0.0f : log_s - s.t / s.s;
+}
+__device__ __forceinline__ void store_top(const ScoresArgs& a, unsigned row, int k, const Stats& s, Key key)
+{
+    const bool none = !(s.s == s.s);
+    if (a.top_logp)
+        a.top_logp[(long long)row * a.top_k + k] = none ? s.s : s.s == 0.0f ? -INFINITY : (value_of(key) - s.m) - logf(s.s);
+    if (a.top_token) a.top_token[(long long)row * a.top_k + k] = none ? -1 : (int64_t)id_of(key);
+}
+
+// A workgroup takes a row, or one of its `splits` parts where there are few rows.  With kTop a lane also keeps which of its pieces of
+// eight first had the largest logit.  The best pieces of the lanes are all different, so the k lanes with the best of them hold
+// the k best logits of the row: these lanes' pieces alone are read again (from the caches), spread over all lanes, k times for the
+// best logit below the one before.
+constexpr int kScoresThreads = 256, kScoresWaves = kScoresThreads / 64, kScoresAhead = 4;
+template <typename IO, bool kEntropy, bool kTop>
+__global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs a)
+{
+    const unsigned row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
+    const unsigned b = row / a.L, t = row - b * a.L;
+    const long long target = target_of(a, b, t);
+    if (a.targets_only && target < 0) {
+        if (split == 0 && threadIdx.x == 0) store_nothing(a, row);
+        return;
+    }
+    typedef typename IO::T T;
+    const int from = split * a.per_split, n = min(a.per_split, a.vocab - from), pieces = (n + kPiece - 1) / kPiece;
+    const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t) + from;
+    const T lowest = io_value<IO>(-INFINITY);
+    Stats s{-FLT_MAX, 0.0f, 0.0f};
+    float best = -INFINITY;
+    unsigned best_piece = ~0u;
+    for (int first = threadIdx.x; first < pieces; first += kScoresThreads * kScoresAhead) {
+        Piece<IO> p[kScoresAhead];
+#pragma unroll
+        for (int j = 0; j < kScoresAhead; j++)
+            if (first + j * kScoresThreads < pieces) p[j] = load_piece_of<IO>(x, (first + j * kScoresThreads) * kPiece, n, lowest);
+#pragma unroll
+        for (int j = 0; j < kScoresAhead; j++) {
+            const int piece = first + j * kScoresThreads;
+            if (piece < pieces) {
+                float m = p[j][0];
+#pragma unroll
+                for (int i = 1; i < kPiece; i++) m = fmaxf(m, p[j][i]);
+                if constexpr (kTop) {
+                    if (m > best || best_piece == ~0u) {
+                        best = m;
+                        best_piece = piece;
+                    }
+                }
+                move_to<kEntropy>(s, fmaxf(s.m, m));
+#pragma unroll
+                for (int i = 0; i < kPiece; i++) {
+                    const float d = p[j][i] - s.m, e = fast_exp2(d * kLog2e);
+                    s.s += e;
+                    if constexpr (kEntropy) s.t += e * fmaxf(d, kFarBelow);
+                }
+            }
+        }
+    }
+    // over the workgroup
+    __shared__ Stats part[kScoresWaves];
+    __shared__ Key wave_key[kScoresWaves * kMaxTop], best_key[kScoresWaves];
+    __shared__ int chosen[kMaxTop], n_chosen;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    move_to<kEntropy>(s, wave_max(s.m));
+    s.s = wave_sum(s.s);
+    if constexpr (kEntropy) s.t = wave_sum(s.t);
+    if (lane == 0) part[wave] = s;
+    Key mine = 0;
+    if constexpr (kTop) {
+        mine = best_piece == ~0u ? 0 : key_of(best, best_piece * kPiece);
+        Key left = mine;
+        for (int k = 0; k < a.top_k; k++) {
+            const Key top = wave_max_key(left);
+            if (left == top) left = 0;
+            if (lane == 0) wave_key[wave * a.top_k + k] = top;
+        }
+        if (threadIdx.x == 0) n_chosen = 0;
+    }
+    __syncthreads();
+    s = part[0];
+#pragma unroll
+    for (int w = 1; w < kScoresWaves; w++) s.m = fmaxf(s.m, part[w].m);
+    {
+        Stats all{s.m, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kScoresWaves; w++) {
+            Stats q = part[w];
+            move_to<kEntropy>(q, all.m);
+            all.s += q.s;
+            all.t += q.t;
+        }
+        s = all;
+    }
+    const bool whole = a.splits == 1;
+    if (threadIdx.x == 0) {
+        if (whole) store_stats(a, row, s, target, target < 0 ? 0.0f : IO::cvt(x[target]));
+        else a.part[blockIdx.x] = s;
+    }
+    if constexpr (kTop) {
+        // the k-th best of the lanes' best pieces
+        Key threshold = 0;
+        {
+            const int count = kScoresWaves * a.top_k;
+            const Key own = lane < count ? wave_key[lane] : 0;
+            int above = 0;
+            for (int j = 0; j < count; j++) above += wave_key[j] > own;
+            const unsigned long long at = __ballot(lane < count && above == a.top_k - 1);
+            if (at) threshold = __shfl(own, __builtin_ctzll(at));
+        }
+        if (mine != 0 && mine >= threshold) chosen[atomicAdd(&n_chosen, 1)] = threadIdx.x;   // (top_k of them at most)
+        __syncthreads();
+        const int rounds = (pieces + kScoresThreads - 1) / kScoresThreads, items = n_chosen * rounds;
+        Key below = ~0ull;
+        for (int k = 0; k < a.top_k; k++) {
+            Key top = 0;
+            for (int item = threadIdx.x; item < items; item += kScoresThreads) {
+                const int which = item / rounds, piece = (item - which * rounds) * kScoresThreads + chosen[which];
+                if (piece < pieces) {
+                    const Piece<IO> p = load_piece_of<IO>(x, piece * kPiece, n, lowest);
+#pragma unroll
+                    for (int i = 0; i < kPiece; i++) {
+                        const Key key = piece * kPiece + i < n ? key_of(p[i], from + piece * kPiece + i) : 0;
+                        if (key < below && key > top) top = key;
+                    }
+                }
+            }
+            top = wave_max_key(top);
+            __syncthreads();
+            if (lane == 0) best_key[wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kScoresWaves; w++) top = best_key[w] > top ? best_key[w] : top;
+            below = top;
+            if (threadIdx.x == 0) {
+                if (whole) store_top(a, row, k, s, top);
+                else a.part_top[(long long)blockIdx.x * a.top_k + k] = top;
+            }
+        }
+    }
+}
+
+// A wave joins the parts of a row, a part a lane; the lanes' alternatives are in descending order already.
+template <typename IO, bool kEntropy, bool kTop>
+__global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
+{
+    const unsigned row = blockIdx.x, b = row / a.L, t = row - b * a.L;
+    const long long target = target_of(a, b, t);
+    if (a.targets_only && target < 0) return;
+    const int lane = threadIdx.x;
+    Stats s{-FLT_MAX, 0.0f, 0.0f};
+    Key top[kMaxTop] = {};
+    if (lane < a.splits) {
+        const long long at = (long long)row * a.splits + lane;
+        s = a.part[at];
+        if constexpr (kTop) {
+#pragma unroll
+            for (int k = 0; k < kMaxTop; k++)
+                if (k < a.top_k) top[k] = a.part_top[at * a.top_k + k];
+        }
+    }
+    move_to<kEntropy>(s, wave_max(s.m));
+    s.s = wave_sum(s.s);
+    if constexpr (kEntropy) s.t = wave_sum(s.t);
+    if (lane == 0) {
+        float x = 0.0f;
+        if (target >= 0) x = IO::cvt((static_cast<const typename IO::T*>(a.logits.p) + row_offset(a.logits, b, t))[target]);
+        store_stats(a, row, s, target, x);
+    }
+    if constexpr (kTop) {
+        for (int k = 0; k < a.top_k; k++) {
+            const Key best = wave_max_key(top[0]);
+            if (top[0] == best)
+#pragma unroll
+                for (int i = 0; i < kMaxTop; i++) top[i] = i + 1 < kMaxTop ? top[i + 1] : 0;
+            if (lane == 0) store_top(a, row, k, s, best);
+        }
+    }
+}
+
+// ---- gradient ----
+//
+// Elementwise, given lse and the entropy: p = exp(x - lse), dx = dlogp (1[target] - p) - dentropy p (log p + H).  A logit is read and its
+// gradient written by the same lane, so the gradient may take the logits' place.
+constexpr int kGradPieces = 4, kGradThreads = 256, kGradPart = kGradThreads * kGradPieces * kPiece;
+struct ScoresBwdArgs {
+    RowView logits, dlogits;
+    const int64_t* ids;
+    long long ids_sb, ids_st;
+    const float *lse, *entropy, *dlogp, *dentropy;
+    unsigned rows, L, parts;
+    int vocab;
+};
+template <typename IO>
+__global__ __launch_bounds__(kGradThreads) void scores_bwd_kernel(const ScoresBwdArgs a)
+{
+    typedef typename IO::T T;
+    const unsigned long long all = (unsigned long long)a.rows * a.parts;
+    for (unsigned long long w = blockIdx.x; w < all; w += gridDim.x) {
+        const unsigned row = w / a.parts, part = w - (unsigned long long)row * a.parts, b = row / a.L, t = row - b * a.L;
+        long long target = -1;
+        if (a.ids) {
+            const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
+            if (id >= 0 && id < a.vocab) target = id;
+        }
+        const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f, de = a.dentropy ? a.dentropy[row] : 0.0f;
+        const float lse = a.lse[row], h = a.dentropy ? a.entropy[row] : 0.0f;
+        const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t);
+        T* const dx = static_cast<T*>(a.dlogits.p) + row_offset(a.dlogits, b, t);
+        const int first = part * kGradPart + threadIdx.x * kPiece;
+        const auto at = [&](int k) { return first + k * kGradThreads * kPiece; };
+        if ((dl == 0.0f && de == 0.0f) || lse == -INFINITY) {
+            const float zero[kPiece] = {};
+#pragma unroll
+            for (int k = 0; k < kGradPieces; k++)
+                if (at(k) < a.vocab) store_piece_of<IO>(dx, at(k), a.vocab, zero);
+            continue;
+        }
+        Piece<IO> p[kGradPieces];
+#pragma unroll
+        for (int k = 0; k < kGradPieces; k++)
+            if (at(k) < a.vocab) p[k] = load_piece_of<IO>(x, at(k), a.vocab, T(0));
+#pragma unroll
+        for (int k = 0; k < kGradPieces; k++) {
+            if (at(k) >= a.vocab) continue;
+            float f[kPiece];
+#pragma unroll
+            for (int i = 0; i < kPiece; i++) {
+                const float d = p[k][i] - lse, e = fast_exp2(d * kLog2e);
+                f[i] = -e * (dl + de * (fmaxf(d, kFarBelow) + h));
+                if (at(k) + i == target) f[i] += dl;
+            }
+            store_piece_of<IO>(dx, at(k), a.vocab, f);
+        }
+    }
+}
+
+namespace {
+
+int check_logits(const bimamba_logits_desc* d)
+{
+    if (!d) return BIMAMBA_ERR_NULL_POINTER;
+    if (d->struct_size != sizeof(bimamba_logits_desc) || d->vocab < 1 || (d->targets_only | 1) != 1) return BIMAMBA_ERR_BAD_SHAPE;
+    if (d->top_k < 0 || d->top_k > d->vocab) return BIMAMBA_ERR_BAD_SHAPE;
+    if (const int rc = check_rows(d->batch, d->seqlen)) return rc;
+    if (!known_dtype(d->io_dtype) || d->top_k > kMaxTop || d->vocab > 1 << 30) return BIMAMBA_ERR_UNSUPPORTED;
+    return BIMAMBA_OK;
+}
+
+// Parts of a row: until four workgroups a CU exist, none of them under 2048 logits.
+struct ScoresPlan {
+    unsigned rows;
+    int splits, per_split;
+    size_t stats, total;   // bytes of the parts' statistics, and of the workspace
+};
+ScoresPlan plan_scores(const bimamba_logits_desc* d)
+{
+    ScoresPlan p{};
+    p.rows = (unsigned)((long long)d->batch * d->seqlen);
+    p.splits = 1;
+    if (p.rows > 0) {
+        const long long want = (4ll * cu_count() + p.rows - 1) / p.rows, most = d->vocab / (kScoresThreads * kPiece);
+        p.splits = (int)(want < most ? want : most);
+        if (p.splits > kMaxSplits) p.splits = kMaxSplits;
+        if (p.splits < 1) p.splits = 1;
+    }
+    p.per_split = ((d->vocab + p.splits - 1) / p.splits + kPiece - 1) / kPiece * kPiece;
+    p.splits = (d->vocab + p.per_split - 1) / p.per_split;
+    if (p.splits > 1) {
+        p.stats = ((size_t)p.rows * p.splits * sizeof(Stats) + 15) / 16 * 16;
+        p.total = p.stats + (size_t)p.rows * p.splits * d->top_k * sizeof(Key);
+    }
+    return p;
+}
+
+template <typename IO, bool kEntropy, bool kTop>
+void launch_scores(const ScoresArgs& a, hipStream_t st)
+{
+    hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop>), dim3(a.rows * (unsigned)a.splits), dim3(kScoresThreads), 0, st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((scores_join_kernel<IO, kEntropy, kTop>), dim3(a.rows), dim3(64), 0, st, a);
+}
+template <typename IO>
+void launch_scores(const ScoresArgs& a, hipStream_t st)
+{
+    const bool top = a.top_k > 0;
+    if (a.entropy && top) launch_scores<IO, true, true>(a, st);
+    else if (a.entropy) launch_scores<IO, true, false>(a, st);
+    else if (top) launch_scores<IO, false, true>(a, st);
+    else launch_scores<IO, false, false>(a, st);
+}
+
+}  // namespace
+}  // namespace bm
+
+using namespace bm;
+
+extern "C" {
+
+size_t bimamba_log_probs_workspace_bytes(const bimamba_logits_desc* d) { return check_logits(d) ? 0 : plan_scores(d).total; }
+
+int bimamba_log_probs(const bimamba_logits_desc* d, const bimamba_tensor* logits, const bimamba_tokens* targets,
+                      const bimamba_scores* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    int rc = check_logits(d);
+    if (rc) return rc;
+    if (!logits || !out) return BIMAMBA_ERR_NULL_POINTER;
+    if (!targets && (out->logp || d->targets_only)) return BIMAMBA_ERR_NULL_POINTER;
+    if ((d->top_k == 0) != (!out->top_logp && !out->top_token)) return BIMAMBA_ERR_BAD_SHAPE;
+    if (!aligned_to(out->logp, 4) || !aligned_to(out->lse, 4) || !aligned_to(out->entropy, 4) || !aligned_to(out->top_logp, 4) ||
+        !aligned_to(out->top_token, 8))
+        return BIMAMBA_ERR_MISALIGNED;
+    if (d->batch == 0 || d->seqlen == 0) return BIMAMBA_OK;
+    if (!out->logp && !out->lse && !out->entropy && d->top_k == 0) return BIMAMBA_ERR_NULL_POINTER;
+    const ScoresPlan p = plan_scores(d);
+    if ((unsigned long long)p.rows * p.splits >= 1u << 24) return BIMAMBA_ERR_UNSUPPORTED;   // (a grid holds 2^32 threads)
+    Bytes from, ids{0, 0};
+    if ((rc = check_view(logits, d->batch, d->seqlen, d->vocab, d->io_dtype, false, &from))) return rc;
+    if (targets && (rc = check_tokens(targets, d->batch, d->seqlen, &ids))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, p.total))) return rc;
+    const Bytes written[] = {bytes_of(out->logp, p.rows, 4), bytes_of(out->lse, p.rows, 4), bytes_of(out->entropy, p.rows, 4),
+                             bytes_of(out->top_logp, (long long)p.rows * d->top_k, 4), bytes_of(out->top_token, (long long)p.rows * d->top_k, 8),
+                             bytes_of(p.total ? workspace : nullptr, p.total, 1)};
+    for (int i = 0; i < 6; i++) {
+        if (meet(written[i], from) || meet(written[i], ids)) return BIMAMBA_ERR_ALIAS;
+        for (int j = 0; j < i; j++)
+            if (meet(written[i], written[j])) return BIMAMBA_ERR_ALIAS;
+    }
+    ScoresArgs a{};
+    a.logits = row_view(logits);
+    if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
+    a.logp = out->logp, a.lse = out->lse, a.entropy = out->entropy, a.top_logp = out->top_logp, a.top_token = out->top_token;
+    a.part = static_cast<Stats*>(workspace);
+    a.part_top = reinterpret_cast<Key*>(static_cast<char*>(workspace) + p.stats);
+    a.rows = p.rows, a.L = d->seqlen, a.vocab = d->vocab, a.top_k = d->top_k;
+    a.splits = p.splits, a.per_split = p.per_split, a.targets_only = d->targets_only;
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    const Launches launches;
+    if (d->io_dtype == BIMAMBA_BF16) launch_scores<IoBF16>(a, st);
+    else launch_scores<IoF32>(a, st);
+    return launches.status();
+}
+
+int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* logits, const bimamba_tokens* targets,
+                          const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                          const bimamba_tensor* dlogits, void* hip_stream)
+{
+    int rc = check_logits(d);
+    if (rc) return rc;
+    if (!logits || !dlogits) return BIMAMBA_ERR_NULL_POINTER;
+    if (d->batch == 0 || d->seqlen == 0) return BIMAMBA_OK;
+    if (!lse || (dlogp && !targets) || (dentropy && !entropy)) return BIMAMBA_ERR_NULL_POINTER;
+    const long long rows = (long long)d->batch * d->seqlen;
+    const size_t elem = dtype_bytes(d->io_dtype);
+    Bytes from, to, ids{0, 0};
+    if ((rc = check_view(logits, d->batch, d->seqlen, d->vocab, d->io_dtype, false, &from))) return rc;
+    if ((rc = check_view(dlogits, d->batch, d->seqlen, d->vocab, d->io_dtype, true, &to))) return rc;
+    if (targets && (rc = check_tokens(targets, d->batch, d->seqlen, &ids))) return rc;
+    if (!aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(dlogp, 4) || !aligned_to(dentropy, 4)) return BIMAMBA_ERR_MISALIGNED;
+    const bool same = logits->ptr == dlogits->ptr && (d->seqlen == 1 || logits->stride_token == dlogits->stride_token) &&
+                      (d->batch == 1 || logits->stride_batch == dlogits->stride_batch);
+    if (!same && views_meet(dlogits, d->vocab, to, logits, d->vocab, from, d->batch, elem, elem)) return BIMAMBA_ERR_ALIAS;
+    if (meet(to, ids)) return BIMAMBA_ERR_ALIAS;
+    for (const float* r : {lse, entropy, dlogp, dentropy})
+        if (meet(to, bytes_of(r, rows, 4))) return BIMAMBA_ERR_ALIAS;
+    ScoresBwdArgs a{};
+    a.logits = row_view(logits), a.dlogits = row_view(dlogits);
+    if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
+    a.lse = lse, a.entropy = entropy, a.dlogp = dlogp, a.dentropy = dentropy;
+    a.rows = (unsigned)rows, a.L = d->seqlen, a.vocab = d->vocab;
+    a.parts = (unsigned)((d->vocab + (long long)kGradPart - 1) / kGradPart);
+    const unsigned long long all = (unsigned long long)rows * a.parts;
+    const unsigned grid = all < 1u << 22 ? (unsigned)all : 1u << 22;
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    const Launches launches;
+    if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(scores_bwd_kernel<IoBF16>, dim3(grid), dim3(kGradThreads), 0, st, a);
+    else hipLaunchKernelGGL(scores_bwd_kernel<IoF32>, dim3(grid), dim3(kGradThreads), 0, st, a);
+    return launches.status();
+}
+
+}  // extern "C"
