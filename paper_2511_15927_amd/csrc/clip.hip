@@ -8,7 +8,6 @@ namespace bm {
 // workgroup adds up all of these in the same order, which gives it the norm, and scales its run.  The second launch walks backwards, so
 // that it starts with what the first has left in the caches.
 constexpr int kClipThreads = 256, kClipPiece = 8192;
-constexpr int kClipSteps = kClipPiece / (kClipThreads * kPiece);
 struct ClipArgs {
     const bimamba_grad* table;
     long long pieces, per_group;
@@ -30,42 +29,53 @@ __device__ __forceinline__ int tensor_of(const ClipArgs& a, long long piece)
     return lo;
 }
 
+// What a lane does with its elements of a piece, four loads in flight at a time: use(elements, where they start).  A piece of fewer elements
+// than one load takes goes an element a lane.
+constexpr int kClipAhead = 4;
+template <typename IO, int N, typename Use>
+__device__ __forceinline__ void for_piece(const typename IO::T* from, int n, Use use)
+{
+    for (int first = threadIdx.x * N; first < n; first += kClipThreads * N * kClipAhead) {
+        Piece<IO, N> p[kClipAhead];
+#pragma unroll
+        for (int k = 0; k < kClipAhead; k++) p[k] = load_clamped<IO, N>(from, first + k * kClipThreads * N, n);
+#pragma unroll
+        for (int k = 0; k < kClipAhead; k++) {
+            const int at = first + k * kClipThreads * N;
+            settle(p[k], at, n, typename IO::T(0));
+            use(p[k], at);
+        }
+    }
+}
+template <typename IO, typename Use>
+__device__ __forceinline__ void for_piece(const typename IO::T* from, int n, Use use)
+{
+    if (n >= kPieceOf<IO>) for_piece<IO, kPieceOf<IO>>(from, n, use);
+    else for_piece<IO, 1>(from, n, use);
+}
 template <typename IO>
 __device__ __forceinline__ double piece_squares(const typename IO::T* from, int n)
 {
     double s = 0.0;
-    Piece<IO> p[kClipSteps];
+    for_piece<IO>(from, n, [&](const auto& p, int) {
 #pragma unroll
-    for (int k = 0; k < kClipSteps; k++) {
-        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
-        p[k] = load_piece_of<IO>(from, at, n, typename IO::T(0));
-    }
-#pragma unroll
-    for (int k = 0; k < kClipSteps; k++)
-#pragma unroll
-        for (int i = 0; i < kPiece; i++) {
-            const double v = p[k][i];
+        for (auto e : p.v) {
+            const double v = IO::cvt(e);
             s += v * v;
         }
+    });
     return s;
 }
 template <typename IO>
 __device__ __forceinline__ void piece_scaled(const typename IO::T* from, typename IO::T* to, int n, float scale)
 {
-    Piece<IO> p[kClipSteps];
+    for_piece<IO>(from, n, [&](const auto& p, int at) {
+        constexpr int N = sizeof p.v / sizeof p.v[0];
+        float f[N];
 #pragma unroll
-    for (int k = 0; k < kClipSteps; k++) {
-        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
-        if (at < n) p[k] = load_piece_of<IO>(from, at, n, typename IO::T(0));
-    }
-#pragma unroll
-    for (int k = 0; k < kClipSteps; k++) {
-        const int at = (k * kClipThreads + threadIdx.x) * kPiece;
-        float f[kPiece];
-#pragma unroll
-        for (int i = 0; i < kPiece; i++) f[i] = scale == 1.0f ? p[k][i] : p[k][i] * scale;
-        if (at < n) store_piece_of<IO>(to, at, n, f);
-    }
+        for (int i = 0; i < N; i++) f[i] = scale == 1.0f ? p[i] : p[i] * scale;
+        store_piece_of<IO>(to, at, n, f);
+    });
 }
 
 // The sum over a workgroup, the same in all lanes.

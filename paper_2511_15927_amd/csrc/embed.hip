@@ -4,7 +4,8 @@
 namespace bm {
 
 // out[row] = scale * table[id].  A copy: bound by the rows written (and those of the table that are read).  `lanes` threads to a row,
-// eight elements a thread, so that a row's accesses are one run and a workgroup takes several short rows.
+// 16 bytes of the wider
+// type a thread, so that a row's accesses are one run and a workgroup takes several short rows.
 struct EmbedArgs {
     const int64_t* ids;
     long long ids_sb, ids_st;
@@ -14,9 +15,10 @@ struct EmbedArgs {
     int d, vocab, lanes;
     float scale;
 };
-template <typename TT, typename IO>
-__global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
+template <typename TT, typename IO, int N>
+__device__ __forceinline__ void embed_rows(const EmbedArgs& a)
 {
+    constexpr int kAhead = 2;
     const unsigned per = 256 / a.lanes, lane = threadIdx.x % a.lanes;
     for (unsigned row = blockIdx.x * per + threadIdx.x / a.lanes; row < a.rows; row += gridDim.x * per) {
         const unsigned b = row / a.L, t = row - b * a.L;
@@ -24,16 +26,28 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
         const bool known = id >= 0 && id < a.vocab;
         const typename TT::T* const from = static_cast<const typename TT::T*>(a.table) + (known ? id : 0) * a.d;
         typename IO::T* const to = static_cast<typename IO::T*>(a.out.p) + row_offset(a.out, b, t);
-        for (int at = lane * kPiece; at < a.d; at += a.lanes * kPiece) {
-            float f[kPiece] = {};
-            if (known) {
-                const Piece<TT> p = load_piece_of<TT>(from, at, a.d, typename TT::T(0));
+        for (int first = lane * N; first < a.d; first += a.lanes * N * kAhead) {
+            Piece<TT, N> p[kAhead];
 #pragma unroll
-                for (int i = 0; i < kPiece; i++) f[i] = a.scale * p[i];
+            for (int k = 0; k < kAhead; k++) p[k] = load_clamped<TT, N>(from, first + k * a.lanes * N, a.d);
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const int at = first + k * a.lanes * N;
+                settle(p[k], at, a.d, typename TT::T(0));
+                float f[N];
+#pragma unroll
+                for (int i = 0; i < N; i++) f[i] = known ? a.scale * p[k][i] : 0.0f;
+                store_piece_of<IO>(to, at, a.d, f);
             }
-            store_piece_of<IO>(to, at, a.d, f);
         }
     }
+}
+template <typename TT, typename IO>
+__global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
+{
+    constexpr int N = kPieceOf<TT> < kPieceOf<IO> ? kPieceOf<TT> : kPieceOf<IO>;
+    if (a.d >= N) embed_rows<TT, IO, N>(a);
+    else embed_rows<TT, IO, 1>(a);
 }
 
 // ---- gradient ----
@@ -41,13 +55,37 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 // dtable[v] = scale * sum of dout over the places with id v.  The places are sorted by (id, place); a sum then is over neighbours, in a
 // fixed order, without atomics, and however many places share an id (in a noised sequence half of them are the mask token) they are
 // summed by as many waves as they have slices.  Sorting: chunks of 2048 in shared memory, then merges of sixteen runs at a time, each
-// place counting by binary search what precedes it in the other fifteen.  It moves 8 bytes a place; the rows of dout and of dtable
-// are what bounds the call.
+// place counting by binary search what precedes it in the other fifteen.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
+// meanwhile the other workgroups of its launches clear the table, half of it each, so that only rows of ids that occur are left to
+// write.  (Looking up which rows are absent instead, after the sort, writes those rows once and not twice, but hides nothing.)
 
 constexpr int kChunkBits = 11, kChunk = 1 << kChunkBits;   // places sorted by one workgroup: 21 + 11 bits of a key
+constexpr int kSortThreads = 512, kSortKeys = kChunk / kSortThreads;   // four neighbouring keys a lane
 constexpr int kMaxVocab = (1 << 21) - 1;
 constexpr int kMaxWidth = 1 << 20;
 constexpr int kMergeRuns = 16;
+constexpr unsigned kMergeSamples = 256, kMergeWindow = 8;   // kChunk = samples x window
+
+struct EmbedClear {
+    float* p;
+    long long n;
+    unsigned first_wg;   // of the launch; the workgroups before it sort
+};
+// (kThreads: of a workgroup.)  Floats that a workgroup clears, 16 bytes a lane side by side (at 32 bytes a lane, two stores that each leave every other 16 bytes to the
+// other, it was 4.1 TB/s).
+constexpr int kClearFloats = 32768;
+template <int kThreads>
+__device__ __forceinline__ void clear_part(const EmbedClear& c)
+{
+    const long long from = (long long)(blockIdx.x - c.first_wg) * kClearFloats;
+    const int n = (int)min((long long)kClearFloats, c.n - from);
+    const float zero[4] = {};
+    float* const p = c.p + from;
+#pragma unroll 8
+    for (int at = threadIdx.x * 4; at + 4 <= n; at += kThreads * 4) __builtin_memcpy(p + at, zero, sizeof zero);
+    const int rest = n & ~3;
+    if (rest + (int)threadIdx.x < n) p[rest + threadIdx.x] = 0.0f;
+}
 
 struct EmbedSortArgs {
     const int64_t* ids;
@@ -56,37 +94,102 @@ struct EmbedSortArgs {
     int vocab;
     unsigned* id;     // sorted within each chunk; ids outside [0, vocab) are `vocab`
     unsigned* place;
+    EmbedClear clear;
 };
-__global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedSortArgs a)
+// The value of the lane whose number differs in bit kXor.
+template <int kXor>
+__device__ __forceinline__ unsigned from_lane(unsigned v)
 {
-    __shared__ unsigned key[kChunk];
-    const unsigned base = blockIdx.x << kChunkBits;
-    for (unsigned i = threadIdx.x; i < kChunk; i += 1024) {
-        unsigned k = ~0u;
-        const unsigned row = base + i;
+#define BM_DPP(ctrl) (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, true)
+    if constexpr (kXor == 1) {
+        return BM_DPP(0xB1);    // quad_perm 1 0 3 2
+    } else if constexpr (kXor == 2) {
+        return BM_DPP(0x4E);    // quad_perm 2 3 0 1
+    } else if constexpr (kXor == 4) {
+        v = BM_DPP(0x141);      // row_half_mirror: differs in bits 0 to 2
+        return BM_DPP(0x1B);    // quad_perm 3 2 1 0
+    } else if constexpr (kXor == 8) {
+        return BM_DPP(0x128);   // row_ror 8
+    } else if constexpr (kXor == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+#undef BM_DPP
+}
+// One step of a bitonic sort of the workgroup's keys, four neighbours a lane: keys kStep apart are put in order, ascending where the bit
+// kSize of their place is clear.
+template <int kSize, int kStep>
+__device__ __forceinline__ void sort_step(unsigned (&key)[kSortKeys], unsigned (*across)[kChunk])
+{
+    const unsigned first = threadIdx.x * kSortKeys;
+    if constexpr (kStep < kSortKeys) {
+#pragma unroll
+        for (int k = 0; k < kSortKeys; k++)
+            if (!(k & kStep)) {
+                const unsigned x = key[k], y = key[k + kStep];
+                const bool up = ((first + k) & kSize) == 0;
+                key[k] = up ? min(x, y) : max(x, y);
+                key[k + kStep] = up ? max(x, y) : min(x, y);
+            }
+    } else {
+        const bool low = ((first & kStep) == 0) == ((first & kSize) == 0);   // (steps of a lane or more: the same for its four keys)
+        unsigned other[kSortKeys];
+        if constexpr (kStep < 64 * kSortKeys) {
+#pragma unroll
+            for (int k = 0; k < kSortKeys; k++) other[k] = from_lane<kStep / kSortKeys>(key[k]);
+        } else {
+            // two buffers in turn, so that one barrier a step is enough: the number of such steps before this one says which
+            constexpr int kBlock = 64 * kSortKeys, kLevel = __builtin_ctz(kSize / kBlock), kWithin = __builtin_ctz(kSize / kStep) - 1;
+            constexpr int kTurn = (kLevel * (kLevel - 1) / 2 + kWithin) & 1;
+            unsigned* const b = across[kTurn];
+#pragma unroll
+            for (int k = 0; k < kSortKeys; k++) b[first + k] = key[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kSortKeys; k++) other[k] = b[(first ^ kStep) + k];
+        }
+#pragma unroll
+        for (int k = 0; k < kSortKeys; k++) key[k] = low ? min(key[k], other[k]) : max(key[k], other[k]);
+    }
+}
+template <int kSize, int kStep>
+__device__ __forceinline__ void sort_steps(unsigned (&key)[kSortKeys], unsigned (*across)[kChunk])
+{
+    sort_step<kSize, kStep>(key, across);
+    if constexpr (kStep > 1) sort_steps<kSize, kStep / 2>(key, across);
+    else if constexpr (kSize < kChunk) sort_steps<kSize * 2, kSize>(key, across);
+}
+
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedSortArgs a)
+{
+    if (blockIdx.x >= a.clear.first_wg) {
+        clear_part<kSortThreads>(a.clear);
+        return;
+    }
+    __shared__ __align__(16) unsigned across[2][kChunk];
+    const unsigned base = blockIdx.x << kChunkBits, first = threadIdx.x * kSortKeys;
+    unsigned key[kSortKeys];
+#pragma unroll
+    for (int k = 0; k < kSortKeys; k++) {
+        key[k] = ~0u;
+        const unsigned row = base + first + k;
         if (row < a.rows) {
             const unsigned b = row / a.L, t = row - b * a.L;
             const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
-            k = (unsigned)(id >= 0 && id < a.vocab ? id : a.vocab) << kChunkBits | i;
-        }
-        key[i] = k;
-    }
-    for (int size = 2; size <= kChunk; size *= 2) {
-        for (int step = size / 2; step > 0; step /= 2) {
-            __syncthreads();
-            const int i = 2 * threadIdx.x - (threadIdx.x & (step - 1)), j = i + step;   // a pair `step` apart
-            const unsigned x = key[i], y = key[j];
-            if ((x > y) == ((i & size) == 0)) {
-                key[i] = y;
-                key[j] = x;
-            }
+            key[k] = (unsigned)(id >= 0 && id < a.vocab ? id : a.vocab) << kChunkBits | (first + k);
         }
     }
-    __syncthreads();
-    for (unsigned i = threadIdx.x; i < kChunk && base + i < a.rows; i += 1024) {
-        const unsigned k = key[i];
-        a.id[base + i] = k >> kChunkBits;
-        a.place[base + i] = base + (k & (kChunk - 1));
+    sort_steps<2, 1>(key, across);
+#pragma unroll
+    for (int k = 0; k < kSortKeys; k++) {
+        const unsigned row = base + first + k;
+        if (row < a.rows) {
+            a.id[row] = key[k] >> kChunkBits;
+            a.place[row] = base + (key[k] & (kChunk - 1));
+        }
     }
 }
 
@@ -95,13 +198,26 @@ struct EmbedMergeArgs {
     const unsigned *id, *place;
     unsigned *to_id, *to_place;
     unsigned rows, run;
+    EmbedClear clear;
 };
 __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a)
 {
+    if (blockIdx.x >= a.clear.first_wg) {
+        clear_part<256>(a.clear);
+        return;
+    }
+    // (a run's places are whole workgroups)
+    __shared__ unsigned sample[kMergeRuns * kMergeSamples];
+    const unsigned run = a.run, r = blockIdx.x * 256 / run, first = r / kMergeRuns * kMergeRuns;
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; q++) {
+        const unsigned long long at = (unsigned long long)(first + q) * run + (threadIdx.x + 1) * (run / kMergeSamples) - 1;
+        sample[q * kMergeSamples + threadIdx.x] = a.id[at < a.rows ? at : 0];   // (beyond the list: not looked at)
+    }
     const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    const unsigned id = i < a.rows ? a.id[i] : 0, place = i < a.rows ? a.place[i] : 0;
+    __syncthreads();
     if (i >= a.rows) return;
-    const unsigned run = a.run, r = i / run, first = r / kMergeRuns * kMergeRuns;
-    const unsigned id = a.id[i], place = a.place[i];
     unsigned below[kMergeRuns], len[kMergeRuns];
 #pragma unroll
     for (int q = 0; q < kMergeRuns; q++) {
@@ -109,14 +225,46 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
         len[q] = first + q == r || start >= a.rows ? 0u : min(run, a.rows - (unsigned)start);
         below[q] = 0;
     }
-    for (unsigned step = run; step > 0; step /= 2) {
+    // the last of every 256th part of each run, in shared memory, gives the first eight bits of a place
+    const unsigned part = run / kMergeSamples;
+    const auto precedes = [&](int q, unsigned other) { return first + q < r ? other <= id : other < id; };   // (equal ids keep the order of their places)
+#pragma unroll
+    for (unsigned step = kMergeSamples / 2; step > 0; step /= 2) {
 #pragma unroll
         for (int q = 0; q < kMergeRuns; q++) {
-            const unsigned at = below[q] + step;
-            if (at <= len[q]) {
-                const unsigned other = a.id[(first + q) * run + at - 1];
-                if (first + q < r ? other <= id : other < id) below[q] = at;   // (equal ids keep the order of their places)
-            }
+            const unsigned other = sample[q * kMergeSamples + below[q] + step - 1];
+            if ((below[q] + step) * part <= len[q] && precedes(q, other)) below[q] += step;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; q++) {   // (255 parts at most so far)
+        const unsigned other = sample[q * kMergeSamples + below[q]];
+        if ((below[q] + 1) * part <= len[q] && precedes(q, other)) below[q]++;
+        below[q] *= part;
+    }
+    // long runs: halves of a part, all runs' loads of a step in flight at once, down to eight places; those are looked at together
+    for (unsigned step = part / 2; step >= kMergeWindow; step /= 2) {
+        unsigned other[kMergeRuns];
+#pragma unroll
+        for (int q = 0; q < kMergeRuns; q++) other[q] = a.id[below[q] + step <= len[q] ? (first + q) * run + below[q] + step - 1 : i];
+#pragma unroll
+        for (int q = 0; q < kMergeRuns; q++)
+            if (below[q] + step <= len[q] && precedes(q, other[q])) below[q] += step;
+    }
+#pragma unroll
+    for (int q0 = 0; q0 < kMergeRuns; q0 += 4) {
+        unsigned window[4][kMergeWindow];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {   // (the lists are as long as whole chunks; a run that is not there: this place's own)
+            const unsigned at = below[q0 + q] < len[q0 + q] ? (first + q0 + q) * run + below[q0 + q] : i & ~(kMergeWindow - 1u);
+            __builtin_memcpy(window[q], __builtin_assume_aligned(a.id + at, 16), sizeof window[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            unsigned count = 0;
+#pragma unroll
+            for (unsigned k = 0; k < kMergeWindow; k++) count += below[q0 + q] + k < len[q0 + q] && precedes(q0 + q, window[q][k]);
+            below[q0 + q] += count;
         }
     }
     unsigned to = first * run + (i - r * run);
@@ -126,12 +274,11 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
     a.to_place[to] = place;
 }
 
-// A wave sums a slice of neighbouring places over 512 channels, eight a lane.  A run of one id that lies within the slice gives its
-// row of dtable; what a run that goes on into the next slice, or came from the one before, adds up to here is left in the slice's two
-// slots for embed_join_kernel.  Other workgroups of the launch write the rows whose ids do not occur.
+// A wave sums a slice of neighbouring places over 512 channels, eight a lane.  A run of one id that lies within the slice gives its row of
+// dtable; what a run that goes on into the next slice, or came from the one before, adds up to here is left in the slice's two slots
+// for embed_join_kernel.
 constexpr int kMaxSlice = 64;
-constexpr int kSumCols = 64 * kPiece;
-constexpr int kZeroRows = 8;   // rows of the table that a wave looks up and, where they are absent, clears
+constexpr int kSumCols = 512;
 struct EmbedSumArgs {
     const unsigned *id, *place;
     RowView dout;
@@ -139,41 +286,17 @@ struct EmbedSumArgs {
     float* slots;   // [slices][2][d]: of the run that came into the slice, of the one that starts in it and goes on
     unsigned rows, L;
     int d, vocab, slice, col_blocks;
-    unsigned slices, sum_wgs;
+    unsigned slices;
     float scale;
 };
-template <typename IO>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
+// A lane's eight of the wave's 512 channels from `col`: two groups of four.  N 8: neighbours, one load of bf16; what is stored goes through
+// pairs of lanes, so that each pair writes 32 bytes side by side.  N 4: one group in each half, two loads of fp32.  N 1: rows of
+// fewer channels than that, one a lane.
+template <typename IO, int N>
+__device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice, int block, int lane)
 {
-    const int lane = threadIdx.x % 64;
-    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (blockIdx.x >= a.sum_wgs) {   // rows of ids that do not occur
-        const unsigned v0 = ((blockIdx.x - a.sum_wgs) * 4 + wave) * kZeroRows;
-        bool absent = false;
-        if (lane < kZeroRows && v0 + lane < (unsigned)a.vocab) {
-            const unsigned v = v0 + lane;
-            unsigned lo = 0, hi = a.rows;
-            while (lo < hi) {
-                const unsigned mid = lo + (hi - lo) / 2;
-                if (a.id[mid] < v) lo = mid + 1;
-                else hi = mid;
-            }
-            absent = lo >= a.rows || a.id[lo] != v;
-        }
-        unsigned long long todo = __ballot(absent);
-        const float zero[kPiece] = {};
-        while (todo) {
-            const int k = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            float* const row = a.dtable + (long long)(v0 + k) * a.d;
-            for (int at = lane * kPiece; at < a.d; at += kSumCols) store_piece_of<IoF32>(row, at, a.d, zero);
-        }
-        return;
-    }
-    const unsigned w = blockIdx.x * 4 + wave, slice = w / a.col_blocks;
-    if (slice >= a.slices) return;
-    const int col = (w - slice * a.col_blocks) * kSumCols + lane * kPiece;
-    const bool mine = col < a.d;
+    constexpr int kLoads = N == 8 ? 1 : N == 4 ? 2 : 1;   // pieces a row and lane
+    const int col = block * kSumCols + lane * N;
     const unsigned i0 = slice * a.slice, n = min((unsigned)a.slice, a.rows - i0);
     // a lane's place of the slice: its id and where its row of dout starts
     unsigned my_id = ~0u;
@@ -187,26 +310,44 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
     const typename IO::T* const dout = static_cast<const typename IO::T*>(a.dout.p);
     unsigned cur = __builtin_amdgcn_readlane(my_id, 0);
     bool came = cur == before;
-    float acc[kPiece] = {};
+    float acc[kLoads][N] = {};
     auto flush = [&](bool goes_on) {
-        if (cur >= (unsigned)a.vocab || !mine) return;
-        if (came || goes_on) {
-            store_piece_of<IoF32>(a.slots + ((long long)slice * 2 + (came ? 0 : 1)) * a.d, col, a.d, acc);
-        } else {
-            float f[kPiece];
+        if (cur >= (unsigned)a.vocab) return;
+        const bool slot = came || goes_on;
+        float* const to = slot ? a.slots + ((long long)slice * 2 + (came ? 0 : 1)) * a.d : a.dtable + (long long)cur * a.d;
+        const float scale = slot ? 1.0f : a.scale;
+        if constexpr (N == 8) {
+            float x[4], y[4];
 #pragma unroll
-            for (int i = 0; i < kPiece; i++) f[i] = a.scale * acc[i];
-            store_piece_of<IoF32>(a.dtable + (long long)cur * a.d, col, a.d, f);
+            for (int i = 0; i < 4; i++) {
+                const float lo = scale * acc[0][i], hi = scale * acc[0][4 + i];
+                const float other = __uint_as_float(from_lane<1>(__float_as_uint(lane & 1 ? lo : hi)));
+                x[i] = lane & 1 ? other : lo;
+                y[i] = lane & 1 ? hi : other;
+            }
+            const int at = block * kSumCols + (lane & ~1) * 8 + (lane & 1) * 4;
+            store_piece_of<IoF32>(to, at, a.d, x);
+            store_piece_of<IoF32>(to, at + 8, a.d, y);
+        } else {
+#pragma unroll
+            for (int h = 0; h < kLoads; h++) {
+                float x[N];
+#pragma unroll
+                for (int i = 0; i < N; i++) x[i] = scale * acc[h][i];
+                store_piece_of<IoF32>(to, col + h * 64 * N, a.d, x);
+            }
         }
     };
     constexpr int kAhead = 8;
     for (unsigned e = 0; e < n; e += kAhead) {
-        Piece<IO> p[kAhead];
+        Piece<IO, N> p[kAhead][kLoads];
 #pragma unroll
         for (int j = 0; j < kAhead; j++) {
-            const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_row, e + j), hi = __builtin_amdgcn_readlane((unsigned)(my_row >> 32), e + j);
-            if (e + j < n && mine)
-                p[j] = load_piece_of<IO>(dout + (long long)((unsigned long long)hi << 32 | lo), col, a.d, typename IO::T(0));
+            const unsigned at = min(e + j, n - 1);   // (past the slice: its last row again, not added)
+            const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_row, at), hi = __builtin_amdgcn_readlane((unsigned)(my_row >> 32), at);
+            const typename IO::T* const row = dout + (long long)((unsigned long long)hi << 32 | lo);
+#pragma unroll
+            for (int h = 0; h < kLoads; h++) p[j][h] = load_clamped<IO, N>(row, col + h * 64 * N, a.d);
         }
 #pragma unroll
         for (int j = 0; j < kAhead; j++) {
@@ -217,15 +358,29 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
                     cur = id;
                     came = false;
 #pragma unroll
-                    for (int i = 0; i < kPiece; i++) acc[i] = 0.0f;
-                }
-                if (mine)
+                    for (int h = 0; h < kLoads; h++)
 #pragma unroll
-                    for (int i = 0; i < kPiece; i++) acc[i] += p[j][i];
+                        for (int i = 0; i < N; i++) acc[h][i] = 0.0f;
+                }
+#pragma unroll
+                for (int h = 0; h < kLoads; h++) {
+                    settle(p[j][h], col + h * 64 * N, a.d, typename IO::T(0));
+#pragma unroll
+                    for (int i = 0; i < N; i++) acc[h][i] += p[j][h][i];
+                }
             }
         }
     }
     flush(cur == after);
+}
+template <typename IO>
+__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
+{
+    const unsigned w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), slice = w / a.col_blocks;
+    if (slice >= a.slices) return;
+    const int block = w - slice * a.col_blocks, lane = threadIdx.x % 64;
+    if (a.d >= kPieceOf<IO>) sum_slice<IO, kPieceOf<IO>>(a, slice, block, lane);
+    else sum_slice<IO, 1>(a, slice, block, lane);
 }
 
 // The rows of runs that span slices: the workgroup of the slice in which a run starts adds up its slots, 256 channels at a time, the
@@ -235,7 +390,7 @@ struct EmbedJoinArgs {
     const unsigned* id;
     const float* slots;
     float* dtable;
-    unsigned rows;
+    unsigned slices;
     int d, vocab, slice;
     float scale;
 };
@@ -244,23 +399,32 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
     const unsigned slice = blockIdx.x, i0 = slice * a.slice, i1 = i0 + a.slice;   // (the last slice has no workgroup)
     const unsigned v = a.id[i1 - 1];
     if (v >= (unsigned)a.vocab || a.id[i1] != v || (a.id[i0] == v && i0 > 0 && a.id[i0 - 1] == v)) return;
-    unsigned lo = i1 + 1, hi = a.rows;   // where the run ends
-    while (lo < hi) {
-        const unsigned mid = lo + (hi - lo) / 2;
-        if (a.id[mid] == v) lo = mid + 1;
-        else hi = mid;
-    }
-    const unsigned last = (lo - 1) / a.slice;   // slices slice + 1 .. last came into it
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, col = blockIdx.y * kJoinCols + lane * 4;
+    // the last slice that the run came into: 64 slices are looked at together
+    unsigned last = slice + 1;
+    for (unsigned range = a.slices - last; range > 1;) {
+        const unsigned step = (range + 63) / 64, at = last + lane * step;
+        const unsigned long long in = __ballot(lane * step < range && a.id[lane * step < range ? (unsigned long long)at * a.slice : i1] == v);
+        const unsigned count = __popcll(in);   // (a prefix of the lanes, the first among them)
+        range = min(step, range - (count - 1) * step);
+        last += (count - 1) * step;
+    }
     __shared__ float sum[kJoinWaves][kJoinCols];
     float acc[4] = {};
     auto add = [&](const float* row) {
+        float f[4] = {};
+        if (col + 4 <= a.d) {
+            __builtin_memcpy(f, row + col, sizeof f);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (col + i < a.d) acc[i] += row[col + i];
+            for (int i = 0; i < 4; i++)
+                if (col + i < a.d) f[i] = row[col + i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) acc[i] += f[i];
     };
     if (wave == 0) add(a.slots + ((long long)slice * 2 + 1) * a.d);
-#pragma unroll 4
+#pragma unroll 8
     for (unsigned s = slice + 1 + wave; s <= last; s += kJoinWaves) add(a.slots + (long long)s * 2 * a.d);
 #pragma unroll
     for (int i = 0; i < 4; i++) sum[wave][lane * 4 + i] = acc[i];
@@ -300,7 +464,7 @@ EmbedPlan plan_embed(const bimamba_embed_desc* d)
     p.slice = kMaxSlice;
     while (p.slice > 8 && (long long)(p.rows / p.slice) * p.col_blocks < 8 * cu_count()) p.slice /= 2;
     p.slices = (p.rows + p.slice - 1) / p.slice;
-    p.list = ((size_t)p.rows * 4 + 15) / 16 * 16;
+    p.list = (size_t)p.chunks * kChunk * 4;   // (whole chunks: a merge reads eight places at a time)
     p.total = 4 * p.list + (size_t)p.slices * 2 * d->d_model * sizeof(float);
     return p;
 }
@@ -327,11 +491,11 @@ int bimamba_embed(const bimamba_embed_desc* d, const bimamba_tokens* tokens, con
     if (meet(to, ids) || meet(to, bytes_of(table, (long long)d->vocab * d->d_model, dtype_bytes(d->table_dtype)))) return BIMAMBA_ERR_ALIAS;
     EmbedArgs a{tokens->ptr, tokens->stride_batch, tokens->stride_token, table, row_view(out), (unsigned)(d->batch * (long long)d->seqlen),
                 (unsigned)d->seqlen, d->d_model, d->vocab, 256, d->scale};
-    while (a.lanes > 1 && (a.lanes / 2) * kPiece >= d->d_model) a.lanes /= 2;
+    const bool tb = d->table_dtype == BIMAMBA_BF16, ib = d->io_dtype == BIMAMBA_BF16;
+    while (a.lanes > 1 && (a.lanes / 2) * (tb && ib ? 8 : 4) >= d->d_model) a.lanes /= 2;
     const unsigned per = 256 / a.lanes, want = (a.rows + per - 1) / per, grid = want < 1u << 20 ? want : 1u << 20;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    const bool tb = d->table_dtype == BIMAMBA_BF16, ib = d->io_dtype == BIMAMBA_BF16;
     if (tb && ib) hipLaunchKernelGGL((embed_kernel<IoBF16, IoBF16>), dim3(grid), dim3(256), 0, st, a);
     else if (tb) hipLaunchKernelGGL((embed_kernel<IoBF16, IoF32>), dim3(grid), dim3(256), 0, st, a);
     else if (ib) hipLaunchKernelGGL((embed_kernel<IoF32, IoBF16>), dim3(grid), dim3(256), 0, st, a);
@@ -365,26 +529,32 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     unsigned *id = reinterpret_cast<unsigned*>(ws), *place = reinterpret_cast<unsigned*>(ws + p.list);
     unsigned *to_id = reinterpret_cast<unsigned*>(ws + 2 * p.list), *to_place = reinterpret_cast<unsigned*>(ws + 3 * p.list);
     float* const slots = reinterpret_cast<float*>(ws + 4 * p.list);
-    if (p.rows > 0) {
-        const EmbedSortArgs sa{tokens->ptr, tokens->stride_batch, tokens->stride_token, p.rows, (unsigned)d->seqlen, d->vocab, id, place};
-        hipLaunchKernelGGL(embed_sort_kernel, dim3(p.chunks), dim3(1024), 0, st, sa);
-        for (unsigned long long run = kChunk; run < p.rows; run *= kMergeRuns) {
-            const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run};
-            hipLaunchKernelGGL(embed_merge_kernel, dim3((p.rows + 255) / 256), dim3(256), 0, st, ma);
-            unsigned* const i = id;
-            unsigned* const q = place;
-            id = to_id, place = to_place;
-            to_id = i, to_place = q;
-        }
+    // the table is cleared beside the sort and, where there is one, the first merge
+    const long long all = (long long)d->vocab * d->d_model;
+    const long long half = p.rows > kChunk ? (all / 2 + kClearFloats - 1) / kClearFloats * kClearFloats : all, early = half < all ? half : all;
+    const auto wgs = [](long long n) { return (unsigned)((n + kClearFloats - 1) / kClearFloats); };
+    const EmbedSortArgs sa{tokens->ptr, tokens->stride_batch, tokens->stride_token, p.rows, (unsigned)d->seqlen, d->vocab, id, place,
+                           EmbedClear{dtable, early, p.chunks}};
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(p.chunks + wgs(early)), dim3(kSortThreads), 0, st, sa);
+    if (p.rows == 0) return launches.status();
+    long long left = all - early;
+    for (unsigned long long run = kChunk; run < p.rows; run *= kMergeRuns) {
+        const unsigned merge_wgs = (p.rows + 255) / 256;
+        const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run, EmbedClear{dtable + early, left, merge_wgs}};
+        hipLaunchKernelGGL(embed_merge_kernel, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
+        left = 0;
+        unsigned* const i = id;
+        unsigned* const q = place;
+        id = to_id, place = to_place;
+        to_id = i, to_place = q;
     }
-    EmbedSumArgs a{id, place, row_view(dout), dtable, slots, p.rows, (unsigned)d->seqlen, d->d_model, d->vocab, p.slice, p.col_blocks,
-                   p.slices, 0, d->scale};
-    a.sum_wgs = (unsigned)(((unsigned long long)p.slices * p.col_blocks + 3) / 4);
-    const unsigned zero_wgs = (d->vocab + 4 * kZeroRows - 1) / (4 * kZeroRows);
-    if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(a.sum_wgs + zero_wgs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(a.sum_wgs + zero_wgs), dim3(256), 0, st, a);
+    const EmbedSumArgs a{id, place, row_view(dout), dtable, slots, p.rows, (unsigned)d->seqlen, d->d_model, d->vocab, p.slice, p.col_blocks,
+                         p.slices, d->scale};
+    const unsigned sum_wgs = (unsigned)(((unsigned long long)p.slices * p.col_blocks + 3) / 4);
+    if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(sum_wgs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(sum_wgs), dim3(256), 0, st, a);
     if (p.slices > 1) {
-        const EmbedJoinArgs ja{id, slots, dtable, p.rows, d->d_model, d->vocab, p.slice, d->scale};
+        const EmbedJoinArgs ja{id, slots, dtable, p.slices, d->d_model, d->vocab, p.slice, d->scale};
         hipLaunchKernelGGL(embed_join_kernel, dim3(p.slices - 1, (d->d_model + kJoinCols - 1) / kJoinCols), dim3(64 * kJoinWaves), 0, st, ja);
     }
     return launches.status();

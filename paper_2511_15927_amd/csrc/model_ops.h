@@ -1,4 +1,4 @@
-// What the operators around the mixers share: rows moved in pieces of eight elements, sums over a wave, and the host's checks.
+// What the operators around the mixers share: rows moved in pieces of 16 bytes, sums over a wave, and the host's checks.
 #pragma once
 #include "bimamba.h"
 #include "kernels.h"
@@ -10,56 +10,80 @@
 
 namespace bm {
 
-constexpr int kPiece = 8;   // elements a lane moves at once: 16 bytes of bf16, 32 of fp32
-
-// Eight elements of a row, at any alignment that the element type allows (the memory unit takes the 16 bytes as they lie).
+// Elements that a lane moves at once: 16 bytes, so that a wave's access is one run.  (fp32 rows in pieces of eight, two accesses that each
+// leave every other 16 bytes to the other, were written at 4.1 TB/s, in these pieces at 7.4.)
 template <typename IO>
+constexpr int kPieceOf = 16 / (int)sizeof(typename IO::T);
+
+// Neighbouring elements of a row, at any alignment that the element type allows (the memory unit takes the bytes as they lie).
+template <typename IO, int N = kPieceOf<IO>>
 struct Piece {
-    typename IO::T v[kPiece];
+    typename IO::T v[N];
     __device__ __forceinline__ float operator[](int i) const { return IO::cvt(v[i]); }
 };
-template <typename IO>
-__device__ __forceinline__ Piece<IO> load_piece(const typename IO::T* p)
+template <typename IO, int N = kPieceOf<IO>>
+__device__ __forceinline__ Piece<IO, N> load_piece(const typename IO::T* p)
 {
-    Piece<IO> r;
+    Piece<IO, N> r;
     __builtin_memcpy(&r, p, sizeof r);
     return r;
 }
-template <typename IO>
-__device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[kPiece])
+template <typename IO, int N>
+__device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[N])
 {
-    Piece<IO> r;
+    Piece<IO, N> r;
 #pragma unroll
-    for (int i = 0; i < kPiece; i++) r.v[i] = io_value<IO>(f[i]);
+    for (int i = 0; i < N; i++) r.v[i] = io_value<IO>(f[i]);
     __builtin_memcpy(p, &r, sizeof r);
 }
-// The piece of a row that starts at element `at`, which may reach beyond the row's n elements: those read `fill`.
-template <typename IO>
-__device__ __forceinline__ Piece<IO> load_piece_of(const typename IO::T* row, int at, int n, typename IO::T fill)
+// The piece of a row that starts at element `at`, which may reach beyond the row's n >= N elements, in two steps.  The load takes the last N
+// elements where the piece would reach beyond, so there is no branch around it and all loads of a lane are in flight together (with
+// the row's end told apart by a branch the compiler waited for each load where the two ways join: the sum of a table's
+// gradient ran at 1.5 TB/s).  settle() then puts what is left of the piece in its place, and `fill` beyond the row.
+template <typename IO, int N = kPieceOf<IO>>
+__device__ __forceinline__ Piece<IO, N> load_clamped(const typename IO::T* row, int at, int n)
 {
-    if (at + kPiece <= n) return load_piece<IO>(row + at);
-    Piece<IO> r;
+    return load_piece<IO, N>(row + min(at, n - N));
+}
+template <typename IO, int N>
+__device__ __forceinline__ void settle(Piece<IO, N>& p, int at, int n, typename IO::T fill)
+{
+    if (at + N <= n) return;
+    const int off = at - (n - N);   // places to move by; N or more: beyond the row
 #pragma unroll
-    for (int i = 0; i < kPiece; i++) r.v[i] = at + i < n ? row[at + i] : fill;
+    for (int step = N / 2; step > 0; step /= 2) {
+#pragma unroll
+        for (int i = 0; i < N; i++) p.v[i] = off & step ? (i + step < N ? p.v[i + step < N ? i + step : i] : fill) : p.v[i];
+    }
+    if (off >= N)
+#pragma unroll
+        for (int i = 0; i < N; i++) p.v[i] = fill;
+}
+template <typename IO, int N = kPieceOf<IO>>
+__device__ __forceinline__ Piece<IO, N> load_piece_of(const typename IO::T* row, int at, int n, typename IO::T fill)
+{
+    Piece<IO, N> r = load_clamped<IO, N>(row, at, n);
+    settle(r, at, n, fill);
     return r;
 }
-template <typename IO>
-__device__ __forceinline__ void store_piece_of(typename IO::T* row, int at, int n, const float (&f)[kPiece])
+template <typename IO, int N>
+__device__ __forceinline__ void store_piece_of(typename IO::T* row, int at, int n, const float (&f)[N])
 {
-    if (at + kPiece <= n) {
+    if (at + N <= n) {
         store_piece<IO>(row + at, f);
     } else {
 #pragma unroll
-        for (int i = 0; i < kPiece; i++)
+        for (int i = 0; i < N; i++)
             if (at + i < n) row[at + i] = io_value<IO>(f[i]);
     }
 }
-// fp32 parameters and gradients in the same pieces.
-__device__ __forceinline__ void load_floats(float (&f)[kPiece], const float* row, int at, int n, float fill)
+// fp32 parameters beside them, in elements [at, at + N) of n >= N.
+template <int N>
+__device__ __forceinline__ void load_floats(float (&f)[N], const float* row, int at, int n, float fill)
 {
-    const Piece<IoF32> p = load_piece_of<IoF32>(row, at, n, fill);
+    const Piece<IoF32, N> p = load_piece_of<IoF32, N>(row, at, n, fill);
 #pragma unroll
-    for (int i = 0; i < kPiece; i++) f[i] = p[i];
+    for (int i = 0; i < N; i++) f[i] = p[i];
 }
 
 // A value combined over the 64 lanes, the same in all of them: lane permutes within a row of sixteen, then the swaps between rows.

@@ -3,7 +3,7 @@
 
 namespace bm {
 
-// A row stays in registers: `waves` waves hold it, `pieces` pieces of eight elements a lane, lanes side by side.  The statistics are
+// A row stays in registers: `waves` waves hold it, 8, 16 or 32 elements a lane in pieces of 16 bytes, lanes side by side.  The statistics are
 // taken in two steps over the registers (the mean, then the squares of what is left), so that a large mean costs no precision; where
 // four waves share a row each takes both of its own part, and one exchange joins them (the squares around the common mean are the
 // parts' own plus what their means are off by).
@@ -56,8 +56,8 @@ __device__ __forceinline__ float2 row_sum(float2 v, Exchange<kWaves>& ex, int wa
 }
 
 // kWaves 1: each of the workgroup's four waves takes rows of its own.
-template <typename IO, int kWaves, int kPieces>
-__global__ __launch_bounds__(256) void norm_kernel(const NormArgs a)
+template <typename IO, int kWaves, int kPieces, int kPiece>
+__device__ __forceinline__ void norm_rows(const NormArgs& a)
 {
     __shared__ Exchange<kWaves> ex;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -78,23 +78,25 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormArgs a)
         }
     }
     const float inv = 1.0f / a.d;
-    Piece<IO> next[kPieces];
+    Piece<IO, kPiece> next[kPieces];
     const auto request = [&](unsigned r) {
         const NormRow row = norm_row(a.n, vector, r);
         const typename IO::T* const x = static_cast<const typename IO::T*>(a.x.p) + row_offset(a.x, row.b, row.t);
 #pragma unroll
-        for (int k = 0; k < kPieces; k++) next[k] = load_piece_of<IO>(x, at(k), a.d, typename IO::T(0));
+        for (int k = 0; k < kPieces; k++) next[k] = load_clamped<IO, kPiece>(x, at(k), a.d);
     };
     request(r0);
     for (unsigned r = r0; r < r1; r++) {
         float x[kPieces][kPiece], sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kPieces; k++)
+        for (int k = 0; k < kPieces; k++) {
+            settle(next[k], at(k), a.d, typename IO::T(0));
 #pragma unroll
             for (int i = 0; i < kPiece; i++) {
                 x[k][i] = next[k][i];
                 sum += x[k][i];
             }
+        }
         if (r + 1 < r1) request(r + 1);
         sum = wave_sum(sum);
         // the part's own mean and squares around it
@@ -146,6 +148,15 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormArgs a)
     }
 }
 
+template <typename IO, int kWaves, int kElems>
+__global__ __launch_bounds__(256) void norm_kernel(const NormArgs a)
+{
+    if constexpr (kWaves == 1 && kElems == 8) {   // (rows shorter than a piece: an element a lane)
+        if (a.d < kPieceOf<IO>) return norm_rows<IO, 1, 1, 1>(a);
+    }
+    norm_rows<IO, kWaves, kElems / kPieceOf<IO>, kPieceOf<IO>>(a);
+}
+
 // Rows longer than the registers of four waves: one workgroup of sixteen waves to a row, which it reads three times (from the caches
 // the second and third time).
 constexpr int kLongThreads = 1024;
@@ -163,6 +174,7 @@ __device__ __forceinline__ float workgroup_sum(float v, float* part)
 template <typename IO>
 __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(const NormArgs a)
 {
+    constexpr int kPiece = kPieceOf<IO>;
     __shared__ float part[kLongThreads / 64];
     const unsigned vector = blockIdx.y;
     const int first = threadIdx.x * kPiece, step = kLongThreads * kPiece;
@@ -217,8 +229,8 @@ struct NormBwdArgs {
     NormRows n;
     int d;
 };
-template <typename IO, int kWaves, int kPieces>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(const NormBwdArgs a)
+template <typename IO, int kWaves, int kPieces, int kPiece>
+__device__ __forceinline__ void norm_bwd_rows(const NormBwdArgs& a)
 {
     __shared__ Exchange<kWaves> ex;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -241,15 +253,17 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const NormBwdArgs a)
         const NormRow row = norm_row(a.n, vector, r);
         const typename IO::T* const x = static_cast<const typename IO::T*>(a.x.p) + row_offset(a.x, row.b, row.t);
         const typename IO::T* const dy = static_cast<const typename IO::T*>(a.dy.p) + row_offset(a.dy, row.b, row.t);
-        Piece<IO> px[kPieces], pd[kPieces];
+        Piece<IO, kPiece> px[kPieces], pd[kPieces];
 #pragma unroll
-        for (int k = 0; k < kPieces; k++) px[k] = load_piece_of<IO>(x, at(k), a.d, typename IO::T(0));
+        for (int k = 0; k < kPieces; k++) px[k] = load_clamped<IO, kPiece>(x, at(k), a.d);
 #pragma unroll
-        for (int k = 0; k < kPieces; k++) pd[k] = load_piece_of<IO>(dy, at(k), a.d, typename IO::T(0));   // (beyond the row: g = 0)
+        for (int k = 0; k < kPieces; k++) pd[k] = load_clamped<IO, kPiece>(dy, at(k), a.d);
         const float mean = a.mean[row.at], rstd = a.rstd[row.at];
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int k = 0; k < kPieces; k++)
+        for (int k = 0; k < kPieces; k++) {
+            settle(px[k], at(k), a.d, typename IO::T(0));
+            settle(pd[k], at(k), a.d, typename IO::T(0));   // (beyond the row: g = 0)
 #pragma unroll
             for (int i = 0; i < kPiece; i++) {
                 const float xh = (px[k][i] - mean) * rstd, d = pd[k][i], g = d * w[k][i];
@@ -258,6 +272,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const NormBwdArgs a)
                 s.x += g;
                 s.y += g * xh;
             }
+        }
         s.x = wave_sum(s.x);
         s.y = wave_sum(s.y);
         s = row_sum<kWaves>(s, ex, wave, (r - r0) & 1);
@@ -294,10 +309,20 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const NormBwdArgs a)
     }
 }
 
+template <typename IO, int kWaves, int kElems>
+__global__ __launch_bounds__(256) void norm_bwd_kernel(const NormBwdArgs a)
+{
+    if constexpr (kWaves == 1 && kElems == 8) {   // (rows shorter than a piece: an element a lane)
+        if (a.d < kPieceOf<IO>) return norm_bwd_rows<IO, 1, 1, 1>(a);
+    }
+    norm_bwd_rows<IO, kWaves, kElems / kPieceOf<IO>, kPieceOf<IO>>(a);
+}
+
 // Long rows: two reads of a row; the sums over rows are taken by norm_long_cols_kernel from x and dy again.
 template <typename IO>
 __global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(const NormBwdArgs a)
 {
+    constexpr int kPiece = kPieceOf<IO>;
     __shared__ float part[kLongThreads / 64];
     const unsigned vector = blockIdx.y;
     const int first = threadIdx.x * kPiece, step = kLongThreads * kPiece;
@@ -335,10 +360,11 @@ __global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(const NormB
         }
     }
 }
-// grid (groups of rows, vectors, columns of 256 threads): a thread sums its eight channels over the group's rows.
+// grid (groups of rows, vectors, columns of 256 threads): a thread sums the channels of a piece over the group's rows.
 template <typename IO>
 __global__ __launch_bounds__(256) void norm_long_cols_kernel(const NormBwdArgs a)
 {
+    constexpr int kPiece = kPieceOf<IO>;
     const unsigned vector = blockIdx.y, r0 = blockIdx.x * a.n.per_group, r1 = min(r0 + a.n.per_group, a.n.rows);
     const int at = (blockIdx.z * 256 + threadIdx.x) * kPiece;
     if (at >= a.d) return;
@@ -359,8 +385,8 @@ __global__ __launch_bounds__(256) void norm_long_cols_kernel(const NormBwdArgs a
     store_piece_of<IoF32>(slot + a.d, at, a.d, db);
 }
 
-// dweight and dbias: the slots of a vector, added up 32 channels to a workgroup, each of its eight rows of threads a share of the slots.
-constexpr int kSumRows = 8, kSumChannels = 32;
+// dweight and dbias: the slots of a vector, added up 32 channels to a workgroup, each of its 32 rows of threads a share of the slots.
+constexpr int kSumRows = 32, kSumChannels = 32;
 struct NormSumArgs {
     const float* slots;
     float *dweight, *dbias;
@@ -403,7 +429,7 @@ int check_norm(const bimamba_norm_desc* d)
 
 // Which waves hold a row, and how many rows a group of them takes.
 struct NormPlan {
-    int waves, pieces;   // pieces 0: a long row
+    int waves, elems;   // elements a lane; 0: a long row
     unsigned vectors, groups;   // vectors that rows share; workgroups of each
     NormRows n;
 };
@@ -411,16 +437,16 @@ NormPlan plan_norm(const bimamba_norm_desc* d, bool per_batch, bool bwd)
 {
     NormPlan p{};
     const unsigned rows = (unsigned)((long long)d->batch * d->seqlen);
-    const int one = 64 * kPiece;   // elements that a wave holds in one piece a lane
+    const int one = 64 * 8;
     const bool spread = rows < 4u * cu_count() || bwd;
-    p.waves = d->d_model <= one || (!spread && d->d_model <= 4 * one) ? 1 : 4;
+    p.waves = d->d_model <= (bwd ? 2 : 1) * one || (!spread && d->d_model <= 4 * one) ? 1 : 4;
     const int need = (d->d_model + p.waves * one - 1) / (p.waves * one);
-    p.pieces = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 0;
+    p.elems = need <= 1 ? 8 : need <= 2 ? 16 : need <= 4 ? 32 : 0;
     p.vectors = per_batch ? d->batch : 1;
     p.n.L = d->seqlen;
     p.n.rows = per_batch ? d->seqlen : rows;
     p.n.per_batch = per_batch;
-    const unsigned together = p.pieces && p.waves == 1 ? 4 : 1;   // rows that a workgroup has in hand at once
+    const unsigned together = p.elems && p.waves == 1 ? 4 : 1;   // rows that a workgroup has in hand at once
     const unsigned want = (bwd ? 4u : 8u) * cu_count();           // workgroups in all
     const unsigned groups = p.vectors ? (want + p.vectors - 1) / p.vectors : 1;
     const unsigned per_workgroup = (p.n.rows + groups - 1) / groups;
@@ -436,13 +462,13 @@ template <typename IO>
 void launch_norm(const NormPlan& p, const NormArgs& a, hipStream_t st)
 {
     const dim3 grid(p.groups, p.vectors), wg(256);
-    switch (p.pieces * 8 + p.waves) {
-        case 1 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 1>), grid, wg, 0, st, a); break;
-        case 2 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 2>), grid, wg, 0, st, a); break;
-        case 4 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 4>), grid, wg, 0, st, a); break;
-        case 1 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 1>), grid, wg, 0, st, a); break;
-        case 2 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 2>), grid, wg, 0, st, a); break;
-        case 4 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 4>), grid, wg, 0, st, a); break;
+    switch (p.elems * 8 + p.waves) {
+        case 8 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 8>), grid, wg, 0, st, a); break;
+        case 16 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 16>), grid, wg, 0, st, a); break;
+        case 32 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 32>), grid, wg, 0, st, a); break;
+        case 8 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 8>), grid, wg, 0, st, a); break;
+        case 16 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 16>), grid, wg, 0, st, a); break;
+        case 32 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 32>), grid, wg, 0, st, a); break;
         default: hipLaunchKernelGGL(norm_long_kernel<IO>, dim3(long_groups(a.n), p.vectors), dim3(kLongThreads), 0, st, a);
     }
 }
@@ -450,15 +476,16 @@ template <typename IO>
 void launch_norm_bwd(const NormPlan& p, const NormBwdArgs& a, hipStream_t st)
 {
     const dim3 grid(p.groups, p.vectors), wg(256);
-    switch (p.pieces * 8 + p.waves) {
-        case 1 * 8 + 1: hipLaunchKernelGGL((norm_bwd_kernel<IO, 1, 1>), grid, wg, 0, st, a); break;
-        case 1 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 1>), grid, wg, 0, st, a); break;
-        case 2 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 2>), grid, wg, 0, st, a); break;
-        case 4 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 4>), grid, wg, 0, st, a); break;
+    switch (p.elems * 8 + p.waves) {
+        case 8 * 8 + 1: hipLaunchKernelGGL((norm_bwd_kernel<IO, 1, 8>), grid, wg, 0, st, a); break;
+        case 16 * 8 + 1: hipLaunchKernelGGL((norm_bwd_kernel<IO, 1, 16>), grid, wg, 0, st, a); break;
+        case 8 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 8>), grid, wg, 0, st, a); break;
+        case 16 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 16>), grid, wg, 0, st, a); break;
+        case 32 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 32>), grid, wg, 0, st, a); break;
         default:
             hipLaunchKernelGGL(norm_bwd_long_kernel<IO>, dim3(long_groups(a.n), p.vectors), dim3(kLongThreads), 0, st, a);
             if (a.slots)
-                hipLaunchKernelGGL(norm_long_cols_kernel<IO>, dim3(p.groups, p.vectors, (a.d + 256 * kPiece - 1) / (256 * kPiece)), wg, 0, st, a);
+                hipLaunchKernelGGL(norm_long_cols_kernel<IO>, dim3(p.groups, p.vectors, (a.d + 256 * kPieceOf<IO> - 1) / (256 * kPieceOf<IO>)), wg, 0, st, a);
     }
 }
 

@@ -91,13 +91,13 @@ __device__ __forceinline__ void store_top(const ScoresArgs& a, unsigned row, int
     if (a.top_token) a.top_token[(long long)row * a.top_k + k] = none ? -1 : (int64_t)id_of(key);
 }
 
-// A workgroup takes a row, or one of its `splits` parts where there are few rows.  With kTop a lane also keeps which of its pieces of
-// eight first had the largest logit.  The best pieces of the lanes are all different, so the k lanes with the best of them hold
+// A workgroup takes a row, or one of its `splits` parts where there are few rows.  With kTop a lane also keeps which of its pieces
+// first had the largest logit.  The best pieces of the lanes are all different, so the k lanes with the best of them hold
 // the k best logits of the row: these lanes' pieces alone are read again (from the caches), spread over all lanes, k times for the
 // best logit below the one before.
 constexpr int kScoresThreads = 256, kScoresWaves = kScoresThreads / 64, kScoresAhead = 4;
-template <typename IO, bool kEntropy, bool kTop>
-__global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs a)
+template <typename IO, bool kEntropy, bool kTop, int kPiece>
+__device__ __forceinline__ void scores_row(const ScoresArgs& a)
 {
     const unsigned row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
     const unsigned b = row / a.L, t = row - b * a.L;
@@ -114,14 +114,14 @@ __global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs
     float best = -INFINITY;
     unsigned best_piece = ~0u;
     for (int first = threadIdx.x; first < pieces; first += kScoresThreads * kScoresAhead) {
-        Piece<IO> p[kScoresAhead];
+        Piece<IO, kPiece> p[kScoresAhead];
 #pragma unroll
-        for (int j = 0; j < kScoresAhead; j++)
-            if (first + j * kScoresThreads < pieces) p[j] = load_piece_of<IO>(x, (first + j * kScoresThreads) * kPiece, n, lowest);
+        for (int j = 0; j < kScoresAhead; j++) p[j] = load_clamped<IO, kPiece>(x, (first + j * kScoresThreads) * kPiece, n);
 #pragma unroll
         for (int j = 0; j < kScoresAhead; j++) {
             const int piece = first + j * kScoresThreads;
             if (piece < pieces) {
+                settle(p[j], piece * kPiece, n, lowest);
                 float m = p[j][0];
 #pragma unroll
                 for (int i = 1; i < kPiece; i++) m = fmaxf(m, p[j][i]);
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs
             for (int item = threadIdx.x; item < items; item += kScoresThreads) {
                 const int which = item / rounds, piece = (item - which * rounds) * kScoresThreads + chosen[which];
                 if (piece < pieces) {
-                    const Piece<IO> p = load_piece_of<IO>(x, piece * kPiece, n, lowest);
+                    const Piece<IO, kPiece> p = load_piece_of<IO, kPiece>(x, piece * kPiece, n, lowest);
 #pragma unroll
                     for (int i = 0; i < kPiece; i++) {
                         const Key key = piece * kPiece + i < n ? key_of(p[i], from + piece * kPiece + i) : 0;
@@ -222,6 +222,14 @@ __global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs
             }
         }
     }
+}
+
+template <typename IO, bool kEntropy, bool kTop>
+__global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs a)
+{
+    // (rows shorter than a piece: a logit a lane)
+    if (a.vocab >= kPieceOf<IO>) scores_row<IO, kEntropy, kTop, kPieceOf<IO>>(a);
+    else scores_row<IO, kEntropy, kTop, 1>(a);
 }
 
 // A wave joins the parts of a row, a part a lane; the lanes' alternatives are in descending order already.
@@ -266,56 +274,67 @@ __global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
 //
 // Elementwise, given lse and the entropy: p = exp(x - lse), dx = dlogp (1[target] - p) - dentropy p (log p + H).  A logit is read and its
 // gradient written by the same lane, so the gradient may take the logits' place.
-constexpr int kGradPieces = 4, kGradThreads = 256, kGradPart = kGradThreads * kGradPieces * kPiece;
+constexpr int kGradThreads = 256, kGradPart = kGradThreads * 32;
 struct ScoresBwdArgs {
     RowView logits, dlogits;
     const int64_t* ids;
     long long ids_sb, ids_st;
     const float *lse, *entropy, *dlogp, *dentropy;
-    unsigned rows, L, parts;
+    unsigned L, parts, all;   // parts of a row, and of all rows
     int vocab;
 };
-template <typename IO>
-__global__ __launch_bounds__(kGradThreads) void scores_bwd_kernel(const ScoresBwdArgs a)
+template <typename IO, bool kEntropy, int kPiece>
+__device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned row, unsigned part)
 {
     typedef typename IO::T T;
-    const unsigned long long all = (unsigned long long)a.rows * a.parts;
-    for (unsigned long long w = blockIdx.x; w < all; w += gridDim.x) {
-        const unsigned row = w / a.parts, part = w - (unsigned long long)row * a.parts, b = row / a.L, t = row - b * a.L;
-        long long target = -1;
-        if (a.ids) {
-            const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
-            if (id >= 0 && id < a.vocab) target = id;
+    constexpr int kPieces = kGradPart / (kGradThreads * kPieceOf<IO>);
+    const unsigned b = row / a.L, t = row - b * a.L;
+    int target = -1;
+    if (a.ids) {
+        const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
+        if (id >= 0 && id < a.vocab) target = (int)id;
+    }
+    const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f, de = kEntropy ? a.dentropy[row] : 0.0f;
+    const float lse = a.lse[row], h = kEntropy ? a.entropy[row] : 0.0f;
+    const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t);
+    T* const dx = static_cast<T*>(a.dlogits.p) + row_offset(a.dlogits, b, t);
+    const int first = part * kGradPart + threadIdx.x * kPiece;
+    const auto at = [&](int k) { return first + k * kGradThreads * kPiece; };
+    if ((dl == 0.0f && de == 0.0f) || lse == -INFINITY) {
+        const float zero[kPiece] = {};
+#pragma unroll
+        for (int k = 0; k < kPieces; k++)
+            if (at(k) < a.vocab) store_piece_of<IO>(dx, at(k), a.vocab, zero);
+        return;
+    }
+    Piece<IO, kPiece> p[kPieces];
+#pragma unroll
+    for (int k = 0; k < kPieces; k++) p[k] = load_clamped<IO, kPiece>(x, at(k), a.vocab);
+    // (in place a lane's later pieces, clamped to the row's end, may have been overwritten by then: those are not stored)
+#pragma unroll
+    for (int k = 0; k < kPieces; k++) {
+        if (at(k) >= a.vocab) continue;
+        settle(p[k], at(k), a.vocab, T(0));
+        float f[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; i++) {
+            const float d = p[k][i] - lse, e = fast_exp2(d * kLog2e);
+            if constexpr (kEntropy) f[i] = -e * (dl + de * (fmaxf(d, kFarBelow) + h));
+            else f[i] = -e * dl;
         }
-        const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f, de = a.dentropy ? a.dentropy[row] : 0.0f;
-        const float lse = a.lse[row], h = a.dentropy ? a.entropy[row] : 0.0f;
-        const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t);
-        T* const dx = static_cast<T*>(a.dlogits.p) + row_offset(a.dlogits, b, t);
-        const int first = part * kGradPart + threadIdx.x * kPiece;
-        const auto at = [&](int k) { return first + k * kGradThreads * kPiece; };
-        if ((dl == 0.0f && de == 0.0f) || lse == -INFINITY) {
-            const float zero[kPiece] = {};
+        if ((unsigned)(target - at(k)) < (unsigned)kPiece)   // (no target: far outside)
 #pragma unroll
-            for (int k = 0; k < kGradPieces; k++)
-                if (at(k) < a.vocab) store_piece_of<IO>(dx, at(k), a.vocab, zero);
-            continue;
-        }
-        Piece<IO> p[kGradPieces];
-#pragma unroll
-        for (int k = 0; k < kGradPieces; k++)
-            if (at(k) < a.vocab) p[k] = load_piece_of<IO>(x, at(k), a.vocab, T(0));
-#pragma unroll
-        for (int k = 0; k < kGradPieces; k++) {
-            if (at(k) >= a.vocab) continue;
-            float f[kPiece];
-#pragma unroll
-            for (int i = 0; i < kPiece; i++) {
-                const float d = p[k][i] - lse, e = fast_exp2(d * kLog2e);
-                f[i] = -e * (dl + de * (fmaxf(d, kFarBelow) + h));
-                if (at(k) + i == target) f[i] += dl;
-            }
-            store_piece_of<IO>(dx, at(k), a.vocab, f);
-        }
+            for (int i = 0; i < kPiece; i++) f[i] += at(k) + i == target ? dl : 0.0f;
+        store_piece_of<IO>(dx, at(k), a.vocab, f);
+    }
+}
+template <typename IO, bool kEntropy>
+__global__ __launch_bounds__(kGradThreads) void scores_bwd_kernel(const ScoresBwdArgs a)
+{
+    for (unsigned w = blockIdx.x; w < a.all; w += gridDim.x) {
+        const unsigned row = w / a.parts, part = w - row * a.parts;
+        if (a.vocab >= kPieceOf<IO>) scores_bwd_part<IO, kEntropy, kPieceOf<IO>>(a, row, part);
+        else scores_bwd_part<IO, kEntropy, 1>(a, row, part);
     }
 }
 
@@ -343,13 +362,16 @@ ScoresPlan plan_scores(const bimamba_logits_desc* d)
     p.rows = (unsigned)((long long)d->batch * d->seqlen);
     p.splits = 1;
     if (p.rows > 0) {
-        const long long want = (4ll * cu_count() + p.rows - 1) / p.rows, most = d->vocab / (kScoresThreads * kPiece);
+        const long long want = (4ll * cu_count() + p.rows - 1) / p.rows, most = d->vocab / 2048;
         p.splits = (int)(want < most ? want : most);
         if (p.splits > kMaxSplits) p.splits = kMaxSplits;
         if (p.splits < 1) p.splits = 1;
     }
-    p.per_split = ((d->vocab + p.splits - 1) / p.splits + kPiece - 1) / kPiece * kPiece;
-    p.splits = (d->vocab + p.per_split - 1) / p.per_split;
+    p.per_split = ((d->vocab + p.splits - 1) / p.splits + 7) / 8 * 8;   // (whole pieces of either type)
+    for (;; p.per_split += 8) {   // (no last part shorter than a piece)
+        p.splits = (d->vocab + p.per_split - 1) / p.per_split;
+        if (p.splits == 1 || d->vocab - (p.splits - 1) * p.per_split >= 8) break;
+    }
     if (p.splits > 1) {
         p.stats = ((size_t)p.rows * p.splits * sizeof(Stats) + 15) / 16 * 16;
         p.total = p.stats + (size_t)p.rows * p.splits * d->top_k * sizeof(Key);
@@ -450,14 +472,19 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* lo
     a.logits = row_view(logits), a.dlogits = row_view(dlogits);
     if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
     a.lse = lse, a.entropy = entropy, a.dlogp = dlogp, a.dentropy = dentropy;
-    a.rows = (unsigned)rows, a.L = d->seqlen, a.vocab = d->vocab;
+    a.L = d->seqlen, a.vocab = d->vocab;
     a.parts = (unsigned)((d->vocab + (long long)kGradPart - 1) / kGradPart);
     const unsigned long long all = (unsigned long long)rows * a.parts;
+    if (all >= 1ull << 31) return BIMAMBA_ERR_UNSUPPORTED;
+    a.all = (unsigned)all;
     const unsigned grid = all < 1u << 22 ? (unsigned)all : 1u << 22;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(scores_bwd_kernel<IoBF16>, dim3(grid), dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL(scores_bwd_kernel<IoF32>, dim3(grid), dim3(kGradThreads), 0, st, a);
+    const bool bf16 = d->io_dtype == BIMAMBA_BF16;
+    if (bf16 && dentropy) hipLaunchKernelGGL((scores_bwd_kernel<IoBF16, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
+    else if (bf16) hipLaunchKernelGGL((scores_bwd_kernel<IoBF16, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
+    else if (dentropy) hipLaunchKernelGGL((scores_bwd_kernel<IoF32, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
+    else hipLaunchKernelGGL((scores_bwd_kernel<IoF32, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
     return launches.status();
 }
 
