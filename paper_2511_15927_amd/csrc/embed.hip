@@ -54,17 +54,17 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 //
 // dtable[v] = scale * sum of dout over the places with id v.  The places are sorted by (id, place); a sum then is over neighbours, in a
 // fixed order, without atomics, and however many places share an id (in a noised sequence half of them are the mask token) they are
-// summed by as many waves as they have slices.  Sorting: chunks of 2048 in shared memory, then merges of sixteen runs at a time, each
+// summed by as many waves as they have slices.  Sorting: chunks of up to 4096 in a workgroup's registers, then merges of sixteen runs at a time, each
 // place counting by binary search what precedes it in the other fifteen.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
 // meanwhile the other workgroups of its launches clear the table, half of it each, so that only rows of ids that occur are left to
 // write.  (Looking up which rows are absent instead, after the sort, writes those rows once and not twice, but hides nothing.)
 
-constexpr int kChunkBits = 11, kChunk = 1 << kChunkBits;   // places sorted by one workgroup: 21 + 11 bits of a key
-constexpr int kSortThreads = 512, kSortKeys = kChunk / kSortThreads;   // four neighbouring keys a lane
+// Places sorted by one workgroup, 2048 or 4096 by the bits that the ids leave of a 32-bit key, four neighbouring ones a lane.
+constexpr int kChunkBits = 11, kLargeChunkBits = 12, kSortKeys = 4;
 constexpr int kMaxVocab = (1 << 21) - 1;
 constexpr int kMaxWidth = 1 << 20;
-constexpr int kMergeRuns = 16;
-constexpr unsigned kMergeSamples = 256, kMergeWindow = 8;   // kChunk = samples x window
+constexpr int kMergeRuns = 16, kFewRuns = 4;
+constexpr unsigned kMergeSamples = 256, kMergeWindow = 8;   // (a chunk: samples x window, or twice that)
 
 struct EmbedClear {
     float* p;
@@ -94,6 +94,7 @@ struct EmbedSortArgs {
     int vocab;
     unsigned* id;     // sorted within each chunk; ids outside [0, vocab) are `vocab`
     unsigned* place;
+    unsigned* n_spans;   // two counts, set to 0
     EmbedClear clear;
 };
 // The value of the lane whose number differs in bit kXor.
@@ -121,7 +122,7 @@ __device__ __forceinline__ unsigned from_lane(unsigned v)
 }
 // One step of a bitonic sort of the workgroup's keys, four neighbours a lane: keys kStep apart are put in order, ascending where the bit
 // kSize of their place is clear.
-template <int kSize, int kStep>
+template <int kChunk, int kSize, int kStep>
 __device__ __forceinline__ void sort_step(unsigned (&key)[kSortKeys], unsigned (*across)[kChunk])
 {
     const unsigned first = threadIdx.x * kSortKeys;
@@ -155,22 +156,25 @@ __device__ __forceinline__ void sort_step(unsigned (&key)[kSortKeys], unsigned (
         for (int k = 0; k < kSortKeys; k++) key[k] = low ? min(key[k], other[k]) : max(key[k], other[k]);
     }
 }
-template <int kSize, int kStep>
+template <int kChunk, int kSize, int kStep>
 __device__ __forceinline__ void sort_steps(unsigned (&key)[kSortKeys], unsigned (*across)[kChunk])
 {
-    sort_step<kSize, kStep>(key, across);
-    if constexpr (kStep > 1) sort_steps<kSize, kStep / 2>(key, across);
-    else if constexpr (kSize < kChunk) sort_steps<kSize * 2, kSize>(key, across);
+    sort_step<kChunk, kSize, kStep>(key, across);
+    if constexpr (kStep > 1) sort_steps<kChunk, kSize, kStep / 2>(key, across);
+    else if constexpr (kSize < kChunk) sort_steps<kChunk, kSize * 2, kSize>(key, across);
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedSortArgs a)
+template <int kBits>
+__global__ __launch_bounds__((1 << kBits) / kSortKeys) void embed_sort_kernel(const EmbedSortArgs a)
 {
+    constexpr int kChunk = 1 << kBits, kSortThreads = kChunk / kSortKeys;
     if (blockIdx.x >= a.clear.first_wg) {
         clear_part<kSortThreads>(a.clear);
         return;
     }
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.n_spans[threadIdx.x] = 0;
     __shared__ __align__(16) unsigned across[2][kChunk];
-    const unsigned base = blockIdx.x << kChunkBits, first = threadIdx.x * kSortKeys;
+    const unsigned base = blockIdx.x << kBits, first = threadIdx.x * kSortKeys;
     unsigned key[kSortKeys];
 #pragma unroll
     for (int k = 0; k < kSortKeys; k++) {
@@ -179,27 +183,28 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedSor
         if (row < a.rows) {
             const unsigned b = row / a.L, t = row - b * a.L;
             const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
-            key[k] = (unsigned)(id >= 0 && id < a.vocab ? id : a.vocab) << kChunkBits | (first + k);
+            key[k] = (unsigned)(id >= 0 && id < a.vocab ? id : a.vocab) << kBits | (first + k);
         }
     }
-    sort_steps<2, 1>(key, across);
+    sort_steps<kChunk, 2, 1>(key, across);
 #pragma unroll
     for (int k = 0; k < kSortKeys; k++) {
         const unsigned row = base + first + k;
         if (row < a.rows) {
-            a.id[row] = key[k] >> kChunkBits;
+            a.id[row] = key[k] >> kBits;
             a.place[row] = base + (key[k] & (kChunk - 1));
         }
     }
 }
 
-// Runs of `run` sorted places each, sixteen of them merged into one.
+// Runs of `run` sorted places each, kRuns of them merged into one.
 struct EmbedMergeArgs {
     const unsigned *id, *place;
     unsigned *to_id, *to_place;
     unsigned rows, run;
     EmbedClear clear;
 };
+template <int kRuns>
 __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a)
 {
     if (blockIdx.x >= a.clear.first_wg) {
@@ -207,10 +212,10 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
         return;
     }
     // (a run's places are whole workgroups)
-    __shared__ unsigned sample[kMergeRuns * kMergeSamples];
-    const unsigned run = a.run, r = blockIdx.x * 256 / run, first = r / kMergeRuns * kMergeRuns;
+    __shared__ unsigned sample[kRuns * kMergeSamples];
+    const unsigned run = a.run, r = blockIdx.x * 256 / run, first = r / kRuns * kRuns;
 #pragma unroll
-    for (int q = 0; q < kMergeRuns; q++) {
+    for (int q = 0; q < kRuns; q++) {
         const unsigned long long at = (unsigned long long)(first + q) * run + (threadIdx.x + 1) * (run / kMergeSamples) - 1;
         sample[q * kMergeSamples + threadIdx.x] = a.id[at < a.rows ? at : 0];   // (beyond the list: not looked at)
     }
@@ -218,9 +223,9 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
     const unsigned id = i < a.rows ? a.id[i] : 0, place = i < a.rows ? a.place[i] : 0;
     __syncthreads();
     if (i >= a.rows) return;
-    unsigned below[kMergeRuns], len[kMergeRuns];
+    unsigned below[kRuns], len[kRuns];
 #pragma unroll
-    for (int q = 0; q < kMergeRuns; q++) {
+    for (int q = 0; q < kRuns; q++) {
         const unsigned long long start = (unsigned long long)(first + q) * run;
         len[q] = first + q == r || start >= a.rows ? 0u : min(run, a.rows - (unsigned)start);
         below[q] = 0;
@@ -231,36 +236,37 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
 #pragma unroll
     for (unsigned step = kMergeSamples / 2; step > 0; step /= 2) {
 #pragma unroll
-        for (int q = 0; q < kMergeRuns; q++) {
+        for (int q = 0; q < kRuns; q++) {
             const unsigned other = sample[q * kMergeSamples + below[q] + step - 1];
             if ((below[q] + step) * part <= len[q] && precedes(q, other)) below[q] += step;
         }
     }
 #pragma unroll
-    for (int q = 0; q < kMergeRuns; q++) {   // (255 parts at most so far)
+    for (int q = 0; q < kRuns; q++) {   // (255 parts at most so far)
         const unsigned other = sample[q * kMergeSamples + below[q]];
         if ((below[q] + 1) * part <= len[q] && precedes(q, other)) below[q]++;
         below[q] *= part;
     }
     // long runs: halves of a part, all runs' loads of a step in flight at once, down to eight places; those are looked at together
     for (unsigned step = part / 2; step >= kMergeWindow; step /= 2) {
-        unsigned other[kMergeRuns];
+        unsigned other[kRuns];
 #pragma unroll
-        for (int q = 0; q < kMergeRuns; q++) other[q] = a.id[below[q] + step <= len[q] ? (first + q) * run + below[q] + step - 1 : i];
+        for (int q = 0; q < kRuns; q++) other[q] = a.id[below[q] + step <= len[q] ? (first + q) * run + below[q] + step - 1 : i];
 #pragma unroll
-        for (int q = 0; q < kMergeRuns; q++)
+        for (int q = 0; q < kRuns; q++)
             if (below[q] + step <= len[q] && precedes(q, other[q])) below[q] += step;
     }
+    constexpr int kTogether = kRuns < 8 ? kRuns : 8;
 #pragma unroll
-    for (int q0 = 0; q0 < kMergeRuns; q0 += 4) {
-        unsigned window[4][kMergeWindow];
+    for (int q0 = 0; q0 < kRuns; q0 += kTogether) {
+        unsigned window[kTogether][kMergeWindow];
 #pragma unroll
-        for (int q = 0; q < 4; q++) {   // (the lists are as long as whole chunks; a run that is not there: this place's own)
+        for (int q = 0; q < kTogether; q++) {   // (the lists are as long as whole chunks; a run that is not there: this place's own)
             const unsigned at = below[q0 + q] < len[q0 + q] ? (first + q0 + q) * run + below[q0 + q] : i & ~(kMergeWindow - 1u);
             __builtin_memcpy(window[q], __builtin_assume_aligned(a.id + at, 16), sizeof window[q]);
         }
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < kTogether; q++) {
             unsigned count = 0;
 #pragma unroll
             for (unsigned k = 0; k < kMergeWindow; k++) count += below[q0 + q] + k < len[q0 + q] && precedes(q0 + q, window[q][k]);
@@ -269,21 +275,23 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
     }
     unsigned to = first * run + (i - r * run);
 #pragma unroll
-    for (int q = 0; q < kMergeRuns; q++) to += below[q];
+    for (int q = 0; q < kRuns; q++) to += below[q];
     a.to_id[to] = id;
     a.to_place[to] = place;
 }
 
 // A wave sums a slice of neighbouring places over 512 channels, eight a lane.  A run of one id that lies within the slice gives its row of
 // dtable; what a run that goes on into the next slice, or came from the one before, adds up to here is left in the slice's two slots
-// for embed_join_kernel.
+// for embed_join_kernel, and the slice in which such a run starts is put on a list (whose order says nothing about any sum).
 constexpr int kMaxSlice = 64;
 constexpr int kSumCols = 512;
+constexpr unsigned kShortSpan = 16;   // slices that a short run reaches into at most
 struct EmbedSumArgs {
     const unsigned *id, *place;
     RowView dout;
     float* dtable;
     float* slots;   // [slices][2][d]: of the run that came into the slice, of the one that starts in it and goes on
+    unsigned *n_spans, *span;   // lists of slices in which a run starts that goes on: short runs, and after `slices` entries long ones
     unsigned rows, L;
     int d, vocab, slice, col_blocks;
     unsigned slices;
@@ -372,6 +380,11 @@ __device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice,
         }
     }
     flush(cur == after);
+    if (block == 0 && lane == 0 && !came && cur == after && cur < (unsigned)a.vocab) {
+        const unsigned long long far = (unsigned long long)(slice + 1 + kShortSpan) * a.slice;
+        const bool long_run = far < a.rows && a.id[far] == cur;
+        a.span[(long_run ? a.slices : 0) + atomicAdd(a.n_spans + long_run, 1u)] = slice;
+    }
 }
 template <typename IO>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
@@ -383,58 +396,84 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
     else sum_slice<IO, 1>(a, slice, block, lane);
 }
 
-// The rows of runs that span slices: the workgroup of the slice in which a run starts adds up its slots, 256 channels at a time, the
-// waves a share of the slices each.
-constexpr int kJoinWaves = 8, kJoinCols = 256;
+// The rows of runs that span slices.  256 channels of a short run: a wave adds up its slots.  Of a long run: a workgroup, the waves a
+// share of the slots each.
+constexpr int kJoinWaves = 16, kJoinCols = 256, kShortGroups = 256, kLongGroups = 32;
 struct EmbedJoinArgs {
     const unsigned* id;
     const float* slots;
     float* dtable;
-    unsigned slices;
-    int d, vocab, slice;
+    const unsigned *n_spans, *span;
+    unsigned slices, short_groups;
+    int d, slice, col_blocks;
     float scale;
 };
+__device__ __forceinline__ void add_floats(float (&acc)[4], const float* row, int col, int d)
+{
+    float f[4] = {};
+    if (col + 4 <= d) {
+        __builtin_memcpy(f, row + col, sizeof f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (col + i < d) f[i] = row[col + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) acc[i] += f[i];
+}
 __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedJoinArgs a)
 {
-    const unsigned slice = blockIdx.x, i0 = slice * a.slice, i1 = i0 + a.slice;   // (the last slice has no workgroup)
-    const unsigned v = a.id[i1 - 1];
-    if (v >= (unsigned)a.vocab || a.id[i1] != v || (a.id[i0] == v && i0 > 0 && a.id[i0 - 1] == v)) return;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, col = blockIdx.y * kJoinCols + lane * 4;
-    // the last slice that the run came into: 64 slices are looked at together
-    unsigned last = slice + 1;
-    for (unsigned range = a.slices - last; range > 1;) {
-        const unsigned step = (range + 63) / 64, at = last + lane * step;
-        const unsigned long long in = __ballot(lane * step < range && a.id[lane * step < range ? (unsigned long long)at * a.slice : i1] == v);
-        const unsigned count = __popcll(in);   // (a prefix of the lanes, the first among them)
-        range = min(step, range - (count - 1) * step);
-        last += (count - 1) * step;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const auto slot = [&](unsigned s, int which) { return a.slots + ((long long)s * 2 + which) * a.d; };
+    if (blockIdx.x < a.short_groups) {
+        const unsigned n = a.n_spans[0];
+        for (unsigned long long w = blockIdx.x * kJoinWaves + wave; w < (unsigned long long)n * a.col_blocks; w += a.short_groups * kJoinWaves) {
+            const unsigned k = w / a.col_blocks, slice = a.span[k];
+            const int col = (int)(w - (unsigned long long)k * a.col_blocks) * kJoinCols + lane * 4;
+            const unsigned v = a.id[(unsigned long long)(slice + 1) * a.slice];
+            const unsigned s = slice + 1 + min((unsigned)lane, kShortSpan);
+            const unsigned slots = __popcll(__ballot((unsigned)lane < kShortSpan && s < a.slices && a.id[s < a.slices ? (unsigned long long)s * a.slice : 0] == v));
+            float acc[4] = {};
+            add_floats(acc, slot(slice, 1), col, a.d);
+#pragma unroll 4
+            for (unsigned i = 1; i <= slots; i++) add_floats(acc, slot(slice + i, 0), col, a.d);
+#pragma unroll
+            for (int i = 0; i < 4; i++) acc[i] *= a.scale;
+            store_piece_of<IoF32>(a.dtable + (long long)v * a.d, col, a.d, acc);
+        }
+        return;
     }
     __shared__ float sum[kJoinWaves][kJoinCols];
-    float acc[4] = {};
-    auto add = [&](const float* row) {
-        float f[4] = {};
-        if (col + 4 <= a.d) {
-            __builtin_memcpy(f, row + col, sizeof f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (col + i < a.d) f[i] = row[col + i];
+    const unsigned n = a.n_spans[1], first = blockIdx.x - a.short_groups;
+    for (unsigned long long w = first; w < (unsigned long long)n * a.col_blocks; w += gridDim.x - a.short_groups) {
+        const unsigned k = w / a.col_blocks, slice = a.span[a.slices + k];
+        const int block = (int)(w - (unsigned long long)k * a.col_blocks), col = block * kJoinCols + lane * 4;
+        const unsigned long long i1 = (unsigned long long)(slice + 1) * a.slice;
+        const unsigned v = a.id[i1];
+        // the last slice that the run came into: 64 slices are looked at together
+        unsigned last = slice + 1;
+        for (unsigned range = a.slices - last; range > 1;) {
+            const unsigned step = (range + 63) / 64, at = last + lane * step;
+            const unsigned long long in = __ballot(lane * step < range && a.id[lane * step < range ? (unsigned long long)at * a.slice : i1] == v);
+            const unsigned count = __popcll(in);   // (a prefix of the lanes, the first among them)
+            range = min(step, range - (count - 1) * step);
+            last += (count - 1) * step;
         }
-#pragma unroll
-        for (int i = 0; i < 4; i++) acc[i] += f[i];
-    };
-    if (wave == 0) add(a.slots + ((long long)slice * 2 + 1) * a.d);
+        float acc[4] = {};
+        if (wave == 0) add_floats(acc, slot(slice, 1), col, a.d);
 #pragma unroll 8
-    for (unsigned s = slice + 1 + wave; s <= last; s += kJoinWaves) add(a.slots + (long long)s * 2 * a.d);
+        for (unsigned s = slice + 1 + wave; s <= last; s += kJoinWaves) add_floats(acc, slot(s, 0), col, a.d);
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; i++) sum[wave][lane * 4 + i] = acc[i];
-    __syncthreads();
-    const int c = blockIdx.y * kJoinCols + threadIdx.x;
-    if (threadIdx.x < kJoinCols && c < a.d) {
-        float f = 0.0f;
+        for (int i = 0; i < 4; i++) sum[wave][lane * 4 + i] = acc[i];
+        __syncthreads();
+        const int c = block * kJoinCols + threadIdx.x;
+        if (threadIdx.x < kJoinCols && c < a.d) {
+            float f = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kJoinWaves; k++) f += sum[k][threadIdx.x];
-        a.dtable[(long long)v * a.d + c] = a.scale * f;
+            for (int i = 0; i < kJoinWaves; i++) f += sum[i][threadIdx.x];
+            a.dtable[(long long)v * a.d + c] = a.scale * f;
+        }
     }
 }
 
@@ -451,21 +490,24 @@ int check_embed(const bimamba_embed_desc* d)
 
 // Places to a slice: as many as 64, fewer where that leaves the chip short of two waves per SIMD.
 struct EmbedPlan {
-    unsigned rows, chunks, slices;
+    unsigned rows, chunk, chunks, slices;
     int slice, col_blocks;
-    size_t list, total;   // bytes of one list of ids or places, and of the workspace
+    size_t list, slots, total;   // bytes of one list of ids or places, of the slots, and of the workspace
 };
 EmbedPlan plan_embed(const bimamba_embed_desc* d)
 {
     EmbedPlan p{};
     p.rows = (unsigned)((long long)d->batch * d->seqlen);
-    p.chunks = (p.rows + kChunk - 1) / kChunk;
+    // (up to 4096 places need no merge then: 3711 of them 38 -> 34 us)
+    p.chunk = d->vocab < 1 << (32 - kLargeChunkBits) && p.rows > 1u << kChunkBits ? 1u << kLargeChunkBits : 1u << kChunkBits;
+    p.chunks = (p.rows + p.chunk - 1) / p.chunk;
     p.col_blocks = (d->d_model + kSumCols - 1) / kSumCols;
     p.slice = kMaxSlice;
     while (p.slice > 8 && (long long)(p.rows / p.slice) * p.col_blocks < 8 * cu_count()) p.slice /= 2;
     p.slices = (p.rows + p.slice - 1) / p.slice;
-    p.list = (size_t)p.chunks * kChunk * 4;   // (whole chunks: a merge reads eight places at a time)
-    p.total = 4 * p.list + (size_t)p.slices * 2 * d->d_model * sizeof(float);
+    p.list = (size_t)p.chunks * p.chunk * 4;   // (whole chunks: a merge reads eight places at a time)
+    p.slots = ((size_t)p.slices * 2 * d->d_model * sizeof(float) + 15) / 16 * 16;
+    p.total = 4 * p.list + p.slots + (2 * (size_t)p.slices + 2) * sizeof(unsigned);   // (and the lists of runs that span slices, after their lengths)
     return p;
 }
 
@@ -529,33 +571,41 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     unsigned *id = reinterpret_cast<unsigned*>(ws), *place = reinterpret_cast<unsigned*>(ws + p.list);
     unsigned *to_id = reinterpret_cast<unsigned*>(ws + 2 * p.list), *to_place = reinterpret_cast<unsigned*>(ws + 3 * p.list);
     float* const slots = reinterpret_cast<float*>(ws + 4 * p.list);
+    unsigned *const n_spans = reinterpret_cast<unsigned*>(ws + 4 * p.list + p.slots), *const span = n_spans + 2;
     // the table is cleared beside the sort and, where there is one, the first merge
     const long long all = (long long)d->vocab * d->d_model;
-    const long long half = p.rows > kChunk ? (all / 2 + kClearFloats - 1) / kClearFloats * kClearFloats : all, early = half < all ? half : all;
+    const long long half = p.rows > p.chunk ? (all / 2 + kClearFloats - 1) / kClearFloats * kClearFloats : all, early = half < all ? half : all;
     const auto wgs = [](long long n) { return (unsigned)((n + kClearFloats - 1) / kClearFloats); };
     const EmbedSortArgs sa{tokens->ptr, tokens->stride_batch, tokens->stride_token, p.rows, (unsigned)d->seqlen, d->vocab, id, place,
-                           EmbedClear{dtable, early, p.chunks}};
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(p.chunks + wgs(early)), dim3(kSortThreads), 0, st, sa);
+                           n_spans, EmbedClear{dtable, early, p.chunks}};
+    if (p.chunk == 1u << kChunkBits) hipLaunchKernelGGL(embed_sort_kernel<kChunkBits>, dim3(p.chunks + wgs(early)), dim3(p.chunk / kSortKeys), 0, st, sa);
+    else hipLaunchKernelGGL(embed_sort_kernel<kLargeChunkBits>, dim3(p.chunks + wgs(early)), dim3(p.chunk / kSortKeys), 0, st, sa);
     if (p.rows == 0) return launches.status();
     long long left = all - early;
-    for (unsigned long long run = kChunk; run < p.rows; run *= kMergeRuns) {
+    for (unsigned long long run = p.chunk; run < p.rows; run *= kMergeRuns) {
         const unsigned merge_wgs = (p.rows + 255) / 256;
         const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run, EmbedClear{dtable + early, left, merge_wgs}};
-        hipLaunchKernelGGL(embed_merge_kernel, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
+        // (few runs: less to look at.  3711 places 15 -> 10 us)
+        if (run * kFewRuns >= p.rows) hipLaunchKernelGGL(embed_merge_kernel<kFewRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
+        else hipLaunchKernelGGL(embed_merge_kernel<kMergeRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
         left = 0;
         unsigned* const i = id;
         unsigned* const q = place;
         id = to_id, place = to_place;
         to_id = i, to_place = q;
     }
-    const EmbedSumArgs a{id, place, row_view(dout), dtable, slots, p.rows, (unsigned)d->seqlen, d->d_model, d->vocab, p.slice, p.col_blocks,
+    const EmbedSumArgs a{id, place, row_view(dout), dtable, slots, n_spans, span, p.rows, (unsigned)d->seqlen, d->d_model, d->vocab, p.slice, p.col_blocks,
                          p.slices, d->scale};
     const unsigned sum_wgs = (unsigned)(((unsigned long long)p.slices * p.col_blocks + 3) / 4);
     if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(sum_wgs), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(sum_wgs), dim3(256), 0, st, a);
     if (p.slices > 1) {
-        const EmbedJoinArgs ja{id, slots, dtable, p.slices, d->d_model, d->vocab, p.slice, d->scale};
-        hipLaunchKernelGGL(embed_join_kernel, dim3(p.slices - 1, (d->d_model + kJoinCols - 1) / kJoinCols), dim3(64 * kJoinWaves), 0, st, ja);
+        EmbedJoinArgs ja{id, slots, dtable, n_spans, span, p.slices, kShortGroups, d->d_model, p.slice, 0, d->scale};
+        ja.col_blocks = (d->d_model + kJoinCols - 1) / kJoinCols;
+        const unsigned long long most = ((unsigned long long)p.slices * ja.col_blocks + kJoinWaves - 1) / kJoinWaves;
+        if (ja.short_groups > most) ja.short_groups = (unsigned)most;
+        const unsigned long_groups = p.slices - 1 > kShortSpan ? kLongGroups : 1;   // (one: for none)
+        hipLaunchKernelGGL(embed_join_kernel, dim3(ja.short_groups + long_groups), dim3(64 * kJoinWaves), 0, st, ja);
     }
     return launches.status();
 }
