@@ -37,14 +37,29 @@ __device__ __forceinline__ float value_of(Key k)
     return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 __device__ __forceinline__ unsigned id_of(Key k) { return ~(unsigned)k; }
-__device__ __forceinline__ Key wave_max_key(Key k)
+// The largest key of a row of sixteen lanes or of all 64, in all of them: the largest upper half, and the largest lower half beside that.
+template <int kLanes>
+__device__ __forceinline__ unsigned lanes_max(unsigned v)
 {
-#pragma unroll
-    for (int step = 32; step > 0; step /= 2) {
-        const Key other = __shfl_xor(k, step);
-        if (other > k) k = other;
+#define BM_DPP(ctrl) (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, true)
+    v = max(v, BM_DPP(0xB1));    // quad_perm 1 0 3 2
+    v = max(v, BM_DPP(0x4E));    // quad_perm 2 3 0 1
+    v = max(v, BM_DPP(0x141));   // row_half_mirror
+    v = max(v, BM_DPP(0x140));   // row_mirror
+#undef BM_DPP
+    if constexpr (kLanes == 64) {
+        auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(r[0], r[1]);
+        r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(r[0], r[1]);
     }
-    return k;
+    return v;
+}
+template <int kLanes>
+__device__ __forceinline__ Key lanes_max_key(Key k)
+{
+    const unsigned hi = lanes_max<kLanes>((unsigned)(k >> 32)), lo = lanes_max<kLanes>((unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
+    return (Key)hi << 32 | lo;
 }
 
 struct ScoresArgs {
@@ -91,14 +106,18 @@ __device__ __forceinline__ void store_top(const ScoresArgs& a, unsigned row, int
     if (a.top_token) a.top_token[(long long)row * a.top_k + k] = none ? -1 : (int64_t)id_of(key);
 }
 
-// A workgroup takes a row, or one of its `splits` parts where there are few rows.  With kTop a lane also keeps which of its pieces
-// first had the largest logit.  The best pieces of the lanes are all different, so the k lanes with the best of them hold
-// the k best logits of the row: these lanes' pieces alone are read again (from the caches), spread over all lanes, k times for the
-// best logit below the one before.
-constexpr int kScoresThreads = 256, kScoresWaves = kScoresThreads / 64, kScoresAhead = 4;
-template <typename IO, bool kEntropy, bool kTop, int kPiece>
+// A workgroup takes a row, or one of its `splits` parts.  With kTop a lane also keeps which of its pieces first had the largest logit.
+// Of sixteen groups of lanes each has a best piece; the k-th best of these sixteen bounds what the k best logits of the row can be, and
+// holds back all but a few: only lanes whose own best piece reaches it have any, a dozen as a rule.  Their pieces are read again (from the
+// caches), spread over all lanes, and the logits that reach the bound go on a list, where each counts how many are better.  A row
+// that has more of them than the list holds (equal ones, or many large ones that one lane read) looks for the best logit below the one
+// before, k times.
+constexpr int kScoresAhead = 4, kMaxListed = 256;
+constexpr int kManyRowsThreads = 256, kFewRowsThreads = 1024;
+template <typename IO, bool kEntropy, bool kTop, int kPiece, int kScoresThreads>
 __device__ __forceinline__ void scores_row(const ScoresArgs& a)
 {
+    constexpr int kScoresWaves = kScoresThreads / 64, kGroups = 16, kGroupLanes = kScoresThreads / kGroups;   // (kMaxTop groups or more)
     const unsigned row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
     const unsigned b = row / a.L, t = row - b * a.L;
     const long long target = target_of(a, b, t);
@@ -143,8 +162,8 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
     }
     // over the workgroup
     __shared__ Stats part[kScoresWaves];
-    __shared__ Key wave_key[kScoresWaves * kMaxTop], best_key[kScoresWaves];
-    __shared__ int chosen[kMaxTop], n_chosen;
+    __shared__ Key group_key[kGroups], best_key[kScoresWaves], listed[kMaxListed];
+    __shared__ int chosen[kScoresThreads], n_chosen, n_listed;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     move_to<kEntropy>(s, wave_max(s.m));
     s.s = wave_sum(s.s);
@@ -153,28 +172,21 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
     Key mine = 0;
     if constexpr (kTop) {
         mine = best_piece == ~0u ? 0 : key_of(best, best_piece * kPiece);
-        Key left = mine;
-        for (int k = 0; k < a.top_k; k++) {
-            const Key top = wave_max_key(left);
-            if (left == top) left = 0;
-            if (lane == 0) wave_key[wave * a.top_k + k] = top;
-        }
-        if (threadIdx.x == 0) n_chosen = 0;
+        const Key top = lanes_max_key<kGroupLanes>(mine);
+        if (threadIdx.x % kGroupLanes == 0) group_key[threadIdx.x / kGroupLanes] = top;
+        if (threadIdx.x == 0) n_chosen = n_listed = 0;
     }
     __syncthreads();
-    s = part[0];
+    s.m = part[0].m;
 #pragma unroll
     for (int w = 1; w < kScoresWaves; w++) s.m = fmaxf(s.m, part[w].m);
-    {
-        Stats all{s.m, 0.0f, 0.0f};
+    s.s = s.t = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kScoresWaves; w++) {
-            Stats q = part[w];
-            move_to<kEntropy>(q, all.m);
-            all.s += q.s;
-            all.t += q.t;
-        }
-        s = all;
+    for (int w = 0; w < kScoresWaves; w++) {
+        Stats q = part[w];
+        move_to<kEntropy>(q, s.m);
+        s.s += q.s;
+        if constexpr (kEntropy) s.t += q.t;
     }
     const bool whole = a.splits == 1;
     if (threadIdx.x == 0) {
@@ -182,54 +194,79 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
         else a.part[blockIdx.x] = s;
     }
     if constexpr (kTop) {
-        // the k-th best of the lanes' best pieces
+        const auto store = [&](int k, Key key) {
+            if (whole) store_top(a, row, k, s, key);
+            else a.part_top[(long long)blockIdx.x * a.top_k + k] = key;
+        };
+        // the k-th best of the groups' best pieces (or none, of fewer pieces)
         Key threshold = 0;
         {
-            const int count = kScoresWaves * a.top_k;
-            const Key own = lane < count ? wave_key[lane] : 0;
-            int above = 0;
-            for (int j = 0; j < count; j++) above += wave_key[j] > own;
-            const unsigned long long at = __ballot(lane < count && above == a.top_k - 1);
+            const Key own = group_key[lane % kGroups];
+            int better = 0;
+#pragma unroll
+            for (int g = 0; g < kGroups; g++) better += group_key[g] > own;
+            const unsigned long long at = __ballot(better == a.top_k - 1);
             if (at) threshold = __shfl(own, __builtin_ctzll(at));
         }
-        if (mine != 0 && mine >= threshold) chosen[atomicAdd(&n_chosen, 1)] = threadIdx.x;   // (top_k of them at most)
+        if (mine != 0 && mine >= threshold) chosen[atomicAdd(&n_chosen, 1)] = threadIdx.x;
         __syncthreads();
         const int rounds = (pieces + kScoresThreads - 1) / kScoresThreads, items = n_chosen * rounds;
-        Key below = ~0ull;
-        for (int k = 0; k < a.top_k; k++) {
-            Key top = 0;
+        // (the logits of the threshold's piece come first among its equals; any of the piece may be the one)
+        const Key bound = threshold == 0 ? 1 : threshold - (kPiece - 1);
+        const auto for_items = [&](auto use) {
             for (int item = threadIdx.x; item < items; item += kScoresThreads) {
                 const int which = item / rounds, piece = (item - which * rounds) * kScoresThreads + chosen[which];
                 if (piece < pieces) {
                     const Piece<IO, kPiece> p = load_piece_of<IO, kPiece>(x, piece * kPiece, n, lowest);
 #pragma unroll
-                    for (int i = 0; i < kPiece; i++) {
-                        const Key key = piece * kPiece + i < n ? key_of(p[i], from + piece * kPiece + i) : 0;
-                        if (key < below && key > top) top = key;
-                    }
+                    for (int i = 0; i < kPiece; i++) use(piece * kPiece + i < n ? key_of(p[i], piece * kPiece + i) : 0);
                 }
             }
-            top = wave_max_key(top);
-            __syncthreads();
-            if (lane == 0) best_key[wave] = top;
-            __syncthreads();
+        };
+        for_items([&](Key key) {
+            if (key >= bound) {
+                const int at = atomicAdd(&n_listed, 1);
+                if (at < kMaxListed) listed[at] = key;
+            }
+        });
+        __syncthreads();
+        const int count = n_listed;
+        if (count <= kMaxListed) {
+            for (int c = threadIdx.x; c < max(count, a.top_k); c += kScoresThreads) {
+                const Key key = c < count ? listed[c] : 0;
+                int better = c < count ? 0 : c;   // (fewer logits than alternatives, in a part of a row: none)
+                if (c < count) {
+#pragma unroll 4
+                    for (int j = 0; j < count; j++) better += listed[j] > key;
+                }
+                if (better < a.top_k) store(better, key == 0 ? 0 : key - from);   // (ids count down: those of the row)
+            }
+        } else {
+            Key below = ~0ull;
+            for (int k = 0; k < a.top_k; k++) {
+                Key top = 0;
+                for_items([&](Key key) {
+                    if (key < below && key > top) top = key;
+                });
+                top = lanes_max_key<64>(top);
+                __syncthreads();
+                if (lane == 0) best_key[wave] = top;
+                __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kScoresWaves; w++) top = best_key[w] > top ? best_key[w] : top;
-            below = top;
-            if (threadIdx.x == 0) {
-                if (whole) store_top(a, row, k, s, top);
-                else a.part_top[(long long)blockIdx.x * a.top_k + k] = top;
+                for (int w = 0; w < kScoresWaves; w++) top = best_key[w] > top ? best_key[w] : top;
+                below = top;
+                if (threadIdx.x == 0) store(k, top == 0 ? 0 : top - from);
             }
         }
     }
 }
-
-template <typename IO, bool kEntropy, bool kTop>
-__global__ __launch_bounds__(kScoresThreads) void scores_kernel(const ScoresArgs a)
+template <typename IO, bool kEntropy, bool kTop, int kThreads>
+__global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresArgs a)
 {
-    // (rows shorter than a piece: a logit a lane)
-    if (a.vocab >= kPieceOf<IO>) scores_row<IO, kEntropy, kTop, kPieceOf<IO>>(a);
-    else scores_row<IO, kEntropy, kTop, 1>(a);
+    if constexpr (kThreads == kManyRowsThreads) {   // (rows shorter than a piece: a logit a lane)
+        if (a.vocab < kPieceOf<IO>) return scores_row<IO, kEntropy, kTop, 1, kThreads>(a);
+    }
+    scores_row<IO, kEntropy, kTop, kPieceOf<IO>, kThreads>(a);
 }
 
 // A wave joins the parts of a row, a part a lane; the lanes' alternatives are in descending order already.
@@ -261,7 +298,7 @@ __global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
     }
     if constexpr (kTop) {
         for (int k = 0; k < a.top_k; k++) {
-            const Key best = wave_max_key(top[0]);
+            const Key best = lanes_max_key<64>(top[0]);
             if (top[0] == best)
 #pragma unroll
                 for (int i = 0; i < kMaxTop; i++) top[i] = i + 1 < kMaxTop ? top[i + 1] : 0;
@@ -350,10 +387,14 @@ int check_logits(const bimamba_logits_desc* d)
     return BIMAMBA_OK;
 }
 
-// Parts of a row: until four workgroups a CU exist, none of them under 2048 logits.
+// Up to a row a CU, of up to 65536 logits: a workgroup of sixteen waves each, in one launch (32 x 50304 bf16 with entropy and eight
+// alternatives 10.1 us; of four waves each, in 25 parts, 7.2 and 4.4 for the second launch; 256 x 50304 11.2 against 11.9 and 4.0).  Longer rows go
+// in parts until four workgroups a CU exist, none of them under 2048 logits (4 x 130001: 5.8 and 3.9 against 11.9 and 4.0 in two
+// parts of sixteen waves; 300 rows 24 and 4.5).  More rows: a workgroup of four waves each (600 x 50304 20.6 us; in two parts 18.4 and 4.8;
+// 900 rows with sixteen waves 37.6 against 25.5).
 struct ScoresPlan {
     unsigned rows;
-    int splits, per_split;
+    int threads, splits, per_split;
     size_t stats, total;   // bytes of the parts' statistics, and of the workspace
 };
 ScoresPlan plan_scores(const bimamba_logits_desc* d)
@@ -361,12 +402,13 @@ ScoresPlan plan_scores(const bimamba_logits_desc* d)
     ScoresPlan p{};
     p.rows = (unsigned)((long long)d->batch * d->seqlen);
     p.splits = 1;
-    if (p.rows > 0) {
-        const long long want = (4ll * cu_count() + p.rows - 1) / p.rows, most = d->vocab / 2048;
+    p.threads = p.rows <= (unsigned)cu_count() && d->vocab > 4096 && d->vocab <= 65536 ? kFewRowsThreads : kManyRowsThreads;
+    if (d->vocab > 65536 && p.rows > 0) {
+        const long long want = 4ll * cu_count() / p.rows, most = (d->vocab + 2047) / 2048;
         p.splits = (int)(want < most ? want : most);
-        if (p.splits > kMaxSplits) p.splits = kMaxSplits;
-        if (p.splits < 1) p.splits = 1;
     }
+    if (p.splits > kMaxSplits) p.splits = kMaxSplits;
+    if (p.splits < 1) p.splits = 1;
     p.per_split = ((d->vocab + p.splits - 1) / p.splits + 7) / 8 * 8;   // (whole pieces of either type)
     for (;; p.per_split += 8) {   // (no last part shorter than a piece)
         p.splits = (d->vocab + p.per_split - 1) / p.per_split;
@@ -380,19 +422,21 @@ ScoresPlan plan_scores(const bimamba_logits_desc* d)
 }
 
 template <typename IO, bool kEntropy, bool kTop>
-void launch_scores(const ScoresArgs& a, hipStream_t st)
+void launch_scores(const ScoresArgs& a, int threads, hipStream_t st)
 {
-    hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop>), dim3(a.rows * (unsigned)a.splits), dim3(kScoresThreads), 0, st, a);
+    const dim3 grid(a.rows * (unsigned)a.splits), wg(threads);
+    if (threads == kFewRowsThreads) hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kFewRowsThreads>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kManyRowsThreads>), grid, wg, 0, st, a);
     if (a.splits > 1) hipLaunchKernelGGL((scores_join_kernel<IO, kEntropy, kTop>), dim3(a.rows), dim3(64), 0, st, a);
 }
 template <typename IO>
-void launch_scores(const ScoresArgs& a, hipStream_t st)
+void launch_scores(const ScoresArgs& a, int threads, hipStream_t st)
 {
     const bool top = a.top_k > 0;
-    if (a.entropy && top) launch_scores<IO, true, true>(a, st);
-    else if (a.entropy) launch_scores<IO, true, false>(a, st);
-    else if (top) launch_scores<IO, false, true>(a, st);
-    else launch_scores<IO, false, false>(a, st);
+    if (a.entropy && top) launch_scores<IO, true, true>(a, threads, st);
+    else if (a.entropy) launch_scores<IO, true, false>(a, threads, st);
+    else if (top) launch_scores<IO, false, true>(a, threads, st);
+    else launch_scores<IO, false, false>(a, threads, st);
 }
 
 }  // namespace
@@ -441,8 +485,8 @@ int bimamba_log_probs(const bimamba_logits_desc* d, const bimamba_tensor* logits
     a.splits = p.splits, a.per_split = p.per_split, a.targets_only = d->targets_only;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    if (d->io_dtype == BIMAMBA_BF16) launch_scores<IoBF16>(a, st);
-    else launch_scores<IoF32>(a, st);
+    if (d->io_dtype == BIMAMBA_BF16) launch_scores<IoBF16>(a, p.threads, st);
+    else launch_scores<IoF32>(a, p.threads, st);
     return launches.status();
 }
 
