@@ -349,28 +349,33 @@ _TORCH = (torch.float32, torch.bfloat16)
 _NAMES = {"f32": F32, "bf16": BF16}
 
 
-def _rows(t, what, dtype, *shape):
-    """[batch, L, width] activations -> Tensor."""
-    assert t.dtype is dtype and tuple(t.shape) == shape and t.is_cuda, "%s: %s %s, wanted %s %s on the GPU" % (
-        what, t.dtype, tuple(t.shape), dtype, shape)
-    s = t.stride()
-    assert s[2] == 1 or shape[2] == 1 or t.numel() == 0, "%s: the channel dimension must be contiguous" % what
-    return Tensor(t.data_ptr(), s[0], s[1])
+def _wrong(t, what, dtype, shape, more=""):
+    raise AssertionError("%s: %s %s with strides %s on %s, wanted %s %s on the GPU%s" % (
+        what, t.dtype, tuple(t.shape), t.stride(), t.device, dtype, tuple(shape), more))
 
 
-def _ids(t, what, *shape):
-    assert t.dtype is torch.int64 and tuple(t.shape) == shape and t.is_cuda, "%s: %s %s, wanted torch.int64 %s on the GPU" % (
-        what, t.dtype, tuple(t.shape), shape)
-    s = t.stride()
-    return Tokens(t.data_ptr(), s[0], s[1])
+def _rows(t, what, dtype, shape):
+    """[batch, L, width] activations -> Tensor.  (The host's share of a small call counts: each check reads what it needs once.)"""
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape:
+        _wrong(t, what, dtype, shape)
+    sb, st, s1 = t.stride()
+    if s1 != 1 and shape[2] != 1 and t.numel() != 0:
+        _wrong(t, what, dtype, shape, ", the channels contiguous")
+    return Tensor(t.data_ptr(), sb, st)
 
 
-def _flat(t, what, *shape, dtype=torch.float32):
+def _ids(t, what, shape):
+    if t.dtype is not torch.int64 or not t.is_cuda or t.shape != shape:
+        _wrong(t, what, torch.int64, shape)
+    return Tokens(t.data_ptr(), *t.stride())
+
+
+def _flat(t, what, shape, dtype=torch.float32):
     """Contiguous device array of a shape, or None -> pointer."""
     if t is None:
         return None
-    assert t.dtype is dtype and tuple(t.shape) == shape and t.is_contiguous() and t.is_cuda, "%s: %s %s, wanted contiguous %s %s on the GPU" % (
-        what, t.dtype, tuple(t.shape), dtype, shape)
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        _wrong(t, what, dtype, shape, ", contiguous")
     return t.data_ptr()
 
 
@@ -378,13 +383,17 @@ def _vector(t, what, batch, d):
     """A parameter vector [d], or [batch, d] with unit stride along a vector -> (pointer, stride between vectors)."""
     if t is None:
         return None, None
-    assert t.dtype is torch.float32 and t.is_cuda and tuple(t.shape) in ((d,), (batch, d)), "%s: %s %s, wanted float32 [%d] or [%d, %d] on the GPU" % (
-        what, t.dtype, tuple(t.shape), d, batch, d)
-    assert t.stride(-1) == 1 or d == 1 or t.numel() == 0, "%s: a vector must be contiguous" % what
-    if t.dim() == 1:
+    shape = t.shape
+    if t.dtype is not torch.float32 or not t.is_cuda or (shape != (batch, d) and shape != (d,)):
+        _wrong(t, what, torch.float32, (batch, d), ", or one vector")
+    s = t.stride()
+    if s[-1] != 1 and d != 1 and t.numel() != 0:
+        _wrong(t, what, torch.float32, (batch, d), ", each vector contiguous")
+    if len(s) == 1:
         return t.data_ptr(), 0
-    stride = t.stride(0) if batch > 1 else d
-    assert stride >= d, "%s: vectors of batch elements must not overlap" % what
+    stride = s[0] if batch > 1 else d
+    if stride < d:
+        _wrong(t, what, torch.float32, (batch, d), ", the vectors apart")
     return t.data_ptr(), stride
 
 
@@ -400,9 +409,9 @@ def bimamba_embed(desc, tokens, table, out, stream=None, check=True):
     """Enqueue out[b, t] = scale * table[tokens[b, t]].  tokens: int64 [batch, L]; table [vocab, d_model] contiguous; out
     [batch, L, d_model]."""
     Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed(C.byref(desc), C.byref(_ids(tokens, "tokens", Bt, L)),
-                             _flat(table, "table", desc.vocab, D, dtype=_TORCH[desc.table_dtype]),
-                             C.byref(_rows(out, "out", _TORCH[desc.io_dtype], Bt, L, D)), _stream_ptr(stream))
+    rc = lib().bimamba_embed(C.byref(desc), C.byref(_ids(tokens, "tokens", (Bt, L))),
+                             _flat(table, "table", (desc.vocab, D), dtype=_TORCH[desc.table_dtype]),
+                             C.byref(_rows(out, "out", _TORCH[desc.io_dtype], (Bt, L, D))), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_embed")
     return rc
@@ -415,9 +424,9 @@ def bimamba_embed_bwd_workspace_bytes(desc):
 def bimamba_embed_bwd(desc, tokens, dout, dtable, workspace, stream=None, check=True):
     """Enqueue the gradient of the table: dtable float32 [vocab, d_model] contiguous, overwritten."""
     Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed_bwd(C.byref(desc), C.byref(_ids(tokens, "tokens", Bt, L)),
-                                 C.byref(_rows(dout, "dout", _TORCH[desc.io_dtype], Bt, L, D)),
-                                 _flat(dtable, "dtable", desc.vocab, D), *_workspace(workspace), _stream_ptr(stream))
+    rc = lib().bimamba_embed_bwd(C.byref(desc), C.byref(_ids(tokens, "tokens", (Bt, L))),
+                                 C.byref(_rows(dout, "dout", _TORCH[desc.io_dtype], (Bt, L, D))),
+                                 _flat(dtable, "dtable", (desc.vocab, D)), *_workspace(workspace), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_embed_bwd")
     return rc
@@ -435,8 +444,8 @@ def bimamba_layer_norm(desc, x, weight, bias, y, mean=None, rstd=None, stream=No
     w, ws = _vector(weight, "weight", Bt, D)
     b, bs = _vector(bias, "bias", Bt, D)
     assert ws is None or bs is None or ws == bs, "weight and bias: not of the same kind and stride"
-    rc = lib().bimamba_layer_norm(C.byref(desc), C.byref(_rows(x, "x", io, Bt, L, D)), w, b, bs or 0 if ws is None else ws,
-                                  C.byref(_rows(y, "y", io, Bt, L, D)), _flat(mean, "mean", Bt, L), _flat(rstd, "rstd", Bt, L),
+    rc = lib().bimamba_layer_norm(C.byref(desc), C.byref(_rows(x, "x", io, (Bt, L, D))), w, b, bs or 0 if ws is None else ws,
+                                  C.byref(_rows(y, "y", io, (Bt, L, D))), _flat(mean, "mean", (Bt, L)), _flat(rstd, "rstd", (Bt, L)),
                                   _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_layer_norm")
@@ -456,10 +465,10 @@ def bimamba_layer_norm_bwd(desc, x, weight, mean, rstd, dy, dx, dweight, dbias, 
     if ws is None:
         ws = D if any(g is not None and g.dim() == 2 for g in (dweight, dbias)) else 0
     shape = (Bt, D) if ws else (D,)
-    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), C.byref(_rows(x, "x", io, Bt, L, D)), w, ws, _flat(mean, "mean", Bt, L),
-                                      _flat(rstd, "rstd", Bt, L), C.byref(_rows(dy, "dy", io, Bt, L, D)),
-                                      C.byref(_rows(dx, "dx", io, Bt, L, D)), _flat(dweight, "dweight", *shape),
-                                      _flat(dbias, "dbias", *shape), *_workspace(workspace), _stream_ptr(stream))
+    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), C.byref(_rows(x, "x", io, (Bt, L, D))), w, ws, _flat(mean, "mean", (Bt, L)),
+                                      _flat(rstd, "rstd", (Bt, L)), C.byref(_rows(dy, "dy", io, (Bt, L, D))),
+                                      C.byref(_rows(dx, "dx", io, (Bt, L, D))), _flat(dweight, "dweight", shape),
+                                      _flat(dbias, "dbias", shape), *_workspace(workspace), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_layer_norm_bwd")
     return rc
@@ -477,10 +486,10 @@ def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, c
     """Enqueue the log probabilities of targets (int64 [batch, L], or None) under softmax(logits).  out: dict of what is wanted:
     logp, lse, entropy float32 [batch, L]; top_logp float32 and top_token int64 [batch, L, top_k]."""
     Bt, L, k = desc.batch, desc.seqlen, desc.top_k
-    s = Scores(_flat(out.get("logp"), "logp", Bt, L), _flat(out.get("lse"), "lse", Bt, L), _flat(out.get("entropy"), "entropy", Bt, L),
-               _flat(out.get("top_logp"), "top_logp", Bt, L, k), _flat(out.get("top_token"), "top_token", Bt, L, k, dtype=torch.int64))
-    rc = lib().bimamba_log_probs(C.byref(desc), C.byref(_rows(logits, "logits", _TORCH[desc.io_dtype], Bt, L, desc.vocab)),
-                                 None if targets is None else C.byref(_ids(targets, "targets", Bt, L)), C.byref(s),
+    s = Scores(_flat(out.get("logp"), "logp", (Bt, L)), _flat(out.get("lse"), "lse", (Bt, L)), _flat(out.get("entropy"), "entropy", (Bt, L)),
+               _flat(out.get("top_logp"), "top_logp", (Bt, L, k)), _flat(out.get("top_token"), "top_token", (Bt, L, k), dtype=torch.int64))
+    rc = lib().bimamba_log_probs(C.byref(desc), C.byref(_rows(logits, "logits", _TORCH[desc.io_dtype], (Bt, L, desc.vocab))),
+                                 None if targets is None else C.byref(_ids(targets, "targets", (Bt, L))), C.byref(s),
                                  *_workspace(workspace), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_log_probs")
@@ -492,10 +501,10 @@ def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, 
     logits itself."""
     Bt, L = desc.batch, desc.seqlen
     io = _TORCH[desc.io_dtype]
-    rc = lib().bimamba_log_probs_bwd(C.byref(desc), C.byref(_rows(logits, "logits", io, Bt, L, desc.vocab)),
-                                     None if targets is None else C.byref(_ids(targets, "targets", Bt, L)), _flat(lse, "lse", Bt, L),
-                                     _flat(entropy, "entropy", Bt, L), _flat(dlogp, "dlogp", Bt, L), _flat(dentropy, "dentropy", Bt, L),
-                                     C.byref(_rows(dlogits, "dlogits", io, Bt, L, desc.vocab)), _stream_ptr(stream))
+    rc = lib().bimamba_log_probs_bwd(C.byref(desc), C.byref(_rows(logits, "logits", io, (Bt, L, desc.vocab))),
+                                     None if targets is None else C.byref(_ids(targets, "targets", (Bt, L))), _flat(lse, "lse", (Bt, L)),
+                                     _flat(entropy, "entropy", (Bt, L)), _flat(dlogp, "dlogp", (Bt, L)), _flat(dentropy, "dentropy", (Bt, L)),
+                                     C.byref(_rows(dlogits, "dlogits", io, (Bt, L, desc.vocab))), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_log_probs_bwd")
     return rc
@@ -526,7 +535,7 @@ def bimamba_clip_grads_workspace_bytes(table):
 def bimamba_clip_grads(table, max_norm, norm, workspace, stream=None, check=True):
     """Enqueue the norm of a GradTable's gradients (norm: float32 [1], or None) and their scaling to at most max_norm."""
     rc = lib().bimamba_clip_grads(table.host, table.n, None if table.dev is None else table.dev.data_ptr(), max_norm,
-                                  _flat(norm, "norm", 1), *_workspace(workspace), _stream_ptr(stream))
+                                  _flat(norm, "norm", (1,)), *_workspace(workspace), _stream_ptr(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_clip_grads")
     return rc

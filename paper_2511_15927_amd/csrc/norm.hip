@@ -385,30 +385,31 @@ __global__ __launch_bounds__(256) void norm_long_cols_kernel(const NormBwdArgs a
     store_piece_of<IoF32>(slot + a.d, at, a.d, db);
 }
 
-// dweight and dbias: the slots of a vector, added up 32 channels to a workgroup, each of its 32 rows of threads a share of the slots.
-constexpr int kSumRows = 32, kSumChannels = 32;
+// dweight and dbias: the slots of a vector, added up 32 channels to a workgroup, each of its rows of threads a share of the slots.
+constexpr int kSumChannels = 32, kFewSums = 8, kManySums = 32;   // (rows of threads, by the number of slots)
 struct NormSumArgs {
     const float* slots;
     float *dweight, *dbias;
     long long count;   // slots of one vector
     int d;
 };
-__global__ __launch_bounds__(kSumRows * kSumChannels) void norm_sum_kernel(const NormSumArgs a)
+template <int kRows>
+__global__ __launch_bounds__(kRows * kSumChannels) void norm_sum_kernel(const NormSumArgs a)
 {
     float* const out = blockIdx.z ? a.dbias : a.dweight;
     if (!out) return;
     const int c = threadIdx.x % kSumChannels, r = threadIdx.x / kSumChannels, col = blockIdx.x * kSumChannels + c;
-    __shared__ float sum[kSumRows][kSumChannels];
+    __shared__ float sum[kRows][kSumChannels];
     float s = 0.0f;
     const float* const from = a.slots + ((long long)blockIdx.y * a.count * 2 + blockIdx.z) * a.d + col;
     if (col < a.d)
 #pragma unroll 8
-        for (long long i = r; i < a.count; i += kSumRows) s += from[i * 2 * a.d];
+        for (long long i = r; i < a.count; i += kRows) s += from[i * 2 * a.d];
     sum[r][c] = s;
     __syncthreads();
     if (r == 0 && col < a.d) {
 #pragma unroll
-        for (int k = 1; k < kSumRows; k++) s += sum[k][c];
+        for (int k = 1; k < kRows; k++) s += sum[k][c];
         out[(long long)blockIdx.y * a.d + col] = s;
     }
 }
@@ -447,7 +448,14 @@ NormPlan plan_norm(const bimamba_norm_desc* d, bool per_batch, bool bwd)
     p.n.rows = per_batch ? d->seqlen : rows;
     p.n.per_batch = per_batch;
     const unsigned together = p.elems && p.waves == 1 ? 4 : 1;   // rows that a workgroup has in hand at once
-    const unsigned want = (bwd ? 4u : 8u) * cu_count();           // workgroups in all
+    // Workgroups in all.  Forward: 16 a CU.  Gradients: as many as the registers hold at once (four a CU, two with 16 elements a lane or
+    // more), but at least eight rows to each while every CU has one, since each leaves a slot as long as two rows (3711 rows of 740
+    // fp32: 464 workgroups 9.2 + 4.7 us, 928 of them 11.0 + 5.7; 16384 rows of 4096: 512 of them 82 + 5, 1024 91 + 7).
+    unsigned want = 16u * cu_count();
+    if (bwd) {
+        const unsigned most = (p.waves == 4 && p.elems != 8 ? 2u : 4u) * cu_count(), least = cu_count();
+        want = rows / 8 < least ? least : rows / 8 > most ? most : rows / 8;
+    }
     const unsigned groups = p.vectors ? (want + p.vectors - 1) / p.vectors : 1;
     const unsigned per_workgroup = (p.n.rows + groups - 1) / groups;
     p.n.per_group = (per_workgroup + together - 1) / together;
@@ -592,7 +600,9 @@ int bimamba_layer_norm_bwd(const bimamba_norm_desc* d, const bimamba_tensor* x, 
     if (sums) {   // (no rows: sums of nothing)
         const long long count = rows ? p.groups : 0;
         const NormSumArgs a{static_cast<const float*>(workspace), dweight, dbias, count, d->d_model};
-        hipLaunchKernelGGL(norm_sum_kernel, dim3((d->d_model + kSumChannels - 1) / kSumChannels, vectors, 2), dim3(kSumRows * kSumChannels), 0, st, a);
+        const dim3 grid((d->d_model + kSumChannels - 1) / kSumChannels, vectors, 2);
+        if (count <= 8 * kFewSums) hipLaunchKernelGGL(norm_sum_kernel<kFewSums>, grid, dim3(kFewSums * kSumChannels), 0, st, a);
+        else hipLaunchKernelGGL(norm_sum_kernel<kManySums>, grid, dim3(kManySums * kSumChannels), 0, st, a);
     }
     return launches.status();
 }
