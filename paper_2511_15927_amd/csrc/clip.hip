@@ -3,28 +3,33 @@
 
 namespace bm {
 
-// All tensors are cut into pieces of 8192 elements, numbered through; a workgroup takes a run of them, finds the tensor of its first
-// one by binary search and steps on from there.  Two launches: the squares' sums, 64 bits each, one a workgroup; then every
-// workgroup adds up all of these in the same order, which gives it the norm, and scales its run.  The second launch walks backwards, so
-// that it starts with what the first has left in the caches.
+// All tensors are cut into pieces of 8192 elements, numbered through, which the workgroups take in turn; a piece's tensor is found by
+// search.  Two launches: the squares' sums, 64 bits each, one a workgroup; then every workgroup adds up all of these in the same
+// order, which gives it the norm, and scales its pieces.  What bounds it are the bytes: two reads, one write.  The second launch
+// goes from the last piece to the first, so that it starts with what the first has left in the caches, and where the
+// gradients are larger than these its stores go past them: 604 M values 663 us (each workgroup a run of pieces of its own, walked
+// backwards: 761; the stores through the caches: 692).
 constexpr int kClipThreads = 256, kClipPiece = 8192;
 struct ClipArgs {
     const bimamba_grad* table;
-    long long pieces, per_group;
+    long long pieces;
     int n;
     float max_norm;
     float* norm;
     double* sums;
 };
 
-// Index of the last tensor that starts at or before a piece (empty ones start where the next does).
+// Index of the last tensor that starts at or before a piece (empty ones start where the next does); 64 tensors are looked at together.
 __device__ __forceinline__ int tensor_of(const ClipArgs& a, long long piece)
 {
-    int lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.table[mid].first <= piece) lo = mid;
-        else hi = mid;
+    const int lane = threadIdx.x % 64;
+    int lo = 0;
+    for (int range = a.n; range > 1;) {
+        const int step = (range + 63) / 64;
+        const bool there = lane * step < range;
+        const int count = __popcll(__ballot(there && a.table[there ? lo + lane * step : lo].first <= piece));   // (the first lanes)
+        range = min(step, range - (count - 1) * step);
+        lo += (count - 1) * step;
     }
     return lo;
 }
@@ -66,7 +71,7 @@ __device__ __forceinline__ double piece_squares(const typename IO::T* from, int 
     });
     return s;
 }
-template <typename IO>
+template <typename IO, bool kPast>
 __device__ __forceinline__ void piece_scaled(const typename IO::T* from, typename IO::T* to, int n, float scale)
 {
     for_piece<IO>(from, n, [&](const auto& p, int at) {
@@ -74,7 +79,7 @@ __device__ __forceinline__ void piece_scaled(const typename IO::T* from, typenam
         float f[N];
 #pragma unroll
         for (int i = 0; i < N; i++) f[i] = scale == 1.0f ? p[i] : p[i] * scale;
-        store_piece_of<IO>(to, at, n, f);
+        store_piece_of<IO, kPast>(to, at, n, f);
     });
 }
 
@@ -92,12 +97,9 @@ __device__ __forceinline__ double workgroup_sum(double v)
 
 __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipArgs a)
 {
-    const long long p0 = blockIdx.x * a.per_group, p1 = min(p0 + a.per_group, a.pieces);
     double s = 0.0;
-    int i = p0 < p1 ? tensor_of(a, p0) : 0;
-    for (long long p = p0; p < p1; p++) {
-        while (i + 1 < a.n && a.table[i + 1].first <= p) i++;
-        const bimamba_grad g = a.table[i];
+    for (long long p = blockIdx.x; p < a.pieces; p += gridDim.x) {
+        const bimamba_grad g = a.table[tensor_of(a, p)];
         const long long at = (p - g.first) * kClipPiece;
         const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
         if (g.dtype == BIMAMBA_BF16) s += piece_squares<IoBF16>(static_cast<const unsigned short*>(g.from) + at, n);
@@ -107,6 +109,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipAr
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
 
+template <bool kPast>
 __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(const ClipArgs a)
 {
     double s = 0.0;
@@ -116,30 +119,26 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(const ClipArgs
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     // (a norm that is not finite in 32 bits compares false or is taken out here)
     const float scale = isfinite((float)norm) && norm > (double)a.max_norm ? (float)((double)a.max_norm / norm) : 1.0f;
-    const unsigned group = gridDim.x - 1 - blockIdx.x;
-    const long long p0 = group * a.per_group, p1 = min(p0 + a.per_group, a.pieces);
-    if (p0 >= p1) return;
-    int i = tensor_of(a, p1 - 1);
-    for (long long p = p1 - 1; p >= p0; p--) {
-        while (i > 0 && a.table[i].first > p) i--;
-        const bimamba_grad g = a.table[i];
+    for (long long k = blockIdx.x; k < a.pieces; k += gridDim.x) {
+        const long long p = a.pieces - 1 - k;
+        const bimamba_grad g = a.table[tensor_of(a, p)];
         if (scale == 1.0f && g.from == g.to) continue;
         const long long at = (p - g.first) * kClipPiece;
         const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
         if (g.dtype == BIMAMBA_BF16)
-            piece_scaled<IoBF16>(static_cast<const unsigned short*>(g.from) + at, static_cast<unsigned short*>(g.to) + at, n, scale);
-        else piece_scaled<IoF32>(static_cast<const float*>(g.from) + at, static_cast<float*>(g.to) + at, n, scale);
+            piece_scaled<IoBF16, kPast>(static_cast<const unsigned short*>(g.from) + at, static_cast<unsigned short*>(g.to) + at, n, scale);
+        else piece_scaled<IoF32, kPast>(static_cast<const float*>(g.from) + at, static_cast<float*>(g.to) + at, n, scale);
     }
 }
 
 namespace {
 
 // Pieces of a table, or an error; `first` is checked against where the tensors before end, or filled.
-int clip_pieces(const bimamba_grad* table, bimamba_grad* fill, int n, long long* pieces)
+int clip_pieces(const bimamba_grad* table, bimamba_grad* fill, int n, long long* pieces, long long* bytes = nullptr)
 {
     if (n < 0) return BIMAMBA_ERR_BAD_SHAPE;
     if (n > 0 && !table) return BIMAMBA_ERR_NULL_POINTER;
-    long long p = 0;
+    long long p = 0, b = 0;
     for (int i = 0; i < n; i++) {
         const bimamba_grad& g = table[i];
         if (g.count < 0 || g.reserved != 0) return BIMAMBA_ERR_BAD_SHAPE;
@@ -153,8 +152,10 @@ int clip_pieces(const bimamba_grad* table, bimamba_grad* fill, int n, long long*
         if (fill) fill[i].first = p;
         else if (g.first != p) return BIMAMBA_ERR_BAD_SHAPE;
         p += (g.count + kClipPiece - 1) / kClipPiece;
+        b += g.count * (long long)elem;
     }
     *pieces = p;
+    if (bytes) *bytes = b;
     return BIMAMBA_OK;
 }
 
@@ -186,20 +187,20 @@ size_t bimamba_clip_grads_workspace_bytes(const bimamba_grad* table, int n)
 int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, float max_norm, float* norm, void* workspace,
                        size_t workspace_bytes, void* hip_stream)
 {
-    long long pieces;
-    int rc = clip_pieces(table, nullptr, n, &pieces);
+    long long pieces, bytes;
+    int rc = clip_pieces(table, nullptr, n, &pieces, &bytes);
     if (rc) return rc;
     if (!(max_norm >= 0.0f)) return BIMAMBA_ERR_BAD_SHAPE;
     if (n > 0 && !table_dev) return BIMAMBA_ERR_NULL_POINTER;
     if (!aligned_to(table_dev, 8) || !aligned_to(norm, 4)) return BIMAMBA_ERR_MISALIGNED;
     const unsigned groups = clip_groups(pieces);
     if ((rc = check_workspace(workspace, workspace_bytes, groups * sizeof(double)))) return rc;
-    ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, (pieces + groups - 1) / groups, n, max_norm, norm,
-               static_cast<double*>(workspace)};
+    const ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, n, max_norm, norm, static_cast<double*>(workspace)};
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
     hipLaunchKernelGGL(clip_squares_kernel, dim3(groups), dim3(kClipThreads), 0, st, a);
-    hipLaunchKernelGGL(clip_scale_kernel, dim3(groups), dim3(kClipThreads), 0, st, a);
+    if (past_caches(2.0 * bytes)) hipLaunchKernelGGL(clip_scale_kernel<true>, dim3(groups), dim3(kClipThreads), 0, st, a);
+    else hipLaunchKernelGGL(clip_scale_kernel<false>, dim3(groups), dim3(kClipThreads), 0, st, a);
     return launches.status();
 }
 

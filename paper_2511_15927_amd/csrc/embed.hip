@@ -15,10 +15,10 @@ struct EmbedArgs {
     int d, vocab, lanes;
     float scale;
 };
-template <typename TT, typename IO, int N>
+constexpr int kRowAhead = 2;   // pieces that a thread has in flight
+template <typename TT, typename IO, int N, bool kPast>
 __device__ __forceinline__ void embed_rows(const EmbedArgs& a)
 {
-    constexpr int kAhead = 2;
     const unsigned per = 256 / a.lanes, lane = threadIdx.x % a.lanes;
     for (unsigned row = blockIdx.x * per + threadIdx.x / a.lanes; row < a.rows; row += gridDim.x * per) {
         const unsigned b = row / a.L, t = row - b * a.L;
@@ -26,28 +26,28 @@ __device__ __forceinline__ void embed_rows(const EmbedArgs& a)
         const bool known = id >= 0 && id < a.vocab;
         const typename TT::T* const from = static_cast<const typename TT::T*>(a.table) + (known ? id : 0) * a.d;
         typename IO::T* const to = static_cast<typename IO::T*>(a.out.p) + row_offset(a.out, b, t);
-        for (int first = lane * N; first < a.d; first += a.lanes * N * kAhead) {
-            Piece<TT, N> p[kAhead];
+        for (int first = lane * N; first < a.d; first += a.lanes * N * kRowAhead) {
+            Piece<TT, N> p[kRowAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) p[k] = load_clamped<TT, N>(from, first + k * a.lanes * N, a.d);
+            for (int k = 0; k < kRowAhead; k++) p[k] = load_clamped<TT, N>(from, first + k * a.lanes * N, a.d);
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) {
+            for (int k = 0; k < kRowAhead; k++) {
                 const int at = first + k * a.lanes * N;
                 settle(p[k], at, a.d, typename TT::T(0));
                 float f[N];
 #pragma unroll
                 for (int i = 0; i < N; i++) f[i] = known ? a.scale * p[k][i] : 0.0f;
-                store_piece_of<IO>(to, at, a.d, f);
+                store_piece_of<IO, kPast>(to, at, a.d, f);
             }
         }
     }
 }
-template <typename TT, typename IO>
+template <typename TT, typename IO, bool kPast>
 __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 {
     constexpr int N = kPieceOf<TT> < kPieceOf<IO> ? kPieceOf<TT> : kPieceOf<IO>;
-    if (a.d >= N) embed_rows<TT, IO, N>(a);
-    else embed_rows<TT, IO, 1>(a);
+    if (a.d >= N) embed_rows<TT, IO, N, kPast>(a);
+    else embed_rows<TT, IO, 1, kPast>(a);
 }
 
 // ---- gradient ----
@@ -70,21 +70,28 @@ struct EmbedClear {
     float* p;
     long long n;
     unsigned first_wg;   // of the launch; the workgroups before it sort
+    int past;            // stores go past the caches
 };
 // (kThreads: of a workgroup.)  Floats that a workgroup clears, 16 bytes a lane side by side (at 32 bytes a lane, two stores that each leave every other 16 bytes to the
 // other, it was 4.1 TB/s).
 constexpr int kClearFloats = 32768;
-template <int kThreads>
-__device__ __forceinline__ void clear_part(const EmbedClear& c)
+template <int kThreads, bool kPast>
+__device__ __forceinline__ void clear_part_as(const EmbedClear& c)
 {
     const long long from = (long long)(blockIdx.x - c.first_wg) * kClearFloats;
     const int n = (int)min((long long)kClearFloats, c.n - from);
     const float zero[4] = {};
     float* const p = c.p + from;
 #pragma unroll 8
-    for (int at = threadIdx.x * 4; at + 4 <= n; at += kThreads * 4) __builtin_memcpy(p + at, zero, sizeof zero);
+    for (int at = threadIdx.x * 4; at + 4 <= n; at += kThreads * 4) store_piece<IoF32, kPast>(p + at, zero);
     const int rest = n & ~3;
     if (rest + (int)threadIdx.x < n) p[rest + threadIdx.x] = 0.0f;
+}
+template <int kThreads>
+__device__ __forceinline__ void clear_part(const EmbedClear& c)
+{
+    if (c.past) clear_part_as<kThreads, true>(c);
+    else clear_part_as<kThreads, false>(c);
 }
 
 struct EmbedSortArgs {
@@ -286,12 +293,16 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
 constexpr int kMaxSlice = 64;
 constexpr int kSumCols = 512;
 constexpr unsigned kShortSpan = 16;   // slices that a short run reaches into at most
+struct EmbedSpan {
+    unsigned slice, last, id;   // the run of `id` starts in `slice` and ends in `last`
+};
 struct EmbedSumArgs {
     const unsigned *id, *place;
     RowView dout;
     float* dtable;
     float* slots;   // [slices][2][d]: of the run that came into the slice, of the one that starts in it and goes on
-    unsigned *n_spans, *span;   // lists of slices in which a run starts that goes on: short runs, and after `slices` entries long ones
+    unsigned* n_spans;
+    EmbedSpan* span;   // lists of runs that span slices: short ones, and after `slices` entries long ones
     unsigned rows, L;
     int d, vocab, slice, col_blocks;
     unsigned slices;
@@ -380,10 +391,18 @@ __device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice,
         }
     }
     flush(cur == after);
-    if (block == 0 && lane == 0 && !came && cur == after && cur < (unsigned)a.vocab) {
-        const unsigned long long far = (unsigned long long)(slice + 1 + kShortSpan) * a.slice;
-        const bool long_run = far < a.rows && a.id[far] == cur;
-        a.span[(long_run ? a.slices : 0) + atomicAdd(a.n_spans + long_run, 1u)] = slice;
+    if (block == 0 && !came && cur == after && cur < (unsigned)a.vocab) {
+        // the last slice that the run goes into: 64 slices are looked at together
+        unsigned last = slice + 1;
+        for (unsigned range = a.slices - last; range > 1;) {
+            const unsigned step = (range + 63) / 64, at = last + lane * step;
+            const bool there = lane * step < range;
+            const unsigned count = __popcll(__ballot(there && a.id[there ? (unsigned long long)at * a.slice : i0] == cur));   // (the first lanes)
+            range = min(step, range - (count - 1) * step);
+            last += (count - 1) * step;
+        }
+        const bool long_run = last > slice + kShortSpan;
+        if (lane == 0) a.span[(long_run ? a.slices : 0) + atomicAdd(a.n_spans + long_run, 1u)] = EmbedSpan{slice, last, cur};
     }
 }
 template <typename IO>
@@ -400,12 +419,12 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
 // share of the slots each.
 constexpr int kJoinWaves = 16, kJoinCols = 256, kShortGroups = 256, kLongGroups = 32;
 struct EmbedJoinArgs {
-    const unsigned* id;
     const float* slots;
     float* dtable;
-    const unsigned *n_spans, *span;
+    const unsigned* n_spans;
+    const EmbedSpan* span;
     unsigned slices, short_groups;
-    int d, slice, col_blocks;
+    int d, col_blocks;
     float scale;
 };
 __device__ __forceinline__ void add_floats(float (&acc)[4], const float* row, int col, int d)
@@ -428,41 +447,29 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
     if (blockIdx.x < a.short_groups) {
         const unsigned n = a.n_spans[0];
         for (unsigned long long w = blockIdx.x * kJoinWaves + wave; w < (unsigned long long)n * a.col_blocks; w += a.short_groups * kJoinWaves) {
-            const unsigned k = w / a.col_blocks, slice = a.span[k];
+            const unsigned k = w / a.col_blocks;
+            const EmbedSpan span = a.span[k];
             const int col = (int)(w - (unsigned long long)k * a.col_blocks) * kJoinCols + lane * 4;
-            const unsigned v = a.id[(unsigned long long)(slice + 1) * a.slice];
-            const unsigned s = slice + 1 + min((unsigned)lane, kShortSpan);
-            const unsigned slots = __popcll(__ballot((unsigned)lane < kShortSpan && s < a.slices && a.id[s < a.slices ? (unsigned long long)s * a.slice : 0] == v));
             float acc[4] = {};
-            add_floats(acc, slot(slice, 1), col, a.d);
+            add_floats(acc, slot(span.slice, 1), col, a.d);
 #pragma unroll 4
-            for (unsigned i = 1; i <= slots; i++) add_floats(acc, slot(slice + i, 0), col, a.d);
+            for (unsigned s = span.slice + 1; s <= span.last; s++) add_floats(acc, slot(s, 0), col, a.d);
 #pragma unroll
             for (int i = 0; i < 4; i++) acc[i] *= a.scale;
-            store_piece_of<IoF32>(a.dtable + (long long)v * a.d, col, a.d, acc);
+            store_piece_of<IoF32>(a.dtable + (long long)span.id * a.d, col, a.d, acc);
         }
         return;
     }
     __shared__ float sum[kJoinWaves][kJoinCols];
     const unsigned n = a.n_spans[1], first = blockIdx.x - a.short_groups;
     for (unsigned long long w = first; w < (unsigned long long)n * a.col_blocks; w += gridDim.x - a.short_groups) {
-        const unsigned k = w / a.col_blocks, slice = a.span[a.slices + k];
+        const unsigned k = w / a.col_blocks;
+        const EmbedSpan span = a.span[a.slices + k];
         const int block = (int)(w - (unsigned long long)k * a.col_blocks), col = block * kJoinCols + lane * 4;
-        const unsigned long long i1 = (unsigned long long)(slice + 1) * a.slice;
-        const unsigned v = a.id[i1];
-        // the last slice that the run came into: 64 slices are looked at together
-        unsigned last = slice + 1;
-        for (unsigned range = a.slices - last; range > 1;) {
-            const unsigned step = (range + 63) / 64, at = last + lane * step;
-            const unsigned long long in = __ballot(lane * step < range && a.id[lane * step < range ? (unsigned long long)at * a.slice : i1] == v);
-            const unsigned count = __popcll(in);   // (a prefix of the lanes, the first among them)
-            range = min(step, range - (count - 1) * step);
-            last += (count - 1) * step;
-        }
         float acc[4] = {};
-        if (wave == 0) add_floats(acc, slot(slice, 1), col, a.d);
+        if (wave == 0) add_floats(acc, slot(span.slice, 1), col, a.d);
 #pragma unroll 8
-        for (unsigned s = slice + 1 + wave; s <= last; s += kJoinWaves) add_floats(acc, slot(s, 0), col, a.d);
+        for (unsigned s = span.slice + 1 + wave; s <= span.last; s += kJoinWaves) add_floats(acc, slot(s, 0), col, a.d);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; i++) sum[wave][lane * 4 + i] = acc[i];
@@ -472,7 +479,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
             float f = 0.0f;
 #pragma unroll
             for (int i = 0; i < kJoinWaves; i++) f += sum[i][threadIdx.x];
-            a.dtable[(long long)v * a.d + c] = a.scale * f;
+            a.dtable[(long long)span.id * a.d + c] = a.scale * f;
         }
     }
 }
@@ -507,8 +514,15 @@ EmbedPlan plan_embed(const bimamba_embed_desc* d)
     p.slices = (p.rows + p.slice - 1) / p.slice;
     p.list = (size_t)p.chunks * p.chunk * 4;   // (whole chunks: a merge reads eight places at a time)
     p.slots = ((size_t)p.slices * 2 * d->d_model * sizeof(float) + 15) / 16 * 16;
-    p.total = 4 * p.list + p.slots + (2 * (size_t)p.slices + 2) * sizeof(unsigned);   // (and the lists of runs that span slices, after their lengths)
+    p.total = 4 * p.list + p.slots + 16 + 2 * (size_t)p.slices * sizeof(EmbedSpan);   // (and the lists of runs that span slices, after their lengths)
     return p;
+}
+
+template <typename TT, typename IO>
+void launch_embed(const EmbedArgs& a, unsigned grid, hipStream_t st)
+{
+    if (past_caches((double)a.rows * a.d * (sizeof(typename TT::T) + sizeof(typename IO::T)))) hipLaunchKernelGGL((embed_kernel<TT, IO, true>), dim3(grid), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((embed_kernel<TT, IO, false>), dim3(grid), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -534,14 +548,14 @@ int bimamba_embed(const bimamba_embed_desc* d, const bimamba_tokens* tokens, con
     EmbedArgs a{tokens->ptr, tokens->stride_batch, tokens->stride_token, table, row_view(out), (unsigned)(d->batch * (long long)d->seqlen),
                 (unsigned)d->seqlen, d->d_model, d->vocab, 256, d->scale};
     const bool tb = d->table_dtype == BIMAMBA_BF16, ib = d->io_dtype == BIMAMBA_BF16;
-    while (a.lanes > 1 && (a.lanes / 2) * (tb && ib ? 8 : 4) >= d->d_model) a.lanes /= 2;
+    while (a.lanes > 1 && (a.lanes / 2) * (tb && ib ? 8 : 4) * kRowAhead >= d->d_model) a.lanes /= 2;
     const unsigned per = 256 / a.lanes, want = (a.rows + per - 1) / per, grid = want < 1u << 20 ? want : 1u << 20;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    if (tb && ib) hipLaunchKernelGGL((embed_kernel<IoBF16, IoBF16>), dim3(grid), dim3(256), 0, st, a);
-    else if (tb) hipLaunchKernelGGL((embed_kernel<IoBF16, IoF32>), dim3(grid), dim3(256), 0, st, a);
-    else if (ib) hipLaunchKernelGGL((embed_kernel<IoF32, IoBF16>), dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((embed_kernel<IoF32, IoF32>), dim3(grid), dim3(256), 0, st, a);
+    if (tb && ib) launch_embed<IoBF16, IoBF16>(a, grid, st);
+    else if (tb) launch_embed<IoBF16, IoF32>(a, grid, st);
+    else if (ib) launch_embed<IoF32, IoBF16>(a, grid, st);
+    else launch_embed<IoF32, IoF32>(a, grid, st);
     return launches.status();
 }
 
@@ -571,20 +585,22 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     unsigned *id = reinterpret_cast<unsigned*>(ws), *place = reinterpret_cast<unsigned*>(ws + p.list);
     unsigned *to_id = reinterpret_cast<unsigned*>(ws + 2 * p.list), *to_place = reinterpret_cast<unsigned*>(ws + 3 * p.list);
     float* const slots = reinterpret_cast<float*>(ws + 4 * p.list);
-    unsigned *const n_spans = reinterpret_cast<unsigned*>(ws + 4 * p.list + p.slots), *const span = n_spans + 2;
+    unsigned* const n_spans = reinterpret_cast<unsigned*>(ws + 4 * p.list + p.slots);
+    EmbedSpan* const span = reinterpret_cast<EmbedSpan*>(ws + 4 * p.list + p.slots + 16);
     // the table is cleared beside the sort and, where there is one, the first merge
     const long long all = (long long)d->vocab * d->d_model;
+    const bool past = past_caches(4.0 * all);   // (8 x 4096 tokens, a table of 412 MB: 143 -> 137 us)
     const long long half = p.rows > p.chunk ? (all / 2 + kClearFloats - 1) / kClearFloats * kClearFloats : all, early = half < all ? half : all;
     const auto wgs = [](long long n) { return (unsigned)((n + kClearFloats - 1) / kClearFloats); };
     const EmbedSortArgs sa{tokens->ptr, tokens->stride_batch, tokens->stride_token, p.rows, (unsigned)d->seqlen, d->vocab, id, place,
-                           n_spans, EmbedClear{dtable, early, p.chunks}};
+                           n_spans, EmbedClear{dtable, early, p.chunks, past}};
     if (p.chunk == 1u << kChunkBits) hipLaunchKernelGGL(embed_sort_kernel<kChunkBits>, dim3(p.chunks + wgs(early)), dim3(p.chunk / kSortKeys), 0, st, sa);
     else hipLaunchKernelGGL(embed_sort_kernel<kLargeChunkBits>, dim3(p.chunks + wgs(early)), dim3(p.chunk / kSortKeys), 0, st, sa);
     if (p.rows == 0) return launches.status();
     long long left = all - early;
     for (unsigned long long run = p.chunk; run < p.rows; run *= kMergeRuns) {
         const unsigned merge_wgs = (p.rows + 255) / 256;
-        const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run, EmbedClear{dtable + early, left, merge_wgs}};
+        const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run, EmbedClear{dtable + early, left, merge_wgs, past}};
         // (few runs: less to look at.  3711 places 15 -> 10 us)
         if (run * kFewRuns >= p.rows) hipLaunchKernelGGL(embed_merge_kernel<kFewRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
         else hipLaunchKernelGGL(embed_merge_kernel<kMergeRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
@@ -600,7 +616,7 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(sum_wgs), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(sum_wgs), dim3(256), 0, st, a);
     if (p.slices > 1) {
-        EmbedJoinArgs ja{id, slots, dtable, n_spans, span, p.slices, kShortGroups, d->d_model, p.slice, 0, d->scale};
+        EmbedJoinArgs ja{slots, dtable, n_spans, span, p.slices, kShortGroups, d->d_model, 0, d->scale};
         ja.col_blocks = (d->d_model + kJoinCols - 1) / kJoinCols;
         const unsigned long long most = ((unsigned long long)p.slices * ja.col_blocks + kJoinWaves - 1) / kJoinWaves;
         if (ja.short_groups > most) ja.short_groups = (unsigned)most;

@@ -28,13 +28,23 @@ __device__ __forceinline__ Piece<IO, N> load_piece(const typename IO::T* p)
     __builtin_memcpy(&r, p, sizeof r);
     return r;
 }
-template <typename IO, int N>
+// kPast: past the caches.  For calls that move more than these hold (past_caches below): what such a call leaves there is of no use, and
+// the lines it has to push out for its outputs cost it time.  Gradient of 16384 rows of 50304 logits 492 -> 407 us, layer norm of
+// 65536 rows of 2048 101 -> 97.
+// (A flag at run time would not do: the compiler joins the two stores and drops the difference.)
+template <typename IO, bool kPast = false, int N>
 __device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[N])
 {
     Piece<IO, N> r;
 #pragma unroll
     for (int i = 0; i < N; i++) r.v[i] = io_value<IO>(f[i]);
-    __builtin_memcpy(p, &r, sizeof r);
+    if constexpr (kPast && sizeof r >= 8) {
+        typedef unsigned Bits __attribute__((ext_vector_type(sizeof r / 4)));
+        typedef Bits Place __attribute__((aligned(2)));   // (of either element type)
+        __builtin_nontemporal_store(__builtin_bit_cast(Bits, r), reinterpret_cast<Place*>(p));
+    } else {
+        __builtin_memcpy(p, &r, sizeof r);
+    }
 }
 // The piece of a row that starts at element `at`, which may reach beyond the row's n >= N elements, in two steps.  The load takes the last N
 // elements where the piece would reach beyond, so there is no branch around it and all loads of a lane are in flight together (with
@@ -66,11 +76,11 @@ __device__ __forceinline__ Piece<IO, N> load_piece_of(const typename IO::T* row,
     settle(r, at, n, fill);
     return r;
 }
-template <typename IO, int N>
+template <typename IO, bool kPast = false, int N>
 __device__ __forceinline__ void store_piece_of(typename IO::T* row, int at, int n, const float (&f)[N])
 {
     if (at + N <= n) {
-        store_piece<IO>(row + at, f);
+        store_piece<IO, kPast>(row + at, f);
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++)
@@ -120,6 +130,8 @@ __device__ __forceinline__ long long row_offset(const RowView& v, int b, int t) 
 // ---- host ----
 
 constexpr long long kMaxRows = (1ll << 31) - 1;
+// Whether a call moves more bytes than the last cache before the memory holds.
+inline bool past_caches(double bytes) { return bytes > (double)(256ll << 20); }
 
 inline RowView row_view(const bimamba_tensor* t) { return RowView{t->ptr, t->stride_batch, t->stride_token}; }
 inline bool known_dtype(int d) { return d == BIMAMBA_F32 || d == BIMAMBA_BF16; }

@@ -320,7 +320,7 @@ struct ScoresBwdArgs {
     unsigned L, parts, all;   // parts of a row, and of all rows
     int vocab;
 };
-template <typename IO, bool kEntropy, int kPiece>
+template <typename IO, bool kEntropy, bool kPast, int kPiece>
 __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned row, unsigned part)
 {
     typedef typename IO::T T;
@@ -341,7 +341,7 @@ __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned
         const float zero[kPiece] = {};
 #pragma unroll
         for (int k = 0; k < kPieces; k++)
-            if (at(k) < a.vocab) store_piece_of<IO>(dx, at(k), a.vocab, zero);
+            if (at(k) < a.vocab) store_piece_of<IO, kPast>(dx, at(k), a.vocab, zero);
         return;
     }
     Piece<IO, kPiece> p[kPieces];
@@ -362,16 +362,16 @@ __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned
         if ((unsigned)(target - at(k)) < (unsigned)kPiece)   // (no target: far outside)
 #pragma unroll
             for (int i = 0; i < kPiece; i++) f[i] += at(k) + i == target ? dl : 0.0f;
-        store_piece_of<IO>(dx, at(k), a.vocab, f);
+        store_piece_of<IO, kPast>(dx, at(k), a.vocab, f);
     }
 }
-template <typename IO, bool kEntropy>
+template <typename IO, bool kEntropy, bool kPast>
 __global__ __launch_bounds__(kGradThreads) void scores_bwd_kernel(const ScoresBwdArgs a)
 {
     for (unsigned w = blockIdx.x; w < a.all; w += gridDim.x) {
         const unsigned row = w / a.parts, part = w - row * a.parts;
-        if (a.vocab >= kPieceOf<IO>) scores_bwd_part<IO, kEntropy, kPieceOf<IO>>(a, row, part);
-        else scores_bwd_part<IO, kEntropy, 1>(a, row, part);
+        if (a.vocab >= kPieceOf<IO>) scores_bwd_part<IO, kEntropy, kPast, kPieceOf<IO>>(a, row, part);
+        else scores_bwd_part<IO, kEntropy, kPast, 1>(a, row, part);
     }
 }
 
@@ -437,6 +437,16 @@ void launch_scores(const ScoresArgs& a, int threads, hipStream_t st)
     else if (a.entropy) launch_scores<IO, true, false>(a, threads, st);
     else if (top) launch_scores<IO, false, true>(a, threads, st);
     else launch_scores<IO, false, false>(a, threads, st);
+}
+
+template <typename IO>
+void launch_scores_bwd(const ScoresBwdArgs& a, unsigned grid, bool past, hipStream_t st)
+{
+    const dim3 wg(kGradThreads);
+    if (a.dentropy && past) hipLaunchKernelGGL((scores_bwd_kernel<IO, true, true>), dim3(grid), wg, 0, st, a);
+    else if (a.dentropy) hipLaunchKernelGGL((scores_bwd_kernel<IO, true, false>), dim3(grid), wg, 0, st, a);
+    else if (past) hipLaunchKernelGGL((scores_bwd_kernel<IO, false, true>), dim3(grid), wg, 0, st, a);
+    else hipLaunchKernelGGL((scores_bwd_kernel<IO, false, false>), dim3(grid), wg, 0, st, a);
 }
 
 }  // namespace
@@ -524,11 +534,9 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* lo
     const unsigned grid = all < 1u << 22 ? (unsigned)all : 1u << 22;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    const bool bf16 = d->io_dtype == BIMAMBA_BF16;
-    if (bf16 && dentropy) hipLaunchKernelGGL((scores_bwd_kernel<IoBF16, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
-    else if (bf16) hipLaunchKernelGGL((scores_bwd_kernel<IoBF16, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
-    else if (dentropy) hipLaunchKernelGGL((scores_bwd_kernel<IoF32, true>), dim3(grid), dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL((scores_bwd_kernel<IoF32, false>), dim3(grid), dim3(kGradThreads), 0, st, a);
+    const bool past = past_caches(2.0 * rows * d->vocab * elem);
+    if (d->io_dtype == BIMAMBA_BF16) launch_scores_bwd<IoBF16>(a, grid, past, st);
+    else launch_scores_bwd<IoF32>(a, grid, past, st);
     return launches.status();
 }
 
