@@ -141,14 +141,14 @@ def lib():
         L.bimamba_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
         P, V, Z, I = C.POINTER, C.c_void_p, C.c_size_t, C.c_int
         for name, res, args in (
-                ("bimamba_embed", I, [P(EmbedDesc), P(Tokens), V, P(Tensor), V]),
-                ("bimamba_embed_bwd", I, [P(EmbedDesc), P(Tokens), P(Tensor), V, V, Z, V]),
+                ("bimamba_embed", I, [P(EmbedDesc), V, V, V, V]),
+                ("bimamba_embed_bwd", I, [P(EmbedDesc), V, V, V, V, Z, V]),
                 ("bimamba_embed_bwd_workspace_bytes", Z, [P(EmbedDesc)]),
-                ("bimamba_layer_norm", I, [P(NormDesc), P(Tensor), V, V, C.c_int64, P(Tensor), V, V, V]),
-                ("bimamba_layer_norm_bwd", I, [P(NormDesc), P(Tensor), V, C.c_int64, V, V, P(Tensor), P(Tensor), V, V, V, Z, V]),
+                ("bimamba_layer_norm", I, [P(NormDesc), V, V, V, C.c_int64, V, V, V, V]),
+                ("bimamba_layer_norm_bwd", I, [P(NormDesc), V, V, C.c_int64, V, V, V, V, V, V, V, Z, V]),
                 ("bimamba_layer_norm_bwd_workspace_bytes", Z, [P(NormDesc), I]),
-                ("bimamba_log_probs", I, [P(LogitsDesc), P(Tensor), P(Tokens), P(Scores), V, Z, V]),
-                ("bimamba_log_probs_bwd", I, [P(LogitsDesc), P(Tensor), P(Tokens), V, V, V, V, P(Tensor), V]),
+                ("bimamba_log_probs", I, [P(LogitsDesc), V, V, P(Scores), V, Z, V]),
+                ("bimamba_log_probs_bwd", I, [P(LogitsDesc), V, V, V, V, V, V, V, V]),
                 ("bimamba_log_probs_workspace_bytes", Z, [P(LogitsDesc)]),
                 ("bimamba_clip_layout", I, [P(Grad), I]),
                 ("bimamba_clip_grads", I, [P(Grad), I, V, C.c_float, V, V, Z, V]),
@@ -349,25 +349,35 @@ _TORCH = (torch.float32, torch.bfloat16)
 _NAMES = {"f32": F32, "bf16": BF16}
 
 
+def _stream(stream):
+    # (a call's tensors are on the GPU, so torch has been initialised)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
 def _wrong(t, what, dtype, shape, more=""):
     raise AssertionError("%s: %s %s with strides %s on %s, wanted %s %s on the GPU%s" % (
         what, t.dtype, tuple(t.shape), t.stride(), t.device, dtype, tuple(shape), more))
 
 
+_VIEW_WORDS = struct.Struct("=Qqq")   # a Tensor, a Tokens: their bytes go over as they are (a struct and a reference to it cost 0.1 us more)
+assert _VIEW_WORDS.size == C.sizeof(Tensor) == C.sizeof(Tokens)
+
+
 def _rows(t, what, dtype, shape):
-    """[batch, L, width] activations -> Tensor.  (The host's share of a small call counts: each check reads what it needs once.)"""
+    """[batch, L, width] activations -> the bytes of a Tensor.  (The host's share of a small call counts: each check reads what it needs
+    once.)"""
     if t.dtype is not dtype or not t.is_cuda or t.shape != shape:
         _wrong(t, what, dtype, shape)
     sb, st, s1 = t.stride()
     if s1 != 1 and shape[2] != 1 and t.numel() != 0:
         _wrong(t, what, dtype, shape, ", the channels contiguous")
-    return Tensor(t.data_ptr(), sb, st)
+    return _VIEW_WORDS.pack(t.data_ptr(), sb, st)
 
 
 def _ids(t, what, shape):
     if t.dtype is not torch.int64 or not t.is_cuda or t.shape != shape:
         _wrong(t, what, torch.int64, shape)
-    return Tokens(t.data_ptr(), *t.stride())
+    return _VIEW_WORDS.pack(t.data_ptr(), *t.stride())
 
 
 def _flat(t, what, shape, dtype=torch.float32):
@@ -409,9 +419,9 @@ def bimamba_embed(desc, tokens, table, out, stream=None, check=True):
     """Enqueue out[b, t] = scale * table[tokens[b, t]].  tokens: int64 [batch, L]; table [vocab, d_model] contiguous; out
     [batch, L, d_model]."""
     Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed(C.byref(desc), C.byref(_ids(tokens, "tokens", (Bt, L))),
+    rc = lib().bimamba_embed(C.byref(desc), _ids(tokens, "tokens", (Bt, L)),
                              _flat(table, "table", (desc.vocab, D), dtype=_TORCH[desc.table_dtype]),
-                             C.byref(_rows(out, "out", _TORCH[desc.io_dtype], (Bt, L, D))), _stream_ptr(stream))
+                             _rows(out, "out", _TORCH[desc.io_dtype], (Bt, L, D)), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_embed")
     return rc
@@ -424,9 +434,9 @@ def bimamba_embed_bwd_workspace_bytes(desc):
 def bimamba_embed_bwd(desc, tokens, dout, dtable, workspace, stream=None, check=True):
     """Enqueue the gradient of the table: dtable float32 [vocab, d_model] contiguous, overwritten."""
     Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed_bwd(C.byref(desc), C.byref(_ids(tokens, "tokens", (Bt, L))),
-                                 C.byref(_rows(dout, "dout", _TORCH[desc.io_dtype], (Bt, L, D))),
-                                 _flat(dtable, "dtable", (desc.vocab, D)), *_workspace(workspace), _stream_ptr(stream))
+    rc = lib().bimamba_embed_bwd(C.byref(desc), _ids(tokens, "tokens", (Bt, L)),
+                                 _rows(dout, "dout", _TORCH[desc.io_dtype], (Bt, L, D)),
+                                 _flat(dtable, "dtable", (desc.vocab, D)), *_workspace(workspace), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_embed_bwd")
     return rc
@@ -444,9 +454,9 @@ def bimamba_layer_norm(desc, x, weight, bias, y, mean=None, rstd=None, stream=No
     w, ws = _vector(weight, "weight", Bt, D)
     b, bs = _vector(bias, "bias", Bt, D)
     assert ws is None or bs is None or ws == bs, "weight and bias: not of the same kind and stride"
-    rc = lib().bimamba_layer_norm(C.byref(desc), C.byref(_rows(x, "x", io, (Bt, L, D))), w, b, bs or 0 if ws is None else ws,
-                                  C.byref(_rows(y, "y", io, (Bt, L, D))), _flat(mean, "mean", (Bt, L)), _flat(rstd, "rstd", (Bt, L)),
-                                  _stream_ptr(stream))
+    rc = lib().bimamba_layer_norm(C.byref(desc), _rows(x, "x", io, (Bt, L, D)), w, b, bs or 0 if ws is None else ws,
+                                  _rows(y, "y", io, (Bt, L, D)), _flat(mean, "mean", (Bt, L)), _flat(rstd, "rstd", (Bt, L)),
+                                  _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_layer_norm")
     return rc
@@ -465,10 +475,10 @@ def bimamba_layer_norm_bwd(desc, x, weight, mean, rstd, dy, dx, dweight, dbias, 
     if ws is None:
         ws = D if any(g is not None and g.dim() == 2 for g in (dweight, dbias)) else 0
     shape = (Bt, D) if ws else (D,)
-    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), C.byref(_rows(x, "x", io, (Bt, L, D))), w, ws, _flat(mean, "mean", (Bt, L)),
-                                      _flat(rstd, "rstd", (Bt, L)), C.byref(_rows(dy, "dy", io, (Bt, L, D))),
-                                      C.byref(_rows(dx, "dx", io, (Bt, L, D))), _flat(dweight, "dweight", shape),
-                                      _flat(dbias, "dbias", shape), *_workspace(workspace), _stream_ptr(stream))
+    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), _rows(x, "x", io, (Bt, L, D)), w, ws, _flat(mean, "mean", (Bt, L)),
+                                      _flat(rstd, "rstd", (Bt, L)), _rows(dy, "dy", io, (Bt, L, D)),
+                                      _rows(dx, "dx", io, (Bt, L, D)), _flat(dweight, "dweight", shape),
+                                      _flat(dbias, "dbias", shape), *_workspace(workspace), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_layer_norm_bwd")
     return rc
@@ -488,9 +498,9 @@ def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, c
     Bt, L, k = desc.batch, desc.seqlen, desc.top_k
     s = Scores(_flat(out.get("logp"), "logp", (Bt, L)), _flat(out.get("lse"), "lse", (Bt, L)), _flat(out.get("entropy"), "entropy", (Bt, L)),
                _flat(out.get("top_logp"), "top_logp", (Bt, L, k)), _flat(out.get("top_token"), "top_token", (Bt, L, k), dtype=torch.int64))
-    rc = lib().bimamba_log_probs(C.byref(desc), C.byref(_rows(logits, "logits", _TORCH[desc.io_dtype], (Bt, L, desc.vocab))),
-                                 None if targets is None else C.byref(_ids(targets, "targets", (Bt, L))), C.byref(s),
-                                 *_workspace(workspace), _stream_ptr(stream))
+    rc = lib().bimamba_log_probs(C.byref(desc), _rows(logits, "logits", _TORCH[desc.io_dtype], (Bt, L, desc.vocab)),
+                                 None if targets is None else _ids(targets, "targets", (Bt, L)), C.byref(s),
+                                 *_workspace(workspace), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_log_probs")
     return rc
@@ -501,10 +511,10 @@ def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, 
     logits itself."""
     Bt, L = desc.batch, desc.seqlen
     io = _TORCH[desc.io_dtype]
-    rc = lib().bimamba_log_probs_bwd(C.byref(desc), C.byref(_rows(logits, "logits", io, (Bt, L, desc.vocab))),
-                                     None if targets is None else C.byref(_ids(targets, "targets", (Bt, L))), _flat(lse, "lse", (Bt, L)),
+    rc = lib().bimamba_log_probs_bwd(C.byref(desc), _rows(logits, "logits", io, (Bt, L, desc.vocab)),
+                                     None if targets is None else _ids(targets, "targets", (Bt, L)), _flat(lse, "lse", (Bt, L)),
                                      _flat(entropy, "entropy", (Bt, L)), _flat(dlogp, "dlogp", (Bt, L)), _flat(dentropy, "dentropy", (Bt, L)),
-                                     C.byref(_rows(dlogits, "dlogits", io, (Bt, L, desc.vocab))), _stream_ptr(stream))
+                                     _rows(dlogits, "dlogits", io, (Bt, L, desc.vocab)), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_log_probs_bwd")
     return rc
@@ -535,7 +545,7 @@ def bimamba_clip_grads_workspace_bytes(table):
 def bimamba_clip_grads(table, max_norm, norm, workspace, stream=None, check=True):
     """Enqueue the norm of a GradTable's gradients (norm: float32 [1], or None) and their scaling to at most max_norm."""
     rc = lib().bimamba_clip_grads(table.host, table.n, None if table.dev is None else table.dev.data_ptr(), max_norm,
-                                  _flat(norm, "norm", (1,)), *_workspace(workspace), _stream_ptr(stream))
+                                  _flat(norm, "norm", (1,)), *_workspace(workspace), _stream(stream))
     if check and rc != 0:
         raise BimambaError(rc, "bimamba_clip_grads")
     return rc

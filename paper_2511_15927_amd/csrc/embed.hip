@@ -54,8 +54,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 //
 // dtable[v] = scale * sum of dout over the places with id v.  The places are sorted by (id, place); a sum then is over neighbours, in a
 // fixed order, without atomics, and however many places share an id (in a noised sequence half of them are the mask token) they are
-// summed by as many waves as they have slices.  Sorting: chunks of up to 4096 in a workgroup's registers, then merges of sixteen runs at a time, each
-// place counting by binary search what precedes it in the other fifteen.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
+// summed by as many waves as they have slices.  Sorting: chunks of up to 4096 in a workgroup's registers, then merges of eight runs at a time, each
+// place counting by binary search what precedes it in the other seven.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
 // meanwhile the other workgroups of its launches clear the table, half of it each, so that only rows of ids that occur are left to
 // write.  (Looking up which rows are absent instead, after the sort, writes those rows once and not twice, but hides nothing.)
 
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 constexpr int kChunkBits = 11, kLargeChunkBits = 12, kSortKeys = 4;
 constexpr int kMaxVocab = (1 << 21) - 1;
 constexpr int kMaxWidth = 1 << 20;
-constexpr int kMergeRuns = 16, kFewRuns = 4;
+constexpr int kMergeRuns = 8, kFewRuns = 4;
 constexpr unsigned kMergeSamples = 256, kMergeWindow = 8;   // (a chunk: samples x window, or twice that)
 
 struct EmbedClear {
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
         for (int q = 0; q < kRuns; q++)
             if (below[q] + step <= len[q] && precedes(q, other[q])) below[q] += step;
     }
-    constexpr int kTogether = kRuns < 8 ? kRuns : 8;
+    constexpr int kTogether = kRuns;
 #pragma unroll
     for (int q0 = 0; q0 < kRuns; q0 += kTogether) {
         unsigned window[kTogether][kMergeWindow];
@@ -415,73 +415,85 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
     else sum_slice<IO, 1>(a, slice, block, lane);
 }
 
-// The rows of runs that span slices.  256 channels of a short run: a wave adds up its slots.  Of a long run: a workgroup, the waves a
-// share of the slots each.
+// The rows of runs that span slices.  256 channels of a short run: a wave adds up its slots.  Of a long run: a workgroup, each of its
+// groups of lanes a share of the slots.
 constexpr int kJoinWaves = 16, kJoinCols = 256, kShortGroups = 256, kLongGroups = 32;
 struct EmbedJoinArgs {
     const float* slots;
     float* dtable;
     const unsigned* n_spans;
     const EmbedSpan* span;
-    unsigned slices, short_groups;
+    unsigned slices, short_groups, lanes;   // lanes: that a long run's slot takes, fewer where rows are short
     int d, col_blocks;
     float scale;
 };
-__device__ __forceinline__ void add_floats(float (&acc)[4], const float* row, int col, int d)
+// kAt a time, N neighbours of each slot from `col`: slots first, first + step, ... up to last.
+template <int N, int kAt>
+__device__ __forceinline__ void add_slots(float (&acc)[N], const EmbedJoinArgs& a, int col, unsigned first, unsigned last, unsigned step)
 {
-    float f[4] = {};
-    if (col + 4 <= d) {
-        __builtin_memcpy(f, row + col, sizeof f);
-    } else {
+    for (unsigned s = first; s <= last; s += kAt * step) {
+        Piece<IoF32, N> p[kAt];
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (col + i < d) f[i] = row[col + i];
+        for (int j = 0; j < kAt; j++) p[j] = load_clamped<IoF32, N>(a.slots + (long long)min(s + j * step, last) * 2 * a.d, col, a.d);
+#pragma unroll
+        for (int j = 0; j < kAt; j++) {
+            settle(p[j], col, a.d, 0.0f);
+            if (s + j * step <= last)
+#pragma unroll
+                for (int i = 0; i < N; i++) acc[i] += p[j][i];
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; i++) acc[i] += f[i];
 }
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedJoinArgs a)
+template <int N>
+__device__ __forceinline__ void join_runs(const EmbedJoinArgs& a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    const auto slot = [&](unsigned s, int which) { return a.slots + ((long long)s * 2 + which) * a.d; };
+    const auto start = [&](float (&acc)[N], const EmbedSpan& span, int col) {   // what the run's first slice left
+        const Piece<IoF32, N> p = load_piece_of<IoF32, N>(a.slots + ((long long)span.slice * 2 + 1) * a.d, col, a.d, 0.0f);
+#pragma unroll
+        for (int i = 0; i < N; i++) acc[i] = p[i];
+    };
     if (blockIdx.x < a.short_groups) {
         const unsigned n = a.n_spans[0];
         for (unsigned long long w = blockIdx.x * kJoinWaves + wave; w < (unsigned long long)n * a.col_blocks; w += a.short_groups * kJoinWaves) {
             const unsigned k = w / a.col_blocks;
             const EmbedSpan span = a.span[k];
-            const int col = (int)(w - (unsigned long long)k * a.col_blocks) * kJoinCols + lane * 4;
-            float acc[4] = {};
-            add_floats(acc, slot(span.slice, 1), col, a.d);
-#pragma unroll 4
-            for (unsigned s = span.slice + 1; s <= span.last; s++) add_floats(acc, slot(s, 0), col, a.d);
+            const int col = (int)(w - (unsigned long long)k * a.col_blocks) * kJoinCols + lane * N;
+            float acc[N];
+            start(acc, span, col);
+            add_slots<N, 4>(acc, a, col, span.slice + 1, span.last, 1);
 #pragma unroll
-            for (int i = 0; i < 4; i++) acc[i] *= a.scale;
+            for (int i = 0; i < N; i++) acc[i] *= a.scale;
             store_piece_of<IoF32>(a.dtable + (long long)span.id * a.d, col, a.d, acc);
         }
         return;
     }
-    __shared__ float sum[kJoinWaves][kJoinCols];
+    __shared__ float sum[kJoinWaves * 64 * N];
     const unsigned n = a.n_spans[1], first = blockIdx.x - a.short_groups;
     for (unsigned long long w = first; w < (unsigned long long)n * a.col_blocks; w += gridDim.x - a.short_groups) {
         const unsigned k = w / a.col_blocks;
         const EmbedSpan span = a.span[a.slices + k];
-        const int block = (int)(w - (unsigned long long)k * a.col_blocks), col = block * kJoinCols + lane * 4;
-        float acc[4] = {};
-        if (wave == 0) add_floats(acc, slot(span.slice, 1), col, a.d);
-#pragma unroll 8
-        for (unsigned s = span.slice + 1 + wave; s <= span.last; s += kJoinWaves) add_floats(acc, slot(s, 0), col, a.d);
+        const int block = (int)(w - (unsigned long long)k * a.col_blocks), col = block * kJoinCols + (int)(threadIdx.x % a.lanes) * N;
+        float acc[N] = {};
+        if (threadIdx.x < a.lanes) start(acc, span, col);
+        add_slots<N, 8>(acc, a, col, span.slice + 1 + threadIdx.x / a.lanes, span.last, 64 * kJoinWaves / a.lanes);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; i++) sum[wave][lane * 4 + i] = acc[i];
+        for (int i = 0; i < N; i++) sum[threadIdx.x * N + i] = acc[i];
         __syncthreads();
-        const int c = block * kJoinCols + threadIdx.x;
-        if (threadIdx.x < kJoinCols && c < a.d) {
+        const int width = a.lanes * N, c = block * kJoinCols + threadIdx.x;
+        if ((int)threadIdx.x < width && c < a.d) {
             float f = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kJoinWaves; i++) f += sum[i][threadIdx.x];
+#pragma unroll 16
+            for (int i = threadIdx.x; i < kJoinWaves * 64 * N; i += width) f += sum[i];
             a.dtable[(long long)span.id * a.d + c] = a.scale * f;
         }
     }
+}
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedJoinArgs a)
+{
+    if (a.d >= 4) join_runs<4>(a);
+    else join_runs<1>(a);
 }
 
 namespace {
@@ -616,7 +628,8 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(sum_wgs), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(sum_wgs), dim3(256), 0, st, a);
     if (p.slices > 1) {
-        EmbedJoinArgs ja{slots, dtable, n_spans, span, p.slices, kShortGroups, d->d_model, 0, d->scale};
+        EmbedJoinArgs ja{slots, dtable, n_spans, span, p.slices, kShortGroups, 64, d->d_model, 0, d->scale};
+        while (ja.lanes > 4 && ja.lanes / 2 * 4 >= (unsigned)d->d_model) ja.lanes /= 2;
         ja.col_blocks = (d->d_model + kJoinCols - 1) / kJoinCols;
         const unsigned long long most = ((unsigned long long)p.slices * ja.col_blocks + kJoinWaves - 1) / kJoinWaves;
         if (ja.short_groups > most) ja.short_groups = (unsigned)most;

@@ -96,7 +96,7 @@ def embed_bwd(bd, tok, dout, vocab, scale, io):
 @pytest.mark.parametrize("kind", ["spread", "half", "one", "outside"])
 @pytest.mark.parametrize("batch,seqlen,d,vocab", [
     (1, 1, 1, 1), (1, 1, 513, 3), (2, 3, 7, 5), (1, 63, 8, 4), (1, 64, 8, 4), (1, 65, 520, 40), (4, 512, 64, 300), (1, 2049, 72, 1000),
-    (3, 1237, 740, 3201), (2, 20000, 32, 50000), (1, 70000, 8, 70)])
+    (3, 1237, 740, 3201), (2, 20000, 32, 50000), (1, 70000, 8, 70), (1, 300000, 8, 5000), (1, 5000, 3, 1 << 20)])
 def test_embed_gradient(bd, batch, seqlen, d, vocab, kind, io):
     g = gen(seqlen + d)
     tok = torch.randint(0, vocab, (batch, seqlen), generator=g)
