@@ -6,13 +6,15 @@ namespace bm {
 // All tensors are cut into pieces of 8192 elements, numbered through, which the workgroups take in turn; a piece's tensor is found by
 // search.  Two launches: the squares' sums, 64 bits each, one a workgroup; then every workgroup adds up all of these in the same
 // order, which gives it the norm, and scales its pieces.  What bounds it are the bytes: two reads, one write.  The second launch
-// goes from the last piece to the first, so that it starts with what the first has left in the caches, and where the
-// gradients are larger than these its stores go past them: 604 M values 663 us (each workgroup a run of pieces of its own, walked
-// backwards: 761; the stores through the caches: 692).
+// goes from the last piece to the first, so that it starts with what the first has left in the caches; where the gradients are larger
+// than these, the first reads all but the last 192 MB past them, and the second goes past them altogether.  604 M values, 1.2 GB: 615 us
+// (each workgroup a run of pieces of its own, walked backwards, everything through the caches: 761; the pieces in turn 692; stores past
+// the caches 640; nothing kept for the second launch 629).
 constexpr int kClipThreads = 256, kClipPiece = 8192;
+constexpr long long kKept = 192ll << 20;   // bytes that the first launch leaves in the caches for the second
 struct ClipArgs {
     const bimamba_grad* table;
-    long long pieces;
+    long long pieces, past;   // past: so many pieces are read past the caches at first
     int n;
     float max_norm;
     float* norm;
@@ -37,13 +39,13 @@ __device__ __forceinline__ int tensor_of(const ClipArgs& a, long long piece)
 // What a lane does with its elements of a piece, four loads in flight at a time: use(elements, where they start).  A piece of fewer elements
 // than one load takes goes an element a lane.
 constexpr int kClipAhead = 4;
-template <typename IO, int N, typename Use>
+template <typename IO, int N, bool kPast, typename Use>
 __device__ __forceinline__ void for_piece(const typename IO::T* from, int n, Use use)
 {
     for (int first = threadIdx.x * N; first < n; first += kClipThreads * N * kClipAhead) {
         Piece<IO, N> p[kClipAhead];
 #pragma unroll
-        for (int k = 0; k < kClipAhead; k++) p[k] = load_clamped<IO, N>(from, first + k * kClipThreads * N, n);
+        for (int k = 0; k < kClipAhead; k++) p[k] = load_clamped<IO, N, kPast>(from, first + k * kClipThreads * N, n);
 #pragma unroll
         for (int k = 0; k < kClipAhead; k++) {
             const int at = first + k * kClipThreads * N;
@@ -52,17 +54,17 @@ __device__ __forceinline__ void for_piece(const typename IO::T* from, int n, Use
         }
     }
 }
-template <typename IO, typename Use>
+template <typename IO, bool kPast, typename Use>
 __device__ __forceinline__ void for_piece(const typename IO::T* from, int n, Use use)
 {
-    if (n >= kPieceOf<IO>) for_piece<IO, kPieceOf<IO>>(from, n, use);
-    else for_piece<IO, 1>(from, n, use);
+    if (n >= kPieceOf<IO>) for_piece<IO, kPieceOf<IO>, kPast>(from, n, use);
+    else for_piece<IO, 1, kPast>(from, n, use);
 }
-template <typename IO>
+template <typename IO, bool kPast>
 __device__ __forceinline__ double piece_squares(const typename IO::T* from, int n)
 {
     double s = 0.0;
-    for_piece<IO>(from, n, [&](const auto& p, int) {
+    for_piece<IO, kPast>(from, n, [&](const auto& p, int) {
 #pragma unroll
         for (auto e : p.v) {
             const double v = IO::cvt(e);
@@ -74,7 +76,7 @@ __device__ __forceinline__ double piece_squares(const typename IO::T* from, int 
 template <typename IO, bool kPast>
 __device__ __forceinline__ void piece_scaled(const typename IO::T* from, typename IO::T* to, int n, float scale)
 {
-    for_piece<IO>(from, n, [&](const auto& p, int at) {
+    for_piece<IO, kPast>(from, n, [&](const auto& p, int at) {
         constexpr int N = sizeof p.v / sizeof p.v[0];
         float f[N];
 #pragma unroll
@@ -102,8 +104,14 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipAr
         const bimamba_grad g = a.table[tensor_of(a, p)];
         const long long at = (p - g.first) * kClipPiece;
         const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
-        if (g.dtype == BIMAMBA_BF16) s += piece_squares<IoBF16>(static_cast<const unsigned short*>(g.from) + at, n);
-        else s += piece_squares<IoF32>(static_cast<const float*>(g.from) + at, n);
+        const bool past = p < a.past;
+        if (g.dtype == BIMAMBA_BF16) {
+            const unsigned short* const from = static_cast<const unsigned short*>(g.from) + at;
+            s += past ? piece_squares<IoBF16, true>(from, n) : piece_squares<IoBF16, false>(from, n);
+        } else {
+            const float* const from = static_cast<const float*>(g.from) + at;
+            s += past ? piece_squares<IoF32, true>(from, n) : piece_squares<IoF32, false>(from, n);
+        }
     }
     s = workgroup_sum(s);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
@@ -195,7 +203,8 @@ int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, 
     if (!aligned_to(table_dev, 8) || !aligned_to(norm, 4)) return BIMAMBA_ERR_MISALIGNED;
     const unsigned groups = clip_groups(pieces);
     if ((rc = check_workspace(workspace, workspace_bytes, groups * sizeof(double)))) return rc;
-    const ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, n, max_norm, norm, static_cast<double*>(workspace)};
+    const long long past = past_caches(2.0 * bytes) && bytes > kKept ? (long long)((double)pieces * (bytes - kKept) / bytes) : 0;
+    const ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, past, n, max_norm, norm, static_cast<double*>(workspace)};
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
     hipLaunchKernelGGL(clip_squares_kernel, dim3(groups), dim3(kClipThreads), 0, st, a);

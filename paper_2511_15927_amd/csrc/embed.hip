@@ -311,7 +311,7 @@ struct EmbedSumArgs {
 // A lane's eight of the wave's 512 channels from `col`: two groups of four.  N 8: neighbours, one load of bf16; what is stored goes through
 // pairs of lanes, so that each pair writes 32 bytes side by side.  N 4: one group in each half, two loads of fp32.  N 1: rows of
 // fewer channels than that, one a lane.
-template <typename IO, int N>
+template <typename IO, int N, bool kPast>
 __device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice, int block, int lane)
 {
     constexpr int kLoads = N == 8 ? 1 : N == 4 ? 2 : 1;   // pieces a row and lane
@@ -366,7 +366,7 @@ __device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice,
             const unsigned lo = __builtin_amdgcn_readlane((unsigned)my_row, at), hi = __builtin_amdgcn_readlane((unsigned)(my_row >> 32), at);
             const typename IO::T* const row = dout + (long long)((unsigned long long)hi << 32 | lo);
 #pragma unroll
-            for (int h = 0; h < kLoads; h++) p[j][h] = load_clamped<IO, N>(row, col + h * 64 * N, a.d);
+            for (int h = 0; h < kLoads; h++) p[j][h] = load_clamped<IO, N, kPast>(row, col + h * 64 * N, a.d);
         }
 #pragma unroll
         for (int j = 0; j < kAhead; j++) {
@@ -405,14 +405,14 @@ __device__ __forceinline__ void sum_slice(const EmbedSumArgs& a, unsigned slice,
         if (lane == 0) a.span[(long_run ? a.slices : 0) + atomicAdd(a.n_spans + long_run, 1u)] = EmbedSpan{slice, last, cur};
     }
 }
-template <typename IO>
+template <typename IO, bool kPast>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
 {
     const unsigned w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), slice = w / a.col_blocks;
     if (slice >= a.slices) return;
     const int block = w - slice * a.col_blocks, lane = threadIdx.x % 64;
-    if (a.d >= kPieceOf<IO>) sum_slice<IO, kPieceOf<IO>>(a, slice, block, lane);
-    else sum_slice<IO, 1>(a, slice, block, lane);
+    if (a.d >= kPieceOf<IO>) sum_slice<IO, kPieceOf<IO>, kPast>(a, slice, block, lane);
+    else sum_slice<IO, 1, kPast>(a, slice, block, lane);
 }
 
 // The rows of runs that span slices.  256 channels of a short run: a wave adds up its slots.  Of a long run: a workgroup, each of its
@@ -601,7 +601,7 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     EmbedSpan* const span = reinterpret_cast<EmbedSpan*>(ws + 4 * p.list + p.slots + 16);
     // the table is cleared beside the sort and, where there is one, the first merge
     const long long all = (long long)d->vocab * d->d_model;
-    const bool past = past_caches(4.0 * all);   // (8 x 4096 tokens, a table of 412 MB: 143 -> 137 us)
+    const bool past = past_caches(4.0 * all + (double)p.rows * d->d_model * dtype_bytes(d->io_dtype));   // (8 x 4096 tokens, 412 MB: 143 -> 128 us)
     const long long half = p.rows > p.chunk ? (all / 2 + kClearFloats - 1) / kClearFloats * kClearFloats : all, early = half < all ? half : all;
     const auto wgs = [](long long n) { return (unsigned)((n + kClearFloats - 1) / kClearFloats); };
     const EmbedSortArgs sa{tokens->ptr, tokens->stride_batch, tokens->stride_token, p.rows, (unsigned)d->seqlen, d->vocab, id, place,
@@ -625,8 +625,11 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     const EmbedSumArgs a{id, place, row_view(dout), dtable, slots, n_spans, span, p.rows, (unsigned)d->seqlen, d->d_model, d->vocab, p.slice, p.col_blocks,
                          p.slices, d->scale};
     const unsigned sum_wgs = (unsigned)(((unsigned long long)p.slices * p.col_blocks + 3) / 4);
-    if (d->io_dtype == BIMAMBA_BF16) hipLaunchKernelGGL(embed_sum_kernel<IoBF16>, dim3(sum_wgs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(embed_sum_kernel<IoF32>, dim3(sum_wgs), dim3(256), 0, st, a);
+    const bool bf16 = d->io_dtype == BIMAMBA_BF16;
+    if (bf16 && past) hipLaunchKernelGGL((embed_sum_kernel<IoBF16, true>), dim3(sum_wgs), dim3(256), 0, st, a);
+    else if (bf16) hipLaunchKernelGGL((embed_sum_kernel<IoBF16, false>), dim3(sum_wgs), dim3(256), 0, st, a);
+    else if (past) hipLaunchKernelGGL((embed_sum_kernel<IoF32, true>), dim3(sum_wgs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((embed_sum_kernel<IoF32, false>), dim3(sum_wgs), dim3(256), 0, st, a);
     if (p.slices > 1) {
         EmbedJoinArgs ja{slots, dtable, n_spans, span, p.slices, kShortGroups, 64, d->d_model, 0, d->scale};
         while (ja.lanes > 4 && ja.lanes / 2 * 4 >= (unsigned)d->d_model) ja.lanes /= 2;

@@ -21,17 +21,29 @@ struct Piece {
     typename IO::T v[N];
     __device__ __forceinline__ float operator[](int i) const { return IO::cvt(v[i]); }
 };
-template <typename IO, int N = kPieceOf<IO>>
+// kPast: past the caches.  For calls that move more than these hold (past_caches below): what such a call leaves there is of no use, and the
+// lines it has to push out cost it time.  Stores, 65536 rows of 2048: layer norm 101 -> 97 us; gradient of 16384 rows of 50304 logits
+// 492 -> 407.  Loads help where little or nothing is written beside them: log probabilities of those logits 146 -> 127 us, layer norm's
+// gradients 169 -> 162; in those two 97 -> 115 and 402 -> 426, which therefore load through the caches.  (A flag at run time would not
+// do: the compiler joins the two accesses and drops the difference.)
+template <int kBytes>
+struct PastCaches {
+    typedef unsigned Bits __attribute__((ext_vector_type(kBytes / 4)));
+    typedef Bits Place __attribute__((aligned(2)));   // (of either element type)
+};
+template <typename IO, int N = kPieceOf<IO>, bool kPast = false>
 __device__ __forceinline__ Piece<IO, N> load_piece(const typename IO::T* p)
 {
     Piece<IO, N> r;
-    __builtin_memcpy(&r, p, sizeof r);
+    if constexpr (kPast && sizeof r >= 8) {
+        typedef PastCaches<sizeof r> Past;
+        const typename Past::Bits bits = __builtin_nontemporal_load(reinterpret_cast<const typename Past::Place*>(p));
+        __builtin_memcpy(&r, &bits, sizeof r);
+    } else {
+        __builtin_memcpy(&r, p, sizeof r);
+    }
     return r;
 }
-// kPast: past the caches.  For calls that move more than these hold (past_caches below): what such a call leaves there is of no use, and
-// the lines it has to push out for its outputs cost it time.  Gradient of 16384 rows of 50304 logits 492 -> 407 us, layer norm of
-// 65536 rows of 2048 101 -> 97.
-// (A flag at run time would not do: the compiler joins the two stores and drops the difference.)
 template <typename IO, bool kPast = false, int N>
 __device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[N])
 {
@@ -39,9 +51,8 @@ __device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[
 #pragma unroll
     for (int i = 0; i < N; i++) r.v[i] = io_value<IO>(f[i]);
     if constexpr (kPast && sizeof r >= 8) {
-        typedef unsigned Bits __attribute__((ext_vector_type(sizeof r / 4)));
-        typedef Bits Place __attribute__((aligned(2)));   // (of either element type)
-        __builtin_nontemporal_store(__builtin_bit_cast(Bits, r), reinterpret_cast<Place*>(p));
+        typedef PastCaches<sizeof r> Past;
+        __builtin_nontemporal_store(__builtin_bit_cast(typename Past::Bits, r), reinterpret_cast<typename Past::Place*>(p));
     } else {
         __builtin_memcpy(p, &r, sizeof r);
     }
@@ -50,10 +61,10 @@ __device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[
 // elements where the piece would reach beyond, so there is no branch around it and all loads of a lane are in flight together (with
 // the row's end told apart by a branch the compiler waited for each load where the two ways join: the sum of a table's
 // gradient ran at 1.5 TB/s).  settle() then puts what is left of the piece in its place, and `fill` beyond the row.
-template <typename IO, int N = kPieceOf<IO>>
+template <typename IO, int N = kPieceOf<IO>, bool kPast = false>
 __device__ __forceinline__ Piece<IO, N> load_clamped(const typename IO::T* row, int at, int n)
 {
-    return load_piece<IO, N>(row + min(at, n - N));
+    return load_piece<IO, N, kPast>(row + min(at, n - N));
 }
 template <typename IO, int N>
 __device__ __forceinline__ void settle(Piece<IO, N>& p, int at, int n, typename IO::T fill)

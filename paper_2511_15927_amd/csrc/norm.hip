@@ -256,9 +256,9 @@ __device__ __forceinline__ void norm_bwd_rows(const NormBwdArgs& a)
         const typename IO::T* const dy = static_cast<const typename IO::T*>(a.dy.p) + row_offset(a.dy, row.b, row.t);
         Piece<IO, kPiece> px[kPieces], pd[kPieces];
 #pragma unroll
-        for (int k = 0; k < kPieces; k++) px[k] = load_clamped<IO, kPiece>(x, at(k), a.d);
+        for (int k = 0; k < kPieces; k++) px[k] = load_clamped<IO, kPiece, kPast>(x, at(k), a.d);
 #pragma unroll
-        for (int k = 0; k < kPieces; k++) pd[k] = load_clamped<IO, kPiece>(dy, at(k), a.d);
+        for (int k = 0; k < kPieces; k++) pd[k] = load_clamped<IO, kPiece, kPast>(dy, at(k), a.d);
         const float mean = a.mean[row.at], rstd = a.rstd[row.at];
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll

@@ -114,7 +114,7 @@ __device__ __forceinline__ void store_top(const ScoresArgs& a, unsigned row, int
 // before, k times.
 constexpr int kScoresAhead = 4, kMaxListed = 256;
 constexpr int kManyRowsThreads = 256, kFewRowsThreads = 1024;
-template <typename IO, bool kEntropy, bool kTop, int kPiece, int kScoresThreads>
+template <typename IO, bool kEntropy, bool kTop, int kPiece, int kScoresThreads, bool kPast>
 __device__ __forceinline__ void scores_row(const ScoresArgs& a)
 {
     constexpr int kScoresWaves = kScoresThreads / 64, kGroups = 16, kGroupLanes = kScoresThreads / kGroups;   // (kMaxTop groups or more)
@@ -135,7 +135,7 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
     for (int first = threadIdx.x; first < pieces; first += kScoresThreads * kScoresAhead) {
         Piece<IO, kPiece> p[kScoresAhead];
 #pragma unroll
-        for (int j = 0; j < kScoresAhead; j++) p[j] = load_clamped<IO, kPiece>(x, (first + j * kScoresThreads) * kPiece, n);
+        for (int j = 0; j < kScoresAhead; j++) p[j] = load_clamped<IO, kPiece, kPast>(x, (first + j * kScoresThreads) * kPiece, n);
 #pragma unroll
         for (int j = 0; j < kScoresAhead; j++) {
             const int piece = first + j * kScoresThreads;
@@ -260,13 +260,13 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
         }
     }
 }
-template <typename IO, bool kEntropy, bool kTop, int kThreads>
+template <typename IO, bool kEntropy, bool kTop, int kThreads, bool kPast>
 __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresArgs a)
 {
     if constexpr (kThreads == kManyRowsThreads) {   // (rows shorter than a piece: a logit a lane)
-        if (a.vocab < kPieceOf<IO>) return scores_row<IO, kEntropy, kTop, 1, kThreads>(a);
+        if (a.vocab < kPieceOf<IO>) return scores_row<IO, kEntropy, kTop, 1, kThreads, kPast>(a);
     }
-    scores_row<IO, kEntropy, kTop, kPieceOf<IO>, kThreads>(a);
+    scores_row<IO, kEntropy, kTop, kPieceOf<IO>, kThreads, kPast>(a);
 }
 
 // A wave joins the parts of a row, a part a lane; the lanes' alternatives are in descending order already.
@@ -425,8 +425,11 @@ template <typename IO, bool kEntropy, bool kTop>
 void launch_scores(const ScoresArgs& a, int threads, hipStream_t st)
 {
     const dim3 grid(a.rows * (unsigned)a.splits), wg(threads);
-    if (threads == kFewRowsThreads) hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kFewRowsThreads>), grid, wg, 0, st, a);
-    else hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kManyRowsThreads>), grid, wg, 0, st, a);
+    // (up to a row a CU of 65536 logits is less than the caches hold)
+    if (threads == kFewRowsThreads) hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kFewRowsThreads, false>), grid, wg, 0, st, a);
+    else if (past_caches((double)a.rows * a.vocab * sizeof(typename IO::T)))
+        hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kManyRowsThreads, true>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((scores_kernel<IO, kEntropy, kTop, kManyRowsThreads, false>), grid, wg, 0, st, a);
     if (a.splits > 1) hipLaunchKernelGGL((scores_join_kernel<IO, kEntropy, kTop>), dim3(a.rows), dim3(64), 0, st, a);
 }
 template <typename IO>
