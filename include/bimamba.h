@@ -71,13 +71,13 @@ enum bimamba_status {
     BIMAMBA_OK = 0,
     BIMAMBA_ERR_NULL_POINTER = -1,        /* a required pointer is NULL */
     BIMAMBA_ERR_BAD_SHAPE = -2,           /* non-positive or inconsistent dimension, stride smaller than the row */
-    BIMAMBA_ERR_UNSUPPORTED = -3,         /* dtype / d_state / d_conv / grouping / token stride outside the compiled set */
+    BIMAMBA_ERR_UNSUPPORTED = -3,         /* dtype / d_state / d_conv / grouping / token stride / size outside the compiled set */
     BIMAMBA_ERR_MISALIGNED = -4,          /* pointer not aligned to its element size (or 16 bytes for the workspace) */
     BIMAMBA_ERR_WORKSPACE_TOO_SMALL = -5, /* workspace_bytes < bimamba_workspace_bytes() */
     BIMAMBA_ERR_HIP = -6,                 /* a launch of this call failed (errors pending from earlier, unrelated calls are
                                              neither reported nor cleared) */
     BIMAMBA_ERR_SCRATCH_EXCEEDED = -7,    /* bimamba_block_fwd_static: the call needs more than BIMAMBA_STATIC_SCRATCH_BYTES */
-    BIMAMBA_ERR_ALIAS = -8                /* out may overlap an input view; bimamba_bwd: dpf == dpb (checked on the host) */
+    BIMAMBA_ERR_ALIAS = -8                /* what is written may overlap what is read; bimamba_bwd: dpf == dpb (checked on the host) */
 };
 
 enum bimamba_dtype { BIMAMBA_F32 = 0, BIMAMBA_BF16 = 1 };

@@ -1267,11 +1267,11 @@ const char* bimamba_status_string(int status)
         case BIMAMBA_OK: return "ok";
         case BIMAMBA_ERR_NULL_POINTER: return "a required pointer is NULL";
         case BIMAMBA_ERR_BAD_SHAPE: return "bad shape: non-positive or inconsistent dimension or stride";
-        case BIMAMBA_ERR_UNSUPPORTED: return "unsupported dtype, d_state, d_conv, grouping or token stride";
+        case BIMAMBA_ERR_UNSUPPORTED: return "unsupported dtype, size, d_state, d_conv, grouping or token stride";
         case BIMAMBA_ERR_MISALIGNED: return "misaligned pointer";
         case BIMAMBA_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
         case BIMAMBA_ERR_HIP: return "HIP launch error";
-        case BIMAMBA_ERR_ALIAS: return "the output overlaps an input";
+        case BIMAMBA_ERR_ALIAS: return "an output overlaps an input or another output";
         case BIMAMBA_ERR_SCRATCH_EXCEEDED: return "the call needs more scratch than the library's static buffer holds";
         default: return "unknown status";
     }

@@ -5,7 +5,8 @@ namespace bm {
 
 // out[row] = scale * table[id].  A copy: bound by the rows written (and those of the table that are read).  `lanes` threads to a row,
 // 16 bytes of the wider
-// type a thread, so that a row's accesses are one run and a workgroup takes several short rows.
+// type a thread, so that a row's accesses are one run and a workgroup takes several short rows.  8 x 8192 rows of 2048: fp32 to bf16 65 us,
+// bf16 50, fp32 96 (537 MB written, 5.6 TB/s); 16 x 32 rows 3.3 us, the launch and two loads one after the other.
 struct EmbedArgs {
     const int64_t* ids;
     long long ids_sb, ids_st;
@@ -58,6 +59,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 // place counting by binary search what precedes it in the other seven.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
 // meanwhile the other workgroups of its launches clear the table, half of it each, so that only rows of ids that occur are left to
 // write.  (Looking up which rows are absent instead, after the sort, writes those rows once and not twice, but hides nothing.)
+// What bounds it are the bytes, 412 MB of zeros, 135 MB of dout and 53 MB of rows at 8 x 4096 tokens of 2048 channels and 50304 ids: 129 us
+// (sort 37 and merge 38 with the clearing in them, sums 46, join 7; 4.6 TB/s); for few tokens the four launches.
 
 // Places sorted by one workgroup, 2048 or 4096 by the bits that the ids leave of a 32-bit key, four neighbouring ones a lane.
 constexpr int kChunkBits = 11, kLargeChunkBits = 12, kSortKeys = 4;
@@ -72,7 +75,7 @@ struct EmbedClear {
     unsigned first_wg;   // of the launch; the workgroups before it sort
     int past;            // stores go past the caches
 };
-// (kThreads: of a workgroup.)  Floats that a workgroup clears, 16 bytes a lane side by side (at 32 bytes a lane, two stores that each leave every other 16 bytes to the
+// Floats that a workgroup of kThreads clears, 16 bytes a lane side by side (at 32 bytes a lane, two stores that each leave every other 16 bytes to the
 // other, it was 4.1 TB/s).
 constexpr int kClearFloats = 32768;
 template <int kThreads, bool kPast>

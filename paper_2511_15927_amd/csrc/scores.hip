@@ -11,7 +11,9 @@ constexpr float kFarBelow = -1e4f;   // a difference of logits whose exponential
 // One pass over a row.  A lane keeps of the logits x it has seen the largest (m), S = sum exp(x - m) and, for the entropy,
 // T = sum exp(x - m) (x - m); then lse = m + log S and H = log S - T / S, no value of which is large where the row is confident.  To a
 // larger maximum m' both move by r = exp(m - m'): S' = r S, T' = r (T + S (m - m')).  m starts at the lowest finite value, so a row of
-// nothing but -inf keeps S = 0, and a NaN or +inf makes S a NaN.
+// nothing but -inf keeps S = 0, and a NaN or +inf makes S a NaN.  What bounds it is the read: 8192 rows of 50304 bf16 127 us (6.5 TB/s);
+// 12 vector slots a logit, of which the exponential is four, would allow twice that.  32 rows with the entropy and eight alternatives:
+// 9.7 us, of which the alternatives are 3, the rest two rounds of loads and the joining of a workgroup's sums.
 struct Stats {
     float m, s, t;
 };
@@ -310,7 +312,8 @@ __global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
 // ---- gradient ----
 //
 // Elementwise, given lse and the entropy: p = exp(x - lse), dx = dlogp (1[target] - p) - dentropy p (log p + H).  A logit is read and its
-// gradient written by the same lane, so the gradient may take the logits' place.
+// gradient written by the same lane, so the gradient may take the logits' place.  16384 rows of 50304 bf16, half of them without a target
+// and so only written: 403 us (2.47 GB, 6.1 TB/s), bound by the bytes.
 constexpr int kGradThreads = 256, kGradPart = kGradThreads * 32;
 struct ScoresBwdArgs {
     RowView logits, dlogits;
