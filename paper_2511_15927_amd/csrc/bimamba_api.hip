@@ -1271,7 +1271,7 @@ const char* bimamba_status_string(int status)
         case BIMAMBA_ERR_MISALIGNED: return "misaligned pointer";
         case BIMAMBA_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
         case BIMAMBA_ERR_HIP: return "HIP launch error";
-        case BIMAMBA_ERR_ALIAS: return "an output overlaps an input or another output";
+        case BIMAMBA_ERR_ALIAS: return "the output overlaps an input";
         case BIMAMBA_ERR_SCRATCH_EXCEEDED: return "the call needs more scratch than the library's static buffer holds";
         default: return "unknown status";
     }

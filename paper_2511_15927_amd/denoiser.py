@@ -157,7 +157,7 @@ class Denoiser:
                           "%d.%s.A_log" % (l, s): torch.log(torch.arange(1, N + 1).float()).repeat(Dn, 1), "%d.%s.D" % (l, s): torch.ones(Dn),
                           "%d.%s.dt_bias" % (l, s): torch.log(torch.expm1(dt))})
         self.params = {k: t.to(device).requires_grad_() for k, t in p.items()}
-        self._clip = None
+        self._clip = None   # made with the first step: the table of the gradients, which stay where they are, their norm, the workspace
 
     def _linear(self, x, name):
         """x [batch, L, n] times a weight's transpose, as one plain matrix product."""
@@ -200,16 +200,19 @@ class Denoiser:
 
     def train_step(self, tokens, gen, lr=0.05, max_norm=1.0):
         """One step of gradient descent with clipping on clean tokens [batch, L].  Returns the loss and the gradients' norm (on the device)."""
-        loss = self.loss(*self.noised(tokens, gen))
         params = list(self.params.values())
-        grads = torch.autograd.grad(loss, params)
-        if self._clip is None:   # the scaled gradients' places, and the table that says where they go
-            self._clip = [torch.empty_like(p, requires_grad=False) for p in params]
-        table = bd.GradTable([g.contiguous() for g in grads], self._clip)
-        norm = torch.empty(1, device=loss.device)
-        bd.bimamba_clip_grads(table, max_norm, norm, _bytes(bd.bimamba_clip_grads_workspace_bytes(table), loss))
+        if self._clip is None:
+            for p in params:
+                p.grad = torch.zeros_like(p)
+            table = bd.GradTable([p.grad for p in params])
+            self._clip = table, torch.empty(1, device=tokens.device), _bytes(bd.bimamba_clip_grads_workspace_bytes(table), tokens)
+        table, norm, ws = self._clip
+        torch._foreach_zero_(table.grads)
+        loss = self.loss(*self.noised(tokens, gen))
+        loss.backward()
+        bd.bimamba_clip_grads(table, max_norm, norm, ws)
         with torch.no_grad():
-            torch._foreach_add_(params, self._clip, alpha=-lr)
+            torch._foreach_add_(params, table.grads, alpha=-lr)
         return loss.detach(), norm
 
     @torch.no_grad()
