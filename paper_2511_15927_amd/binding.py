@@ -141,14 +141,14 @@ def lib():
         L.bimamba_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
         P, V, Z, I = C.POINTER, C.c_void_p, C.c_size_t, C.c_int
         for name, res, args in (
-                ("bimamba_embed", I, [P(EmbedDesc), V, V, V, V]),
-                ("bimamba_embed_bwd", I, [P(EmbedDesc), V, V, V, V, Z, V]),
+                ("bimamba_embed", I, [P(EmbedDesc), P(Tokens), V, P(Tensor), V]),
+                ("bimamba_embed_bwd", I, [P(EmbedDesc), P(Tokens), P(Tensor), V, V, Z, V]),
                 ("bimamba_embed_bwd_workspace_bytes", Z, [P(EmbedDesc)]),
-                ("bimamba_layer_norm", I, [P(NormDesc), V, V, V, C.c_int64, V, V, V, V]),
-                ("bimamba_layer_norm_bwd", I, [P(NormDesc), V, V, C.c_int64, V, V, V, V, V, V, V, Z, V]),
+                ("bimamba_layer_norm", I, [P(NormDesc), P(Tensor), V, V, C.c_int64, P(Tensor), V, V, V]),
+                ("bimamba_layer_norm_bwd", I, [P(NormDesc), P(Tensor), V, C.c_int64, V, V, P(Tensor), P(Tensor), V, V, V, Z, V]),
                 ("bimamba_layer_norm_bwd_workspace_bytes", Z, [P(NormDesc), I]),
-                ("bimamba_log_probs", I, [P(LogitsDesc), V, V, P(Scores), V, Z, V]),
-                ("bimamba_log_probs_bwd", I, [P(LogitsDesc), V, V, V, V, V, V, V, V]),
+                ("bimamba_log_probs", I, [P(LogitsDesc), P(Tensor), P(Tokens), P(Scores), V, Z, V]),
+                ("bimamba_log_probs_bwd", I, [P(LogitsDesc), P(Tensor), P(Tokens), V, V, V, V, P(Tensor), V]),
                 ("bimamba_log_probs_workspace_bytes", Z, [P(LogitsDesc)]),
                 ("bimamba_clip_layout", I, [P(Grad), I]),
                 ("bimamba_clip_grads", I, [P(Grad), I, V, C.c_float, V, V, Z, V]),
@@ -341,74 +341,39 @@ def bimamba_copy_inputs(desc, src, dst, stream=None, check=True):
 
 # ---- what stands around the mixers: token table, layer norm, log probabilities, clipped gradients ----
 #
-# These take the tensors themselves and check them against the descriptor: shape, type, unit stride along a row.  Tensors of a call are
-# on the current device, and the stream is the current one unless another is given.
+# These take the tensors themselves.  csrc/torch_calls.cpp checks them against the descriptor (shape, type, unit stride along a row, on the
+# GPU: an AssertionError) and makes the call.  Tensors of a call are on the current device, and the stream is the current one unless
+# another is given.
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
-_TORCH = (torch.float32, torch.bfloat16)
 _NAMES = {"f32": F32, "bf16": BF16}
+_calls_module = None
+
+
+def _calls():
+    """The extension module built beside libbimamba.so; raises if it is missing."""
+    global _calls_module
+    if _calls_module is None:
+        lib()   # (which it is linked to)
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise RuntimeError("_calls.so is not built: run `python -m paper_2511_15927_amd.build` (there is no CPU fallback): %s" % e) from e
+        _calls_module = module
+    return _calls_module
 
 
 def _stream(stream):
-    # (a call's tensors are on the GPU, so torch has been initialised)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+    # (a call's tensors are on the GPU, so torch has been initialised; if they are not, the call ends before the stream is used)
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if torch.cuda.is_initialized() else 0
 
 
-def _wrong(t, what, dtype, shape, more=""):
-    raise AssertionError("%s: %s %s with strides %s on %s, wanted %s %s on the GPU%s" % (
-        what, t.dtype, tuple(t.shape), t.stride(), t.device, dtype, tuple(shape), more))
-
-
-_VIEW_WORDS = struct.Struct("=Qqq")   # a Tensor, a Tokens: their bytes go over as they are (a struct and a reference to it cost 0.1 us more)
-assert _VIEW_WORDS.size == C.sizeof(Tensor) == C.sizeof(Tokens)
-
-
-def _rows(t, what, dtype, shape):
-    """[batch, L, width] activations -> the bytes of a Tensor.  (The host's share of a small call counts: each check reads what it needs
-    once.)"""
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape:
-        _wrong(t, what, dtype, shape)
-    sb, st, s1 = t.stride()
-    if s1 != 1 and shape[2] != 1 and t.numel() != 0:
-        _wrong(t, what, dtype, shape, ", the channels contiguous")
-    return _VIEW_WORDS.pack(t.data_ptr(), sb, st)
-
-
-def _ids(t, what, shape):
-    if t.dtype is not torch.int64 or not t.is_cuda or t.shape != shape:
-        _wrong(t, what, torch.int64, shape)
-    return _VIEW_WORDS.pack(t.data_ptr(), *t.stride())
-
-
-def _flat(t, what, shape, dtype=torch.float32):
-    """Contiguous device array of a shape, or None -> pointer."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        _wrong(t, what, dtype, shape, ", contiguous")
-    return t.data_ptr()
-
-
-def _vector(t, what, batch, d):
-    """A parameter vector [d], or [batch, d] with unit stride along a vector -> (pointer, stride between vectors)."""
-    if t is None:
-        return None, None
-    shape = t.shape
-    if t.dtype is not torch.float32 or not t.is_cuda or (shape != (batch, d) and shape != (d,)):
-        _wrong(t, what, torch.float32, (batch, d), ", or one vector")
-    s = t.stride()
-    if s[-1] != 1 and d != 1 and t.numel() != 0:
-        _wrong(t, what, torch.float32, (batch, d), ", each vector contiguous")
-    if len(s) == 1:
-        return t.data_ptr(), 0
-    stride = s[0] if batch > 1 else d
-    if stride < d:
-        _wrong(t, what, torch.float32, (batch, d), ", the vectors apart")
-    return t.data_ptr(), stride
-
-
-def _workspace(t):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+def _checked(rc, name, check):
+    if check and rc != 0:
+        raise BimambaError(rc, name)
+    return rc
 
 
 def make_embed_desc(batch, seqlen, d_model, vocab, table="f32", io="bf16", scale=1.0):
@@ -418,13 +383,7 @@ def make_embed_desc(batch, seqlen, d_model, vocab, table="f32", io="bf16", scale
 def bimamba_embed(desc, tokens, table, out, stream=None, check=True):
     """Enqueue out[b, t] = scale * table[tokens[b, t]].  tokens: int64 [batch, L]; table [vocab, d_model] contiguous; out
     [batch, L, d_model]."""
-    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed(C.byref(desc), _ids(tokens, "tokens", (Bt, L)),
-                             _flat(table, "table", (desc.vocab, D), dtype=_TORCH[desc.table_dtype]),
-                             _rows(out, "out", _TORCH[desc.io_dtype], (Bt, L, D)), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_embed")
-    return rc
+    return _checked((_calls_module or _calls()).embed(desc, tokens, table, out, _stream(stream)), "bimamba_embed", check)
 
 
 def bimamba_embed_bwd_workspace_bytes(desc):
@@ -433,13 +392,7 @@ def bimamba_embed_bwd_workspace_bytes(desc):
 
 def bimamba_embed_bwd(desc, tokens, dout, dtable, workspace, stream=None, check=True):
     """Enqueue the gradient of the table: dtable float32 [vocab, d_model] contiguous, overwritten."""
-    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    rc = lib().bimamba_embed_bwd(C.byref(desc), _ids(tokens, "tokens", (Bt, L)),
-                                 _rows(dout, "dout", _TORCH[desc.io_dtype], (Bt, L, D)),
-                                 _flat(dtable, "dtable", (desc.vocab, D)), *_workspace(workspace), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_embed_bwd")
-    return rc
+    return _checked((_calls_module or _calls()).embed_bwd(desc, tokens, dout, dtable, workspace, _stream(stream)), "bimamba_embed_bwd", check)
 
 
 def make_norm_desc(batch, seqlen, d_model, io="bf16", eps=1e-5):
@@ -449,17 +402,7 @@ def make_norm_desc(batch, seqlen, d_model, io="bf16", eps=1e-5):
 def bimamba_layer_norm(desc, x, weight, bias, y, mean=None, rstd=None, stream=None, check=True):
     """Enqueue the layer norm of every row.  weight, bias: float32 [d_model], or [batch, d_model] with a vector for each batch
     element, or None; both of the same kind and row stride.  mean, rstd: float32 [batch, L] or None (bimamba_layer_norm_bwd takes them)."""
-    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    io = _TORCH[desc.io_dtype]
-    w, ws = _vector(weight, "weight", Bt, D)
-    b, bs = _vector(bias, "bias", Bt, D)
-    assert ws is None or bs is None or ws == bs, "weight and bias: not of the same kind and stride"
-    rc = lib().bimamba_layer_norm(C.byref(desc), _rows(x, "x", io, (Bt, L, D)), w, b, bs or 0 if ws is None else ws,
-                                  _rows(y, "y", io, (Bt, L, D)), _flat(mean, "mean", (Bt, L)), _flat(rstd, "rstd", (Bt, L)),
-                                  _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_layer_norm")
-    return rc
+    return _checked((_calls_module or _calls()).layer_norm(desc, x, weight, bias, y, mean, rstd, _stream(stream)), "bimamba_layer_norm", check)
 
 
 def bimamba_layer_norm_bwd_workspace_bytes(desc, per_batch):
@@ -469,19 +412,8 @@ def bimamba_layer_norm_bwd_workspace_bytes(desc, per_batch):
 def bimamba_layer_norm_bwd(desc, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, stream=None, check=True):
     """Enqueue the gradients of bimamba_layer_norm.  dweight, dbias: float32 [d_model], or [batch, d_model] where each batch element
     has a vector of its own (weight None: their shape says which), or None; overwritten."""
-    Bt, L, D = desc.batch, desc.seqlen, desc.d_model
-    io = _TORCH[desc.io_dtype]
-    w, ws = _vector(weight, "weight", Bt, D)
-    if ws is None:
-        ws = D if any(g is not None and g.dim() == 2 for g in (dweight, dbias)) else 0
-    shape = (Bt, D) if ws else (D,)
-    rc = lib().bimamba_layer_norm_bwd(C.byref(desc), _rows(x, "x", io, (Bt, L, D)), w, ws, _flat(mean, "mean", (Bt, L)),
-                                      _flat(rstd, "rstd", (Bt, L)), _rows(dy, "dy", io, (Bt, L, D)),
-                                      _rows(dx, "dx", io, (Bt, L, D)), _flat(dweight, "dweight", shape),
-                                      _flat(dbias, "dbias", shape), *_workspace(workspace), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_layer_norm_bwd")
-    return rc
+    return _checked((_calls_module or _calls()).layer_norm_bwd(desc, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, _stream(stream)),
+                    "bimamba_layer_norm_bwd", check)
 
 
 def make_logits_desc(batch, seqlen, vocab, io="bf16", top_k=0, targets_only=0):
@@ -495,29 +427,17 @@ def bimamba_log_probs_workspace_bytes(desc):
 def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, check=True):
     """Enqueue the log probabilities of targets (int64 [batch, L], or None) under softmax(logits).  out: dict of what is wanted:
     logp, lse, entropy float32 [batch, L]; top_logp float32 and top_token int64 [batch, L, top_k]."""
-    Bt, L, k = desc.batch, desc.seqlen, desc.top_k
-    s = Scores(_flat(out.get("logp"), "logp", (Bt, L)), _flat(out.get("lse"), "lse", (Bt, L)), _flat(out.get("entropy"), "entropy", (Bt, L)),
-               _flat(out.get("top_logp"), "top_logp", (Bt, L, k)), _flat(out.get("top_token"), "top_token", (Bt, L, k), dtype=torch.int64))
-    rc = lib().bimamba_log_probs(C.byref(desc), _rows(logits, "logits", _TORCH[desc.io_dtype], (Bt, L, desc.vocab)),
-                                 None if targets is None else _ids(targets, "targets", (Bt, L)), C.byref(s),
-                                 *_workspace(workspace), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_log_probs")
-    return rc
+    get = out.get
+    rc = (_calls_module or _calls()).log_probs(desc, logits, targets, get("logp"), get("lse"), get("entropy"), get("top_logp"), get("top_token"),
+                                               workspace, _stream(stream))
+    return _checked(rc, "bimamba_log_probs", check)
 
 
 def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
     """Enqueue the gradient for the logits, given those of logp and of the entropy (float32 [batch, L]; either None).  dlogits may be
     logits itself."""
-    Bt, L = desc.batch, desc.seqlen
-    io = _TORCH[desc.io_dtype]
-    rc = lib().bimamba_log_probs_bwd(C.byref(desc), _rows(logits, "logits", io, (Bt, L, desc.vocab)),
-                                     None if targets is None else _ids(targets, "targets", (Bt, L)), _flat(lse, "lse", (Bt, L)),
-                                     _flat(entropy, "entropy", (Bt, L)), _flat(dlogp, "dlogp", (Bt, L)), _flat(dentropy, "dentropy", (Bt, L)),
-                                     _rows(dlogits, "dlogits", io, (Bt, L, desc.vocab)), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_log_probs_bwd")
-    return rc
+    return _checked((_calls_module or _calls()).log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, _stream(stream)),
+                    "bimamba_log_probs_bwd", check)
 
 
 class GradTable:
@@ -544,11 +464,7 @@ def bimamba_clip_grads_workspace_bytes(table):
 
 def bimamba_clip_grads(table, max_norm, norm, workspace, stream=None, check=True):
     """Enqueue the norm of a GradTable's gradients (norm: float32 [1], or None) and their scaling to at most max_norm."""
-    rc = lib().bimamba_clip_grads(table.host, table.n, None if table.dev is None else table.dev.data_ptr(), max_norm,
-                                  _flat(norm, "norm", (1,)), *_workspace(workspace), _stream(stream))
-    if check and rc != 0:
-        raise BimambaError(rc, "bimamba_clip_grads")
-    return rc
+    return _checked((_calls_module or _calls()).clip_grads(table.host, table.dev, max_norm, norm, workspace, _stream(stream)), "bimamba_clip_grads", check)
 
 
 # ---- conveniences used by tests and the benchmark (allocation through torch, no arithmetic) ----

@@ -1,4 +1,4 @@
-"""Compile the HIP library for gfx950 into paper_2511_15927_amd/libbimamba.so (in-tree, hipcc)."""
+"""Compile the HIP library for gfx950 into paper_2511_15927_amd/libbimamba.so (in-tree, hipcc), and _calls.so beside it (g++)."""
 import os
 import subprocess
 from concurrent.futures import ThreadPoolExecutor
@@ -8,6 +8,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbimamba.so")
+CALLS = os.path.join(HERE, "_calls.so")   # the calls around the mixers as functions of torch tensors (host code)
 # (d_state, lanes per chain) pairs the scan kernels are instantiated for
 VARIANTS = ((4, 1), (8, 1), (16, 1), (16, 2), (16, 4), (32, 1), (32, 2), (32, 4), (64, 1), (64, 4), (128, 1), (128, 4))
 # (d_state, head width) pairs of the many-wave chunk walk
@@ -41,8 +42,29 @@ def newest_dep(src, newest_all):
     return max(os.path.getmtime(p) for p in deps)
 
 
+def compile_calls(force):
+    """Object of the extension module."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    src, obj = os.path.join(CSRC, "torch_calls.cpp"), os.path.join(OBJ, "torch_calls.o")
+    if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src), os.path.getmtime(os.path.join(ROOT, "include", "bimamba.h"))):
+        return ""
+    includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
+    return _run(["g++", "-O2", "-std=c++17", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] +
+                [x for p in includes for x in ("-isystem" if "torch" in p else "-I", p)] + ["-Wall", "-c", src, "-o", obj])
+
+
+def link_calls():
+    """The extension module beside the library, which it finds there; torch's libraries are in the process that imports it."""
+    from torch.utils import cpp_extension
+    return _run(["g++", "-shared", "-o", CALLS, os.path.join(OBJ, "torch_calls.o"), "-L" + HERE, "-l:libbimamba.so", "-Wl,-rpath,$ORIGIN"] +
+                ["-L" + p for p in cpp_extension.library_paths()] + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+
+
 def build(force: bool = True, jobs: int = 8):
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= max(os.path.getmtime(p) for p in sources()):
+    if not force and os.path.exists(LIB) and os.path.exists(CALLS) and min(map(os.path.getmtime, (LIB, CALLS))) >= max(os.path.getmtime(p) for p in sources()):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     units = [(os.path.join(CSRC, "bimamba_api.hip"), os.path.join(OBJ, "bimamba_api.o"), [])]
@@ -62,9 +84,11 @@ def build(force: bool = True, jobs: int = 8):
     newest = max(os.path.getmtime(p) for p in sources())
     todo = [u for u in units if force or not os.path.exists(u[1]) or os.path.getmtime(u[1]) < newest_dep(u[0], newest)]
     cmds = [["hipcc"] + FLAGS + extra + ["-c", src, "-o", obj] for src, obj, extra in todo]
-    with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds)))) as ex:
-        logs = list(ex.map(_run, cmds))
+    with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds) + 1))) as ex:
+        calls = ex.submit(compile_calls, force)
+        logs = list(ex.map(_run, cmds)) + [calls.result()]
     logs.append(_run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [u[1] for u in units]))
+    logs.append(link_calls())
     out = "\n".join(l for l in logs if l.strip())
     if out.strip():
         print(out)
