@@ -11,6 +11,7 @@ namespace bm {
 // (each workgroup a run of pieces of its own, walked backwards, everything through the caches: 761; the pieces in turn 692; stores past
 // the caches 640; nothing kept for the second launch 629).
 constexpr int kClipThreads = 256, kClipPiece = 8192;
+constexpr int kClipSums = 8;               // sums that a thread adds up: of 2048 workgroups, eight a CU
 constexpr long long kKept = 192ll << 20;   // bytes that the first launch leaves in the caches for the second
 struct ClipArgs {
     const bimamba_grad* table;
@@ -21,19 +22,31 @@ struct ClipArgs {
     double* sums;
 };
 
-// Index of the last tensor that starts at or before a piece (empty ones start where the next does); 64 tensors are looked at together.
-__device__ __forceinline__ int tensor_of(const ClipArgs& a, long long piece)
+// The last tensor that starts at or before a piece that there is (empty ones start where the next does).  64 tensors are looked at together, in the
+// last round with all that is to be known of them.
+__device__ __forceinline__ bimamba_grad tensor_of(const ClipArgs& a, long long piece)
 {
     const int lane = threadIdx.x % 64;
-    int lo = 0;
-    for (int range = a.n; range > 1;) {
-        const int step = (range + 63) / 64;
+    int lo = 0, range = a.n, step;
+    while ((step = (range + 63) / 64) > 1) {
         const bool there = lane * step < range;
         const int count = __popcll(__ballot(there && a.table[there ? lo + lane * step : lo].first <= piece));   // (the first lanes)
         range = min(step, range - (count - 1) * step);
         lo += (count - 1) * step;
     }
-    return lo;
+    const bool there = lane < range;
+    const bimamba_grad g = a.table[there ? lo + lane : lo];
+    const int at = __popcll(__ballot(there && g.first <= piece)) - 1;
+    const auto of_lane = [&](long long v) {
+        return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), at) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, at));
+    };
+    bimamba_grad r{};
+    r.from = reinterpret_cast<const void*>(of_lane(reinterpret_cast<long long>(g.from)));
+    r.to = reinterpret_cast<void*>(of_lane(reinterpret_cast<long long>(g.to)));
+    r.count = of_lane(g.count);
+    r.first = of_lane(g.first);
+    r.dtype = __builtin_amdgcn_readlane(g.dtype, at);
+    return r;
 }
 
 // What a lane does with its elements of a piece, four loads in flight at a time: use(elements, where they start).  A piece of fewer elements
@@ -101,7 +114,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipAr
 {
     double s = 0.0;
     for (long long p = blockIdx.x; p < a.pieces; p += gridDim.x) {
-        const bimamba_grad g = a.table[tensor_of(a, p)];
+        const bimamba_grad g = tensor_of(a, p);
         const long long at = (p - g.first) * kClipPiece;
         const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
         const bool past = p < a.past;
@@ -120,8 +133,16 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(const ClipAr
 template <bool kPast>
 __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(const ClipArgs a)
 {
+    // (the sums and the tensor of the first piece are asked for together)
+    double part[kClipSums];
+#pragma unroll
+    for (int k = 0; k < kClipSums; k++) part[k] = k * kClipThreads + threadIdx.x < gridDim.x ? a.sums[k * kClipThreads + threadIdx.x] : 0.0;
+    bimamba_grad g{};
+    if (blockIdx.x < a.pieces) g = tensor_of(a, a.pieces - 1 - blockIdx.x);   // (no pieces: no table either)
     double s = 0.0;
-    for (unsigned k = threadIdx.x; k < gridDim.x; k += kClipThreads) s += a.sums[k];
+#pragma unroll
+    for (int k = 0; k < kClipSums; k++) s += part[k];
+    for (unsigned k = kClipSums * kClipThreads + threadIdx.x; k < gridDim.x; k += kClipThreads) s += a.sums[k];
     s = workgroup_sum(s);
     const double norm = sqrt(s);
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
@@ -129,7 +150,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(const ClipArgs
     const float scale = isfinite((float)norm) && norm > (double)a.max_norm ? (float)((double)a.max_norm / norm) : 1.0f;
     for (long long k = blockIdx.x; k < a.pieces; k += gridDim.x) {
         const long long p = a.pieces - 1 - k;
-        const bimamba_grad g = a.table[tensor_of(a, p)];
+        if (k != blockIdx.x) g = tensor_of(a, p);
         if (scale == 1.0f && g.from == g.to) continue;
         const long long at = (p - g.first) * kClipPiece;
         const int n = (int)min((long long)kClipPiece, (long long)g.count - at);
