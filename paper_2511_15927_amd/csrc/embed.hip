@@ -3,10 +3,9 @@
 
 namespace bm {
 
-// out[row] = scale * table[id].  A copy: bound by the rows written (and those of the table that are read).  `lanes` threads to a row,
-// 16 bytes of the wider
-// type a thread, so that a row's accesses are one run and a workgroup takes several short rows.  8 x 8192 rows of 2048: fp32 to bf16 65 us,
-// bf16 50, fp32 96 (537 MB written, 5.6 TB/s); 16 x 32 rows 3.3 us, the launch and two loads one after the other.
+// out[row] = scale * table[id].  A copy: bound by the rows written (and those of the table that are read).  `lanes` threads to a row, 16
+// bytes of the wider type a thread, so that a row's accesses are one run and a workgroup takes several short rows.  8 x 8192 rows of
+// 2048: fp32 to bf16 65 us, bf16 50, fp32 96 (537 MB written, 5.6 TB/s); 16 x 32 rows 3.3 us, the launch and two loads one after the other.
 struct EmbedArgs {
     const int64_t* ids;
     long long ids_sb, ids_st;
@@ -75,8 +74,7 @@ struct EmbedClear {
     unsigned first_wg;   // of the launch; the workgroups before it sort
     int past;            // stores go past the caches
 };
-// Floats that a workgroup of kThreads clears, 16 bytes a lane side by side (at 32 bytes a lane, two stores that each leave every other 16 bytes to the
-// other, it was 4.1 TB/s).
+// Floats that a workgroup of kThreads clears.
 constexpr int kClearFloats = 32768;
 template <int kThreads, bool kPast>
 __device__ __forceinline__ void clear_part_as(const EmbedClear& c)
@@ -266,22 +264,18 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
         for (int q = 0; q < kRuns; q++)
             if (below[q] + step <= len[q] && precedes(q, other[q])) below[q] += step;
     }
-    constexpr int kTogether = kRuns;
+    unsigned window[kRuns][kMergeWindow];
 #pragma unroll
-    for (int q0 = 0; q0 < kRuns; q0 += kTogether) {
-        unsigned window[kTogether][kMergeWindow];
+    for (int q = 0; q < kRuns; q++) {   // (the lists are as long as whole chunks; a run that is not there: this place's own)
+        const unsigned at = below[q] < len[q] ? (first + q) * run + below[q] : i & ~(kMergeWindow - 1u);
+        __builtin_memcpy(window[q], __builtin_assume_aligned(a.id + at, 16), sizeof window[q]);
+    }
 #pragma unroll
-        for (int q = 0; q < kTogether; q++) {   // (the lists are as long as whole chunks; a run that is not there: this place's own)
-            const unsigned at = below[q0 + q] < len[q0 + q] ? (first + q0 + q) * run + below[q0 + q] : i & ~(kMergeWindow - 1u);
-            __builtin_memcpy(window[q], __builtin_assume_aligned(a.id + at, 16), sizeof window[q]);
-        }
+    for (int q = 0; q < kRuns; q++) {
+        unsigned count = 0;
 #pragma unroll
-        for (int q = 0; q < kTogether; q++) {
-            unsigned count = 0;
-#pragma unroll
-            for (unsigned k = 0; k < kMergeWindow; k++) count += below[q0 + q] + k < len[q0 + q] && precedes(q0 + q, window[q][k]);
-            below[q0 + q] += count;
-        }
+        for (unsigned k = 0; k < kMergeWindow; k++) count += below[q] + k < len[q] && precedes(q, window[q][k]);
+        below[q] += count;
     }
     unsigned to = first * run + (i - r * run);
 #pragma unroll
@@ -292,7 +286,7 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const EmbedMergeArgs a
 
 // A wave sums a slice of neighbouring places over 512 channels, eight a lane.  A run of one id that lies within the slice gives its row of
 // dtable; what a run that goes on into the next slice, or came from the one before, adds up to here is left in the slice's two slots
-// for embed_join_kernel, and the slice in which such a run starts is put on a list (whose order says nothing about any sum).
+// for embed_join_kernel, and such a run is put on a list (whose order says nothing about any sum).
 constexpr int kMaxSlice = 64;
 constexpr int kSumCols = 512;
 constexpr unsigned kShortSpan = 16;   // slices that a short run reaches into at most
@@ -520,7 +514,7 @@ EmbedPlan plan_embed(const bimamba_embed_desc* d)
 {
     EmbedPlan p{};
     p.rows = (unsigned)((long long)d->batch * d->seqlen);
-    // (up to 4096 places need no merge then: 3711 of them 38 -> 34 us)
+    // (up to 4096 places then need no merge: 3711 of them, 740 channels, 38 -> 34 us in all)
     p.chunk = d->vocab < 1 << (32 - kLargeChunkBits) && p.rows > 1u << kChunkBits ? 1u << kLargeChunkBits : 1u << kChunkBits;
     p.chunks = (p.rows + p.chunk - 1) / p.chunk;
     p.col_blocks = (d->d_model + kSumCols - 1) / kSumCols;
@@ -616,7 +610,7 @@ int bimamba_embed_bwd(const bimamba_embed_desc* d, const bimamba_tokens* tokens,
     for (unsigned long long run = p.chunk; run < p.rows; run *= kMergeRuns) {
         const unsigned merge_wgs = (p.rows + 255) / 256;
         const EmbedMergeArgs ma{id, place, to_id, to_place, p.rows, (unsigned)run, EmbedClear{dtable + early, left, merge_wgs, past}};
-        // (few runs: less to look at.  3711 places 15 -> 10 us)
+        // (few runs, less to look at: 16384 places, four runs 7.7 us; 32768, eight runs 11.8)
         if (run * kFewRuns >= p.rows) hipLaunchKernelGGL(embed_merge_kernel<kFewRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
         else hipLaunchKernelGGL(embed_merge_kernel<kMergeRuns>, dim3(merge_wgs + wgs(left)), dim3(256), 0, st, ma);
         left = 0;

@@ -191,15 +191,31 @@ def test_clip_refusals():
 
 
 def test_the_binding_checks_tensors_against_the_descriptor():
-    """Host tensors, other shapes, types and strides never reach the library."""
+    """Host tensors, other shapes and types, descriptors of another call and what is no tensor never reach the library."""
     x = torch.zeros(2, 10, 64, dtype=torch.bfloat16)
-    d = bd.make_norm_desc(2, 10, 64)
-    with pytest.raises(AssertionError):
+    d, e = bd.make_norm_desc(2, 10, 64), bd.make_embed_desc(2, 10, 64, 100)
+    with pytest.raises(AssertionError, match=r"x: BFloat16 \(2, 10, 64\) with strides \(640, 64, 1\) on cpu, wanted BFloat16 \(2, 10, 64\) on the GPU"):
         bd.bimamba_layer_norm(d, x, None, None, x.clone())
+    with pytest.raises(AssertionError, match="x: Float"):
+        bd.bimamba_layer_norm(d, x.float(), None, None, x.clone())
+    with pytest.raises(AssertionError, match=r"tokens: Int .*wanted Long \(2, 10\)"):
+        bd.bimamba_embed(e, torch.zeros(2, 10, dtype=torch.int32), torch.zeros(100, 64), x)
+    with pytest.raises(AssertionError, match="a descriptor of another call"):
+        bd.bimamba_embed(d, torch.zeros(2, 10, dtype=torch.int64), torch.zeros(100, 64), x)
+    with pytest.raises(AssertionError, match="x: not a tensor"):
+        bd.bimamba_layer_norm(d, [1.0], None, None, x)
+    with pytest.raises(AssertionError, match="logits: BFloat16"):
+        bd.bimamba_log_probs(bd.make_logits_desc(2, 10, 65), x, None, {})
+    with pytest.raises(AssertionError, match="logits: BFloat16"):
+        bd.bimamba_log_probs_bwd(bd.make_logits_desc(2, 10, 65), x, None, None, None, None, None, x)
     with pytest.raises(AssertionError):
-        bd.bimamba_embed(bd.make_embed_desc(2, 10, 64, 100), torch.zeros(2, 10, dtype=torch.int32), torch.zeros(100, 64), x)
+        bd.bimamba_embed_bwd(e, torch.zeros(2, 10, dtype=torch.int64), x, torch.zeros(100, 64), None)
+    with pytest.raises(AssertionError):
+        bd.bimamba_layer_norm_bwd(d, x, None, None, None, x, x.clone(), None, None, None)
     with pytest.raises(AssertionError):
         bd.GradTable([torch.zeros(4)])
+    with pytest.raises(AttributeError):
+        bd.bimamba_clip_grads(None, 1.0, None, None)
     with pytest.raises(KeyError):
         bd.make_logits_desc(1, 1, 10, io="f16")
 
