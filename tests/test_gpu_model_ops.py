@@ -73,6 +73,13 @@ def test_embed_rows(bd, batch, seqlen, d, vocab, extra, io, table):
     assert torch.equal(out.cpu(), ref)
 
 
+def test_embed_of_unknown_ids_takes_nothing_from_the_table(bd):
+    table = torch.full((3, 100), float("nan"))
+    out = nans(1, 4, 100)
+    bd.bimamba_embed(bd.make_embed_desc(1, 4, 100, 3, io="f32"), torch.tensor([[-1, 3, 2 ** 62, -2 ** 63]], device="cuda"), table.cuda(), out)
+    assert torch.equal(out, torch.zeros(1, 4, 100, device="cuda"))
+
+
 def embed_bwd_ref(tok, dout, vocab, scale):
     """Gradient, sums of absolute values and counts, in 64 bits."""
     d = dout.shape[-1]
@@ -241,6 +248,28 @@ def test_layer_norm_gradient(bd, batch, seqlen, d, vectors, io):
     if vectors == "shared":
         only = [call((True, False)), call((False, True)), call((False, False))]
         assert all(torch.equal(o[0], dx) for o in only) and torch.equal(only[0][1], dw) and torch.equal(only[1][2], db)
+
+
+@pytest.mark.parametrize("d", [5, 700, 2048, 9000])
+def test_layer_norm_keeps_what_is_not_a_number_in_its_row(bd, d):
+    """A row with a NaN or an infinity is NaN; the others, and the gradients of theirs, are what they are without it."""
+    g = gen(d)
+    x = normal(g, 2, 9, d)
+    desc = bd.make_norm_desc(2, 9, d, io="f32")
+
+    def call(x):
+        y, mean, rstd, dx = nans(2, 9, d), nans(2, 9), nans(2, 9), nans(2, 9, d)
+        bd.bimamba_layer_norm(desc, x.cuda(), None, None, y, mean, rstd)
+        bd.bimamba_layer_norm_bwd(desc, x.cuda(), None, mean, rstd, torch.ones(1, 1, d, device="cuda").expand(2, 9, d), dx, None, None, None)
+        return y, mean, dx
+
+    clean, bad = call(x), x.clone()
+    bad[0, 3, d // 2], bad[1, 8, d - 1] = math.nan, math.inf
+    got = call(bad)
+    hit = torch.zeros(2, 9, dtype=torch.bool, device="cuda")
+    hit[0, 3] = hit[1, 8] = True
+    assert bool(torch.isnan(got[0][hit]).all()) and bool(torch.isnan(got[2][hit]).all())
+    assert all(torch.equal(a[~hit], b[~hit]) for a, b in zip(got, clean))
 
 
 def test_layer_norm_gradient_against_differences(bd):
@@ -444,6 +473,21 @@ def test_scores_gradient(bd, batch, seqlen, V, given, kind, io):
     within(out, want, 8 * U32 * size, io)
     bd.bimamba_log_probs_bwd(desc, logits, *args, logits)      # in place of the logits
     assert torch.equal(logits, out)
+
+
+def test_scores_gradient_reads_no_row_without_one(bd):
+    """Rows whose gradients are 0 get zeros whatever their logits, rows of nothing but -inf whatever their gradients."""
+    x = torch.full((1, 4, 3001), float("nan"))
+    x[0, 2:] = -math.inf
+    x[0, 3, 5] = 0.0
+    zero = torch.zeros(1, 4)
+    dlogp = torch.tensor([[3.0, 0.0, 2.0, 1.0]])
+    targets = torch.tensor([[-1, 7, 7, 5]])
+    lse = torch.tensor([[math.nan, math.nan, -math.inf, 0.0]])
+    for dentropy in (None, zero.cuda()):
+        out = nans(1, 4, 3001)
+        bd.bimamba_log_probs_bwd(bd.make_logits_desc(1, 4, 3001, io="f32"), x.cuda(), targets.cuda(), lse.cuda(), zero.cuda(), dlogp.cuda(), dentropy, out)
+        assert torch.equal(out, torch.zeros(1, 4, 3001, device="cuda"))
 
 
 def test_scores_gradient_against_differences(bd):
