@@ -395,8 +395,8 @@ size_t bimamba_log_probs_workspace_bytes(const bimamba_logits_desc* desc);
  *   lse, entropy      what bimamba_log_probs gave (entropy: required with dentropy).
  *   dlogp, dentropy   fp32 [batch, seqlen] contiguous; either may be NULL (0), dlogp is taken as 0 where there is no target.
  *   dlogits           may be the very view of the logits (same pointer and strides): the gradient takes their place.
- * Rows whose two gradients are 0, and rows of nothing but -inf, get zeros and are not read.  (desc's top_k and targets_only are
- * not used.) */
+ * Rows whose two gradients are 0, and rows of nothing but -inf, get zeros and are not read.  With desc's targets_only so do rows
+ * without a target, whose scores are constants, whatever their dentropy (targets must then be given).  (top_k is not used.) */
 int bimamba_log_probs_bwd(const bimamba_logits_desc* desc, const bimamba_tensor* logits, const bimamba_tokens* targets,
                           const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                           const bimamba_tensor* dlogits, void* hip_stream);

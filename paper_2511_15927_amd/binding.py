@@ -435,7 +435,7 @@ def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, c
 
 def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
     """Enqueue the gradient for the logits, given those of logp and of the entropy (float32 [batch, L]; either None).  dlogits may be
-    logits itself."""
+    logits itself.  A descriptor with targets_only: rows without a target get zeros."""
     return _checked((_calls_module or _calls()).log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, _stream(stream)),
                     "bimamba_log_probs_bwd", check)
 

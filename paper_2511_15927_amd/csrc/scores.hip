@@ -321,7 +321,7 @@ struct ScoresBwdArgs {
     long long ids_sb, ids_st;
     const float *lse, *entropy, *dlogp, *dentropy;
     unsigned L, parts, all;   // parts of a row, and of all rows
-    int vocab;
+    int vocab, targets_only;
 };
 template <typename IO, bool kEntropy, bool kPast, int kPiece>
 __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned row, unsigned part)
@@ -334,7 +334,8 @@ __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned
         const long long id = a.ids[b * a.ids_sb + t * a.ids_st];
         if (id >= 0 && id < a.vocab) target = (int)id;
     }
-    const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f, de = kEntropy ? a.dentropy[row] : 0.0f;
+    const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f;
+    const float de = kEntropy && (target >= 0 || !a.targets_only) ? a.dentropy[row] : 0.0f;   // (a row that was not asked for: its scores are constants)
     const float lse = a.lse[row], h = kEntropy ? a.entropy[row] : 0.0f;
     const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t);
     T* const dx = static_cast<T*>(a.dlogits.p) + row_offset(a.dlogits, b, t);
@@ -514,7 +515,7 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* lo
     if (rc) return rc;
     if (!logits || !dlogits) return BIMAMBA_ERR_NULL_POINTER;
     if (d->batch == 0 || d->seqlen == 0) return BIMAMBA_OK;
-    if (!lse || (dlogp && !targets) || (dentropy && !entropy)) return BIMAMBA_ERR_NULL_POINTER;
+    if (!lse || ((dlogp || d->targets_only) && !targets) || (dentropy && !entropy)) return BIMAMBA_ERR_NULL_POINTER;
     const long long rows = (long long)d->batch * d->seqlen;
     const size_t elem = dtype_bytes(d->io_dtype);
     Bytes from, to, ids{0, 0};
@@ -532,7 +533,7 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* lo
     a.logits = row_view(logits), a.dlogits = row_view(dlogits);
     if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
     a.lse = lse, a.entropy = entropy, a.dlogp = dlogp, a.dentropy = dentropy;
-    a.L = d->seqlen, a.vocab = d->vocab;
+    a.L = d->seqlen, a.vocab = d->vocab, a.targets_only = d->targets_only;
     a.parts = (unsigned)((d->vocab + (long long)kGradPart - 1) / kGradPart);
     const unsigned long long all = (unsigned long long)rows * a.parts;
     if (all >= 1ull << 31) return BIMAMBA_ERR_UNSUPPORTED;

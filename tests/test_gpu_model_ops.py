@@ -490,6 +490,28 @@ def test_scores_gradient_reads_no_row_without_one(bd):
         assert torch.equal(out, torch.zeros(1, 4, 3001, device="cuda"))
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 7, 3001, 8200])
+def test_scores_gradient_of_rows_that_were_not_asked_for(bd, V, io):
+    """With targets_only the scores of a row without a target are constants: its gradient is 0 whatever dentropy is, its logits are not
+    read; the other rows get what they get without the flag."""
+    g = gen(V)
+    x = normal(g, 2, 9, V, scale=3.0, io=io)
+    targets = torch.randint(0, V, (2, 9), generator=g)
+    targets[0, ::2], targets[1, 4], targets[1, 7] = -1, V, 2 ** 40
+    has = (targets >= 0) & (targets < V)
+    x[~has] = 40.0
+    dlogp, dentropy = normal(g, 2, 9).cuda(), normal(g, 2, 9).cuda()
+    some, every = (bd.make_logits_desc(2, 9, V, io=io, targets_only=k) for k in (1, 0))
+    out = scores(bd, x.cuda(), targets.cuda(), targets_only=1)
+    want, got = nans(2, 9, V, dtype=TYPES[io]), nans(2, 9, V, dtype=TYPES[io])
+    bd.bimamba_log_probs_bwd(every, x.cuda(), targets.cuda(), out["lse"], out["entropy"], dlogp, dentropy, want)
+    x[~has] = math.nan
+    bd.bimamba_log_probs_bwd(some, x.cuda(), targets.cuda(), out["lse"], out["entropy"], dlogp, dentropy, got)
+    assert torch.equal(got.cpu()[~has], torch.zeros(int((~has).sum()), V, dtype=TYPES[io]))
+    assert torch.equal(got.cpu()[has], want.cpu()[has])
+
+
 def test_scores_gradient_against_differences(bd):
     g = gen(31)
     x, targets = torch.randn(2, 2, 9, generator=g), torch.tensor([[0, 8], [3, -1]])

@@ -149,6 +149,11 @@ def test_log_probs_bwd_refusals():
     assert scores_bwd(seqlen=0) == OK
 
 
+def test_log_probs_bwd_of_targets_only_wants_targets():
+    assert scores_bwd(targets=None, dlogp=None, targets_only=1, dlogits=view(A + 2, 100)) == NULL
+    assert scores_bwd(targets=None, dlogp=None, dlogits=view(A + 2, 100)) == ALIAS      # (without the flag it is the next check that refuses)
+
+
 def test_views_side_by_side_in_one_buffer_do_not_meet():
     """Column slices of one buffer whose rows both step alike are apart, others are not.  (A misaligned pointer elsewhere ends the call
     on the host in either case: the order of the checks tells which was found.)"""
