@@ -355,7 +355,7 @@ size_t bimamba_layer_norm_bwd_workspace_bytes(const bimamba_norm_desc* desc, int
 
 /* Host struct.  0 <= top_k <= 8, top_k <= vocab. */
 typedef struct bimamba_logits_desc {
-    uint32_t struct_size;   /* sizeof(bimamba_logits_desc), checked */
+    uint32_t struct_size;   /* sizeof(bimamba_logits_desc), checked; 28, the size up to `reserved`: one without lse_rest */
     int32_t batch;          /* >= 0 */
     int32_t seqlen;         /* >= 0 */
     int32_t vocab;
@@ -363,6 +363,9 @@ typedef struct bimamba_logits_desc {
     int32_t top_k;          /* alternatives wanted per row */
     int32_t targets_only;   /* 0 or 1: rows without a target are not read (training on masked places); all they get are zeros,
                                and -1 for tokens */
+    int32_t reserved;       /* 0 */
+    float* lse_rest;        /* device, fp32 [batch, seqlen] contiguous, or NULL: what rounding to fp32 left of lse.  bimamba_log_probs
+                               writes it (0 where lse is not finite), bimamba_log_probs_bwd reads it beside lse */
 } bimamba_logits_desc;
 
 /* What is wanted of a call's rows, device pointers, contiguous; NULL: not wanted.
@@ -381,9 +384,9 @@ typedef struct bimamba_scores {
 
 /*
  * Log probabilities of given tokens under softmax(logits), with the entropy and the most probable tokens of every row.
- *   logits   [batch, seqlen, vocab].  -inf (and the type's lowest value) are masks: probability 0.  A row of nothing but -inf has
- *            lse -inf, logp -inf, entropy 0, alternatives 0, 1, ... with -inf.  A NaN or +inf makes a row's values NaN and its
- *            alternatives -1.
+ *   logits   [batch, seqlen, vocab].  -inf is a mask: probability 0; so, beside others, is the type's lowest value, which is a number:
+ *            a row of nothing but it is uniform.  A row of nothing but -inf has lse -inf, logp -inf, entropy 0, alternatives
+ *            0, 1, ... with -inf.  A NaN or +inf makes a row's values NaN and its alternatives -1.
  *   targets  NULL: none (then out->logp must be NULL and targets_only 0).
  *   workspace   at least bimamba_log_probs_workspace_bytes(desc) bytes, 16-byte aligned (may be NULL if 0).
  */
@@ -391,8 +394,10 @@ int bimamba_log_probs(const bimamba_logits_desc* desc, const bimamba_tensor* log
                       const bimamba_scores* out, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t bimamba_log_probs_workspace_bytes(const bimamba_logits_desc* desc);
 
-/* Gradient for the logits: dlogits_v = dlogp * (1[v = target] - p_v) - dentropy * p_v * (log p_v + entropy).
- *   lse, entropy      what bimamba_log_probs gave (entropy: required with dentropy).
+/* Gradient for the logits: dlogits_v = dlogp * (1[v = target] - p_v) - dentropy * p_v * (log p_v + entropy), log p_v = logits_v - lse.
+ *   lse, entropy      what bimamba_log_probs gave (entropy: required with dentropy).  lse is fp32, so without desc's lse_rest every p
+ *                     of a row is off by up to 2^-24 |lse|, relatively; from |lse| of 2^28 on nothing is left of the sum, and a row
+ *                     of equal logits has p = 1 throughout.  With lse_rest p is right whatever the logits' size.
  *   dlogp, dentropy   fp32 [batch, seqlen] contiguous; either may be NULL (0), dlogp is taken as 0 where there is no target.
  *   dlogits           may be the very view of the logits (same pointer and strides): the gradient takes their place.
  * Rows whose two gradients are 0, and rows of nothing but -inf, get zeros and are not read.  With desc's targets_only so do rows

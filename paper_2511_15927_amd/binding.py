@@ -75,7 +75,7 @@ class NormDesc(C.Structure):
 
 class LogitsDesc(C.Structure):
     _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
-        "batch", "seqlen", "vocab", "io_dtype", "top_k", "targets_only")]
+        "batch", "seqlen", "vocab", "io_dtype", "top_k", "targets_only", "reserved")] + [("lse_rest", C.c_void_p)]
 
 
 class Scores(C.Structure):
@@ -426,17 +426,19 @@ def bimamba_log_probs_workspace_bytes(desc):
 
 def bimamba_log_probs(desc, logits, targets, out, workspace=None, stream=None, check=True):
     """Enqueue the log probabilities of targets (int64 [batch, L], or None) under softmax(logits).  out: dict of what is wanted:
-    logp, lse, entropy float32 [batch, L]; top_logp float32 and top_token int64 [batch, L, top_k]."""
+    logp, lse, entropy float32 [batch, L]; lse_rest, of the same kind, is what rounding left of lse (bimamba_log_probs_bwd takes it);
+    top_logp float32 and top_token int64 [batch, L, top_k]."""
     get = out.get
     rc = (_calls_module or _calls()).log_probs(desc, logits, targets, get("logp"), get("lse"), get("entropy"), get("top_logp"), get("top_token"),
-                                               workspace, _stream(stream))
+                                               get("lse_rest"), workspace, _stream(stream))
     return _checked(rc, "bimamba_log_probs", check)
 
 
-def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
+def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=None, check=True, lse_rest=None):
     """Enqueue the gradient for the logits, given those of logp and of the entropy (float32 [batch, L]; either None).  dlogits may be
-    logits itself.  A descriptor with targets_only: rows without a target get zeros."""
-    return _checked((_calls_module or _calls()).log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, _stream(stream)),
+    logits itself.  A descriptor with targets_only: rows without a target get zeros.  Without lse_rest the
+    probabilities are off by up to 2^-24 |lse|, relatively."""
+    return _checked((_calls_module or _calls()).log_probs_bwd(desc, logits, targets, lse, lse_rest, entropy, dlogp, dentropy, dlogits, _stream(stream)),
                     "bimamba_log_probs_bwd", check)
 
 

@@ -2,6 +2,7 @@
 #include "model_ops.h"
 
 #include <cfloat>
+#include <cstddef>
 
 namespace bm {
 
@@ -68,7 +69,7 @@ struct ScoresArgs {
     RowView logits;
     const int64_t* ids;   // or null
     long long ids_sb, ids_st;
-    float *logp, *lse, *entropy, *top_logp;
+    float *logp, *lse, *lse_rest, *entropy, *top_logp;
     int64_t* top_token;
     Stats* part;          // [rows][splits], and the parts' own alternatives [rows][splits][top_k], where a row is split
     Key* part_top;
@@ -87,6 +88,7 @@ __device__ __forceinline__ void store_nothing(const ScoresArgs& a, unsigned row)
 {
     if (a.logp) a.logp[row] = 0.0f;
     if (a.lse) a.lse[row] = 0.0f;
+    if (a.lse_rest) a.lse_rest[row] = 0.0f;
     if (a.entropy) a.entropy[row] = 0.0f;
     for (int k = 0; k < a.top_k; k++) {
         if (a.top_logp) a.top_logp[(long long)row * a.top_k + k] = 0.0f;
@@ -97,7 +99,12 @@ __device__ __forceinline__ void store_stats(const ScoresArgs& a, unsigned row, c
 {
     const float log_s = logf(s.s);   // (-inf for a row of nothing but -inf)
     if (a.logp) a.logp[row] = target < 0 ? 0.0f : s.s == 0.0f ? -INFINITY : (x - s.m) - log_s;
-    if (a.lse) a.lse[row] = s.m + log_s;
+    const float lse = s.m + log_s;
+    if (a.lse) a.lse[row] = lse;
+    if (a.lse_rest) {   // (what the addition rounded away, exactly; all of log S beside a maximum that is large enough)
+        const float added = lse - s.m;
+        a.lse_rest[row] = isfinite(lse) ? (s.m - (lse - added)) + (log_s - added) : 0.0f;
+    }
     if (a.entropy) a.entropy[row] = s.s == 0.0f ? 0.0f : log_s - s.t / s.s;
 }
 __device__ __forceinline__ void store_top(const ScoresArgs& a, unsigned row, int k, const Stats& s, Key key)
@@ -311,7 +318,9 @@ __global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
 
 // ---- gradient ----
 //
-// Elementwise, given lse and the entropy: p = exp(x - lse), dx = dlogp (1[target] - p) - dentropy p (log p + H).  A logit is read and its
+// Elementwise, given lse and the entropy: log p = x - lse, dx = dlogp (1[target] - p) - dentropy p (log p + H).  lse comes in two parts, the
+// fp32 value and what rounding left of it: 2^-24 |lse|, by which every p of the row would be off, relatively (by e^0.001 at logits near
+// 30000; a row of equal logits from 2^28 on, the type's lowest value among them, would have p = 1 throughout).  A logit is read and its
 // gradient written by the same lane, so the gradient may take the logits' place.  16384 rows of 50304 bf16, half of them without a target
 // and so only written: 403 us (2.47 GB, 6.1 TB/s), bound by the bytes.
 constexpr int kGradThreads = 256, kGradPart = kGradThreads * 32;
@@ -319,7 +328,7 @@ struct ScoresBwdArgs {
     RowView logits, dlogits;
     const int64_t* ids;
     long long ids_sb, ids_st;
-    const float *lse, *entropy, *dlogp, *dentropy;
+    const float *lse, *lse_rest, *entropy, *dlogp, *dentropy;   // lse_rest: or null
     unsigned L, parts, all;   // parts of a row, and of all rows
     int vocab, targets_only;
 };
@@ -336,7 +345,7 @@ __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned
     }
     const float dl = target >= 0 && a.dlogp ? a.dlogp[row] : 0.0f;
     const float de = kEntropy && (target >= 0 || !a.targets_only) ? a.dentropy[row] : 0.0f;   // (a row that was not asked for: its scores are constants)
-    const float lse = a.lse[row], h = kEntropy ? a.entropy[row] : 0.0f;
+    const float lse = a.lse[row], rest = a.lse_rest ? a.lse_rest[row] : 0.0f, h = kEntropy ? a.entropy[row] : 0.0f;
     const T* const x = static_cast<const T*>(a.logits.p) + row_offset(a.logits, b, t);
     T* const dx = static_cast<T*>(a.dlogits.p) + row_offset(a.dlogits, b, t);
     const int first = part * kGradPart + threadIdx.x * kPiece;
@@ -359,7 +368,7 @@ __device__ __forceinline__ void scores_bwd_part(const ScoresBwdArgs& a, unsigned
         float f[kPiece];
 #pragma unroll
         for (int i = 0; i < kPiece; i++) {
-            const float d = p[k][i] - lse, e = fast_exp2(d * kLog2e);
+            const float d = (p[k][i] - lse) - rest, e = fast_exp2(d * kLog2e);
             if constexpr (kEntropy) f[i] = -e * (dl + de * (fmaxf(d, kFarBelow) + h));
             else f[i] = -e * dl;
         }
@@ -381,10 +390,14 @@ __global__ __launch_bounds__(kGradThreads) void scores_bwd_kernel(const ScoresBw
 
 namespace {
 
+constexpr size_t kFirstLogitsDesc = offsetof(bimamba_logits_desc, reserved);   // (a descriptor without what lse_rest brought)
+float* lse_rest_of(const bimamba_logits_desc* d) { return d->struct_size == kFirstLogitsDesc ? nullptr : d->lse_rest; }
 int check_logits(const bimamba_logits_desc* d)
 {
     if (!d) return BIMAMBA_ERR_NULL_POINTER;
-    if (d->struct_size != sizeof(bimamba_logits_desc) || d->vocab < 1 || (d->targets_only | 1) != 1) return BIMAMBA_ERR_BAD_SHAPE;
+    if (d->struct_size != kFirstLogitsDesc && d->struct_size != sizeof(bimamba_logits_desc)) return BIMAMBA_ERR_BAD_SHAPE;
+    if (d->struct_size == sizeof(bimamba_logits_desc) && d->reserved != 0) return BIMAMBA_ERR_BAD_SHAPE;
+    if (d->vocab < 1 || (d->targets_only | 1) != 1) return BIMAMBA_ERR_BAD_SHAPE;
     if (d->top_k < 0 || d->top_k > d->vocab) return BIMAMBA_ERR_BAD_SHAPE;
     if (const int rc = check_rows(d->batch, d->seqlen)) return rc;
     if (!known_dtype(d->io_dtype) || d->top_k > kMaxTop || d->vocab > 1 << 30) return BIMAMBA_ERR_UNSUPPORTED;
@@ -473,8 +486,9 @@ int bimamba_log_probs(const bimamba_logits_desc* d, const bimamba_tensor* logits
     if (!logits || !out) return BIMAMBA_ERR_NULL_POINTER;
     if (!targets && (out->logp || d->targets_only)) return BIMAMBA_ERR_NULL_POINTER;
     if ((d->top_k == 0) != (!out->top_logp && !out->top_token)) return BIMAMBA_ERR_BAD_SHAPE;
-    if (!aligned_to(out->logp, 4) || !aligned_to(out->lse, 4) || !aligned_to(out->entropy, 4) || !aligned_to(out->top_logp, 4) ||
-        !aligned_to(out->top_token, 8))
+    float* const lse_rest = lse_rest_of(d);
+    if (!aligned_to(out->logp, 4) || !aligned_to(out->lse, 4) || !aligned_to(lse_rest, 4) || !aligned_to(out->entropy, 4) ||
+        !aligned_to(out->top_logp, 4) || !aligned_to(out->top_token, 8))
         return BIMAMBA_ERR_MISALIGNED;
     if (d->batch == 0 || d->seqlen == 0) return BIMAMBA_OK;
     if (!out->logp && !out->lse && !out->entropy && d->top_k == 0) return BIMAMBA_ERR_NULL_POINTER;
@@ -486,8 +500,8 @@ int bimamba_log_probs(const bimamba_logits_desc* d, const bimamba_tensor* logits
     if ((rc = check_workspace(workspace, workspace_bytes, p.total))) return rc;
     const Bytes written[] = {bytes_of(out->logp, p.rows, 4), bytes_of(out->lse, p.rows, 4), bytes_of(out->entropy, p.rows, 4),
                              bytes_of(out->top_logp, (long long)p.rows * d->top_k, 4), bytes_of(out->top_token, (long long)p.rows * d->top_k, 8),
-                             bytes_of(p.total ? workspace : nullptr, p.total, 1)};
-    for (int i = 0; i < 6; i++) {
+                             bytes_of(p.total ? workspace : nullptr, p.total, 1), bytes_of(lse_rest, p.rows, 4)};
+    for (int i = 0; i < 7; i++) {
         if (meet(written[i], from) || meet(written[i], ids)) return BIMAMBA_ERR_ALIAS;
         for (int j = 0; j < i; j++)
             if (meet(written[i], written[j])) return BIMAMBA_ERR_ALIAS;
@@ -495,7 +509,7 @@ int bimamba_log_probs(const bimamba_logits_desc* d, const bimamba_tensor* logits
     ScoresArgs a{};
     a.logits = row_view(logits);
     if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
-    a.logp = out->logp, a.lse = out->lse, a.entropy = out->entropy, a.top_logp = out->top_logp, a.top_token = out->top_token;
+    a.logp = out->logp, a.lse = out->lse, a.lse_rest = lse_rest, a.entropy = out->entropy, a.top_logp = out->top_logp, a.top_token = out->top_token;
     a.part = static_cast<Stats*>(workspace);
     a.part_top = reinterpret_cast<Key*>(static_cast<char*>(workspace) + p.stats);
     a.rows = p.rows, a.L = d->seqlen, a.vocab = d->vocab, a.top_k = d->top_k;
@@ -522,17 +536,19 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* d, const bimamba_tensor* lo
     if ((rc = check_view(logits, d->batch, d->seqlen, d->vocab, d->io_dtype, false, &from))) return rc;
     if ((rc = check_view(dlogits, d->batch, d->seqlen, d->vocab, d->io_dtype, true, &to))) return rc;
     if (targets && (rc = check_tokens(targets, d->batch, d->seqlen, &ids))) return rc;
-    if (!aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(dlogp, 4) || !aligned_to(dentropy, 4)) return BIMAMBA_ERR_MISALIGNED;
+    const float* const lse_rest = lse_rest_of(d);
+    for (const float* r : {lse, lse_rest, entropy, dlogp, dentropy})
+        if (!aligned_to(r, 4)) return BIMAMBA_ERR_MISALIGNED;
     const bool same = logits->ptr == dlogits->ptr && (d->seqlen == 1 || logits->stride_token == dlogits->stride_token) &&
                       (d->batch == 1 || logits->stride_batch == dlogits->stride_batch);
     if (!same && views_meet(dlogits, d->vocab, to, logits, d->vocab, from, d->batch, elem, elem)) return BIMAMBA_ERR_ALIAS;
     if (meet(to, ids)) return BIMAMBA_ERR_ALIAS;
-    for (const float* r : {lse, entropy, dlogp, dentropy})
+    for (const float* r : {lse, lse_rest, entropy, dlogp, dentropy})
         if (meet(to, bytes_of(r, rows, 4))) return BIMAMBA_ERR_ALIAS;
     ScoresBwdArgs a{};
     a.logits = row_view(logits), a.dlogits = row_view(dlogits);
     if (targets) a.ids = targets->ptr, a.ids_sb = targets->stride_batch, a.ids_st = targets->stride_token;
-    a.lse = lse, a.entropy = entropy, a.dlogp = dlogp, a.dentropy = dentropy;
+    a.lse = lse, a.lse_rest = lse_rest, a.entropy = entropy, a.dlogp = dlogp, a.dentropy = dentropy;
     a.L = d->seqlen, a.vocab = d->vocab, a.targets_only = d->targets_only;
     a.parts = (unsigned)((d->vocab + (long long)kGradPart - 1) / kGradPart);
     const unsigned long long all = (unsigned long long)rows * a.parts;

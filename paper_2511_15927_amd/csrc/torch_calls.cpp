@@ -225,10 +225,10 @@ PyObject* layer_norm_bwd(PyObject* const* a)   // desc, x, weight, mean, rstd, d
     void* const st = r.stream(a[10]);
     return status_of(r, [&] { return bimamba_layer_norm_bwd(&d, &x, w.p, w.stride, mean, rstd, &dy, &dx, dweight, dbias, ws.p, ws.n, st); });
 }
-PyObject* log_probs(PyObject* const* a)   // desc, logits, targets, logp, lse, entropy, top_logp, top_token, workspace, stream
+PyObject* log_probs(PyObject* const* a)   // desc, logits, targets, logp, lse, entropy, top_logp, top_token, lse_rest, workspace, stream
 {
     Reader r;
-    const auto d = r.desc<bimamba_logits_desc>(a[0]);
+    auto d = r.desc<bimamba_logits_desc>(a[0]);
     const auto logits = r.rows(a[1], "logits", d.io_dtype, d.batch, d.seqlen, d.vocab);
     const bool has = a[2] != Py_None;
     const auto targets = has ? r.ids(a[2], "targets", d.batch, d.seqlen) : bimamba_tokens{};
@@ -238,23 +238,25 @@ PyObject* log_probs(PyObject* const* a)   // desc, logits, targets, logp, lse, e
     out.entropy = r.flat(a[5], "entropy", {d.batch, d.seqlen});
     out.top_logp = r.flat(a[6], "top_logp", {d.batch, d.seqlen, d.top_k});
     out.top_token = r.flat<int64_t>(a[7], "top_token", {d.batch, d.seqlen, d.top_k}, at::kLong);
-    const auto ws = r.workspace(a[8]);
-    void* const st = r.stream(a[9]);
+    if (a[8] != Py_None) d.lse_rest = r.flat(a[8], "lse_rest", {d.batch, d.seqlen});
+    const auto ws = r.workspace(a[9]);
+    void* const st = r.stream(a[10]);
     return status_of(r, [&] { return bimamba_log_probs(&d, &logits, has ? &targets : nullptr, &out, ws.p, ws.n, st); });
 }
-PyObject* log_probs_bwd(PyObject* const* a)   // desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream
+PyObject* log_probs_bwd(PyObject* const* a)   // desc, logits, targets, lse, lse_rest, entropy, dlogp, dentropy, dlogits, stream
 {
     Reader r;
-    const auto d = r.desc<bimamba_logits_desc>(a[0]);
+    auto d = r.desc<bimamba_logits_desc>(a[0]);
     const auto logits = r.rows(a[1], "logits", d.io_dtype, d.batch, d.seqlen, d.vocab);
     const bool has = a[2] != Py_None;
     const auto targets = has ? r.ids(a[2], "targets", d.batch, d.seqlen) : bimamba_tokens{};
     const float* const lse = r.flat(a[3], "lse", {d.batch, d.seqlen});
-    const float* const entropy = r.flat(a[4], "entropy", {d.batch, d.seqlen});
-    const float* const dlogp = r.flat(a[5], "dlogp", {d.batch, d.seqlen});
-    const float* const dentropy = r.flat(a[6], "dentropy", {d.batch, d.seqlen});
-    const auto dlogits = r.rows(a[7], "dlogits", d.io_dtype, d.batch, d.seqlen, d.vocab);
-    void* const st = r.stream(a[8]);
+    if (a[4] != Py_None) d.lse_rest = r.flat(a[4], "lse_rest", {d.batch, d.seqlen});
+    const float* const entropy = r.flat(a[5], "entropy", {d.batch, d.seqlen});
+    const float* const dlogp = r.flat(a[6], "dlogp", {d.batch, d.seqlen});
+    const float* const dentropy = r.flat(a[7], "dentropy", {d.batch, d.seqlen});
+    const auto dlogits = r.rows(a[8], "dlogits", d.io_dtype, d.batch, d.seqlen, d.vocab);
+    void* const st = r.stream(a[9]);
     return status_of(r, [&] { return bimamba_log_probs_bwd(&d, &logits, has ? &targets : nullptr, lse, entropy, dlogp, dentropy, &dlogits, st); });
 }
 PyObject* clip_grads(PyObject* const* a)   // the host table's bytes, its copy on the device or None, max_norm, norm, workspace, stream
@@ -282,7 +284,7 @@ PyObject* clip_grads(PyObject* const* a)   // the host table's bytes, its copy o
 
 #define BM_METHOD(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&method<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BM_METHOD(embed, 5),      BM_METHOD(embed_bwd, 6),      BM_METHOD(layer_norm, 8),
-                         BM_METHOD(layer_norm_bwd, 11), BM_METHOD(log_probs, 10), BM_METHOD(log_probs_bwd, 9),
+                         BM_METHOD(layer_norm_bwd, 11), BM_METHOD(log_probs, 11), BM_METHOD(log_probs_bwd, 10),
                          BM_METHOD(clip_grads, 6), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "The library's calls as functions of torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -117,16 +117,17 @@ class _LogProbs(torch.autograd.Function):
     def forward(ctx, logits, targets, want_entropy):
         Bt, L, V = logits.shape
         ctx.desc = bd.make_logits_desc(Bt, L, V, io=NAME[logits.dtype], targets_only=int(not want_entropy))
-        out = {k: torch.empty(Bt, L, device=logits.device) for k in ("logp", "lse") + (("entropy",) if want_entropy else ())}
+        out = {k: torch.empty(Bt, L, device=logits.device) for k in ("logp", "lse", "lse_rest") + (("entropy",) if want_entropy else ())}
         bd.bimamba_log_probs(ctx.desc, logits, targets, out, _bytes(bd.bimamba_log_probs_workspace_bytes(ctx.desc), logits))
-        ctx.save_for_backward(logits, targets, out["lse"], out.get("entropy"))
+        ctx.save_for_backward(logits, targets, out["lse"], out["lse_rest"], out.get("entropy"))
         return out["logp"], out.get("entropy")
 
     @staticmethod
     def backward(ctx, dlogp, dentropy):
-        logits, targets, lse, entropy = ctx.saved_tensors
+        logits, targets, lse, lse_rest, entropy = ctx.saved_tensors
         dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
-        bd.bimamba_log_probs_bwd(ctx.desc, logits, targets, lse, entropy, dlogp.contiguous(), None if entropy is None else dentropy.contiguous(), dlogits)
+        bd.bimamba_log_probs_bwd(ctx.desc, logits, targets, lse, entropy, dlogp.contiguous(), None if entropy is None else dentropy.contiguous(), dlogits,
+                                 lse_rest=lse_rest)
         return dlogits, None, None
 
 

@@ -101,3 +101,60 @@ def test_training_learns_and_filling_ends(dn, io):
     kept = noised != model.mask
     assert torch.equal(filled[kept], tokens[kept])
     assert torch.equal(model.fill(noised, per_step=5), filled)
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["ordinary", "equal", "far up", "far down", "ties far up", "lowest", "half lowest", "nothing"])
+@pytest.mark.parametrize("V", [1, 9, 3001, 32001])
+def test_gradient_of_log_probs_at_large_logits(dn, V, kind, io):
+    """The gradient against the softmax of the logits in 64 bits: what is rounded away of a large log-sum-exp is not missing from the
+    probabilities, and a row of nothing but the type's lowest value is uniform.  p is off, relatively, by what log S (a sum along a chain
+    of V / 256 additions a lane, the lanes, waves and parts) and the differences of logits are rounded by; the entropy by the same twice,
+    times what it is spread over."""
+    gen, t, u = torch.Generator().manual_seed(V), dn.TYPE[io], 2.0 ** -24
+    x = 3 * torch.randn(2, 3, V, generator=gen)
+    low = torch.finfo(t).min
+    if kind == "equal":
+        x = torch.tensor([30000.0, -30000.0, 1e30, 70000.0, -1e6, 300.0]).view(2, 3, 1).expand(2, 3, V)
+    elif kind == "far up":
+        x = x + 30000.0
+    elif kind == "far down":
+        x = x - 1e6
+    elif kind == "ties far up":
+        x = torch.where(torch.arange(V) % 5 == 0, 65536.0, x)
+    elif kind == "lowest":
+        x = torch.full_like(x, low)
+    elif kind == "half lowest":
+        x = torch.where(torch.rand(2, 3, V, generator=gen) < 0.5, low, x)
+    elif kind == "nothing":
+        x = torch.full_like(x, -math.inf)
+    x = x.to(t)
+    targets = torch.randint(0, V, (2, 3), generator=gen)
+    targets[0, 1] = -1
+    dlogp, dentropy = torch.randn(2, 3, generator=gen), torch.randn(2, 3, generator=gen)
+    leaf = x.cuda().requires_grad_()
+    logp, entropy = dn.log_probs(leaf, targets.cuda(), want_entropy=True)
+    got, = torch.autograd.grad((logp * dlogp.cuda()).sum() + (entropy * dentropy.cuda()).sum(), leaf)
+    alone, = torch.autograd.grad((dn.log_probs(leaf, targets.cuda())[0] * dlogp.cuda()).sum(), leaf)
+    if kind == "nothing":
+        assert torch.equal(got, torch.zeros_like(got)) and torch.equal(alone, torch.zeros_like(alone))
+        return
+    d = x.double() - x.double().amax(-1, keepdim=True)
+    log_s = torch.log(torch.exp(d).sum(-1, keepdim=True))
+    lp = d - log_s
+    p = torch.exp(lp)
+    plp = torch.where(p > 0, p * lp, 0.0)
+    H = -plp.sum(-1, keepdim=True)
+    dl, de = torch.where(targets >= 0, dlogp, 0.0).double()[..., None], dentropy.double()[..., None]
+    hit = torch.zeros_like(p).scatter(-1, targets.clamp(min=0)[..., None], 1.0)
+    spread = (torch.exp(d) * d.abs().clamp(max=1e4)).sum(-1, keepdim=True) / torch.exp(log_s)
+    unit = u * (48 + V / 256 + 4 * spread + 4 * log_s)
+    rel = unit + u * (8 + 4 * lp.abs().clamp(max=1e3))
+    first = dl * (hit - p)
+    first_off = dl.abs() * p * rel + 2 * u * dl.abs() * (hit + p)
+    inner = torch.where(p > 0, lp + H, 0.0)
+    both = first - de * p * inner
+    both_off = first_off + de.abs() * p * (inner.abs() * (rel + 4 * u) + rel + unit * (2 + 2 * spread) + 4 * u * (lp.abs().clamp(max=1e3) + H)) + 2 * u * both.abs()
+    for g, r, off in ((got, both, both_off), (alone, first, first_off)):
+        off = off + 1e-37 + (2.0 ** -8 * r.abs() if io == "bf16" else 0.0)
+        g = g.double().cpu()
+        assert bool(((g - r).abs() <= off).all()), float(((g - r).abs() / off).max())

@@ -427,6 +427,31 @@ def test_scores_of_rows_that_are_not_numbers(bd, V, io):
     assert_scores(scores(bd, x.cuda(), targets.cuda(), 4), ref, torch.nan_to_num(spread), V)
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["plain", "masked", "lowest", "large"])
+@pytest.mark.parametrize("batch,seqlen,V", [(1, 1, 1), (2, 3, 7), (2, 4, 4099), (1, 2, 50257), (1, 2, 131072), (300, 4, 300)])
+def test_scores_in_two_parts(bd, batch, seqlen, V, kind, io):
+    """lse and lse_rest together are log sum exp beyond fp32's digits: off by what log S is (a sum along a chain of V / 256 additions a
+    lane, the lanes, waves and parts), however large lse itself.  Neither lse nor anything else changes with it."""
+    g = gen(V + 17)
+    x = logits_of(g, kind, batch, seqlen, V, io)
+    targets = torch.randint(-1, V + 1, (batch, seqlen), generator=g)
+    ref, spread = scores_ref(x, targets, 1)
+    names = ("logp", "lse", "entropy")
+    got = scores(bd, x.cuda(), targets.cuda(), want=names + ("lse_rest",))
+    assert all(torch.equal(got[n], t) for n, t in scores(bd, x.cuda(), targets.cuda(), want=names).items())
+    fine = torch.isfinite(ref["lse"])
+    top = x.double().amax(-1)
+    # (the reference itself takes the maximum apart: far below it, 64 bits hold what is left)
+    log_s = torch.log(torch.exp(x.double() - torch.where(fine, top, 0.0)[..., None]).sum(-1))
+    off = (got["lse"].double().cpu() - top + got["lse_rest"].double().cpu() - log_s)[fine].abs()
+    assert bool((off <= (U32 * (48 + V / 256 + 4 * spread + 4 * log_s))[fine]).all())
+    assert bool((got["lse_rest"].cpu()[~fine] == 0).all())
+    some = scores(bd, x.cuda(), targets.cuda(), targets_only=1, want=("lse", "lse_rest"))
+    has = (targets >= 0) & (targets < V)
+    assert torch.equal(some["lse_rest"].cpu()[has], got["lse_rest"].cpu()[has]) and bool((some["lse_rest"].cpu()[~has] == 0).all())
+
+
 def scores_bwd_ref(x, targets, lse, entropy, dlogp, dentropy):
     """The formula in 64 bits, and the size of its terms."""
     x = x.double()

@@ -154,6 +154,27 @@ def test_log_probs_bwd_of_targets_only_wants_targets():
     assert scores_bwd(targets=None, dlogp=None, dlogits=view(A + 2, 100)) == ALIAS      # (without the flag it is the next check that refuses)
 
 
+def test_log_probs_with_the_rest_of_a_log_sum():
+    """A descriptor that ends before `reserved` is one without it; with it the array is checked like the others."""
+    d = bd.make_logits_desc(2, 10, 100)
+    assert d.struct_size == 40
+    for d.struct_size in (24, 27, 29, 32, 36, 44):
+        assert scores(d) == SHAPE
+    d.struct_size, d.reserved = 40, 1
+    assert scores(d) == SHAPE
+    d.reserved = 0
+    for at, rc in ((1 << 50 | 2, ALIGN), (A, ALIAS), (B + 4, ALIAS), (E, ALIAS)):
+        d.lse_rest = at
+        assert scores(d) == rc, at
+    d.struct_size, d.reserved, d.lse_rest = 28, 1, 2        # (not read)
+    assert scores(d, out=bd.Scores(D, D, None, None, None)) == ALIAS
+    call = lambda: bd.lib().bimamba_log_probs_bwd(ref(d), ref(view(A, 100)), ref(bd.Tokens(B, 10, 1)), Z, D, E, F, ref(view(7 << 40, 100)), None)  # noqa: E731
+    d.struct_size, d.reserved = 40, 0
+    for at, rc in ((1 << 50 | 2, ALIGN), (7 << 40, ALIAS)):
+        d.lse_rest = at
+        assert call() == rc, at
+
+
 def test_views_side_by_side_in_one_buffer_do_not_meet():
     """Column slices of one buffer whose rows both step alike are apart, others are not.  (A misaligned pointer elsewhere ends the call
     on the host in either case: the order of the checks tells which was found.)"""
