@@ -444,7 +444,8 @@ def bimamba_log_probs_bwd(desc, logits, targets, lse, entropy, dlogp, dentropy, 
 
 class GradTable:
     """The tensors of a clipping call, made once: where each gradient lies and where the scaled one goes (to None: in place).  Holds the
-    tensors and the table's copy on the device."""
+    tensors and the table's copy on the device.  It is of these tensors: gradients that a program frees and makes anew (a parameter's .grad
+    after an optimizer's zero_grad()) are others, and want another table."""
 
     def __init__(self, grads, to=None):
         self.grads, self.to = list(grads), list(grads if to is None else to)

@@ -200,7 +200,8 @@ class Denoiser:
         return -(logp / level[:, None]).sum() / noised.numel()
 
     def train_step(self, tokens, gen, lr=0.05, max_norm=1.0):
-        """One step of gradient descent with clipping on clean tokens [batch, L].  Returns the loss and the gradients' norm (on the device)."""
+        """One step of gradient descent with clipping on clean tokens [batch, L].  Returns the loss and the gradients' norm (on the device).
+        Each parameter's .grad is the model's own tensor, the same in every step, and afterwards holds the clipped gradient."""
         params = list(self.params.values())
         if self._clip is None:
             for p in params:
@@ -208,9 +209,14 @@ class Denoiser:
             table = bd.GradTable([p.grad for p in params])
             self._clip = table, torch.empty(1, device=tokens.device), _bytes(bd.bimamba_clip_grads_workspace_bytes(table), tokens)
         table, norm, ws = self._clip
+        for p, g in zip(params, table.grads):
+            p.grad = g   # (what the program has made of it since: freed it, put another in its place)
         torch._foreach_zero_(table.grads)
         loss = self.loss(*self.noised(tokens, gen))
         loss.backward()
+        for (name, p), g in zip(self.params.items(), table.grads):
+            if p.grad is not g:
+                raise RuntimeError("the gradient of %s was replaced within the step" % name)
         bd.bimamba_clip_grads(table, max_norm, norm, ws)
         with torch.no_grad():
             torch._foreach_add_(params, table.grads, alpha=-lr)

@@ -158,3 +158,25 @@ def test_gradient_of_log_probs_at_large_logits(dn, V, kind, io):
         off = off + 1e-37 + (2.0 ** -8 * r.abs() if io == "bf16" else 0.0)
         g = g.double().cpu()
         assert bool(((g - r).abs() <= off).all()), float(((g - r).abs() / off).max())
+
+@pytest.mark.parametrize("how", ["none", "others"])
+def test_a_step_after_the_gradients_were_freed_or_replaced(dn, how):
+    """What zero_grad() of an optimizer does between steps, or a gradient put in place by the program, changes nothing of a step."""
+    model, same = (dn.Denoiser(33, 32, 2, io="f32", seed=3) for _ in range(2))
+    tokens, _ = batch(dn, model, 5)
+    norms = []
+    for k in range(3):
+        for m in (model, same):
+            if m is model and k > 0:
+                for p in m.params.values():
+                    p.grad = None if how == "none" else torch.full_like(p, 7.0)
+            before = {n: p.detach().clone() for n, p in m.params.items()}
+            norms.append(float(m.train_step(tokens, torch.Generator(device="cuda").manual_seed(9 + k), lr=0.5, max_norm=0.01)[1]))
+            moved = math.sqrt(sum(float((p.detach() - before[n]).double().square().sum()) for n, p in m.params.items()))
+            assert norms[-1] > 0.01 and abs(moved - 0.5 * 0.01) < 1e-3 * 0.5 * 0.01 + 1e-6, (k, norms, moved)
+    # (the products are torch's, whose order of sums need not be the same twice: three steps of a loss that is smooth)
+    assert all(abs(a - b) <= 1e-4 * b for a, b in zip(norms[::2], norms[1::2])), norms
+    # gradients that a hook takes away within the step are an error, not a step of nothing
+    model.params["head"].register_post_accumulate_grad_hook(lambda p: setattr(p, "grad", None))
+    with pytest.raises(RuntimeError, match="head"):
+        model.train_step(tokens, torch.Generator(device="cuda").manual_seed(1))
