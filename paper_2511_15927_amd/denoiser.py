@@ -4,7 +4,8 @@
 
 (the paper's eqs. 7-10 without the MLP).  The token table, the norms, the mixers, the log probabilities and the clipping are calls of
 the library, forward and backward; the projections are plain matrix products of torch.  embed(), layer_norm(), mixer() and
-log_probs() take part in autograd and can be used on their own.
+log_probs() take part in autograd and can be used on their own; they have first derivatives only, and a gradient through them that is
+itself differentiated is an error.
 
     python -m paper_2511_15927_amd.denoiser [--steps 200] [--width 256] [--layers 4] [--io bf16]
 
@@ -30,6 +31,26 @@ def _rows(t):
     return t if t.stride(-1) == 1 else t.contiguous()
 
 
+class _FirstOrder(torch.autograd.Function):
+    """Gradients as they are, tied to what they depend on: differentiating them is an error, for the library has no second derivatives."""
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("embed, layer_norm, mixer and log_probs have no second derivatives")
+
+
+def _first_order(grads, *sources):
+    """The gradients that a backward pass returns, given all that they were computed from."""
+    if not torch.is_grad_enabled():   # (it is with create_graph only)
+        return grads
+    at = [k for k, g in enumerate(grads) if g is not None]
+    tied = _FirstOrder.apply(len(at), *(grads[k] for k in at), *(t for t in sources if t is not None))
+    return tuple(tied[at.index(k)] if k in at else None for k in range(len(grads)))
+
+
 class _Embed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, tokens, scale, io):
@@ -45,7 +66,7 @@ class _Embed(torch.autograd.Function):
         tokens, = ctx.saved_tensors
         dtable = torch.empty(ctx.desc.vocab, ctx.desc.d_model, device=dout.device)
         bd.bimamba_embed_bwd(ctx.desc, tokens, _rows(dout), dtable, _bytes(bd.bimamba_embed_bwd_workspace_bytes(ctx.desc), dout))
-        return dtable, None, None, None
+        return _first_order((dtable, None, None, None), dout)
 
 
 def embed(table, tokens, scale=1.0, io=torch.bfloat16):
@@ -69,7 +90,7 @@ class _LayerNorm(torch.autograd.Function):
         dx, dweight, dbias = torch.empty_like(x, memory_format=torch.contiguous_format), *torch.empty(2, *weight.shape, device=x.device)
         ws = _bytes(bd.bimamba_layer_norm_bwd_workspace_bytes(ctx.desc, weight.dim() == 2), x)
         bd.bimamba_layer_norm_bwd(ctx.desc, x, weight, mean, rstd, _rows(dy), dx, dweight, dbias, ws)
-        return dx, dweight, dbias, None
+        return _first_order((dx, dweight, dbias, None), x, weight, dy)
 
 
 def layer_norm(x, weight, bias, eps=1e-5):
@@ -104,7 +125,7 @@ class _Mixer(torch.autograd.Function):
         bd.bimamba_bwd(desc, pf, pb, bd.make_inputs(dict(x=x, z=z, dt=dt, B=B, C=C)), None, bd.make_tensor(_rows(dout)), bd.make_input_grads(grads),
                        None, bd.make_param_grads(dpar[0]), bd.make_param_grads(dpar[1]), _bytes(bd.bimamba_bwd_workspace_bytes(desc), x))
         dB, dC = (grads[k].view(B.shape).to(B.dtype) for k in ("dB", "dC"))
-        return (None, grads["dx"], grads["dz"], grads["ddt"], dB, dC, *(d["d" + k] for d in dpar for k in PARAMS))
+        return _first_order((None, grads["dx"], grads["dz"], grads["ddt"], dB, dC, *(d["d" + k] for d in dpar for k in PARAMS)), x, z, dt, B, C, *params, dout)
 
 
 def mixer(cfg, x, z, dt, B, C, pf, pb):
@@ -128,7 +149,7 @@ class _LogProbs(torch.autograd.Function):
         dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
         bd.bimamba_log_probs_bwd(ctx.desc, logits, targets, lse, entropy, dlogp.contiguous(), None if entropy is None else dentropy.contiguous(), dlogits,
                                  lse_rest=lse_rest)
-        return dlogits, None, None
+        return _first_order((dlogits, None, None), logits, dlogp, dentropy)
 
 
 def log_probs(logits, targets, want_entropy=False):

@@ -102,6 +102,7 @@ def test_training_learns_and_filling_ends(dn, io):
     assert torch.equal(filled[kept], tokens[kept])
     assert torch.equal(model.fill(noised, per_step=5), filled)
 
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["ordinary", "equal", "far up", "far down", "ties far up", "lowest", "half lowest", "nothing"])
 @pytest.mark.parametrize("V", [1, 9, 3001, 32001])
@@ -159,6 +160,7 @@ def test_gradient_of_log_probs_at_large_logits(dn, V, kind, io):
         g = g.double().cpu()
         assert bool(((g - r).abs() <= off).all()), float(((g - r).abs() / off).max())
 
+
 @pytest.mark.parametrize("how", ["none", "others"])
 def test_a_step_after_the_gradients_were_freed_or_replaced(dn, how):
     """What zero_grad() of an optimizer does between steps, or a gradient put in place by the program, changes nothing of a step."""
@@ -180,3 +182,37 @@ def test_a_step_after_the_gradients_were_freed_or_replaced(dn, how):
     model.params["head"].register_post_accumulate_grad_hook(lambda p: setattr(p, "grad", None))
     with pytest.raises(RuntimeError, match="head"):
         model.train_step(tokens, torch.Generator(device="cuda").manual_seed(1))
+
+
+def test_second_derivatives_are_refused(dn):
+    """A gradient taken with create_graph is what it is without, and says so when it is itself differentiated: its terms through these
+    functions are not there.  What does not go through them has its second derivatives."""
+    gen = torch.Generator().manual_seed(5)
+    r = lambda *s: torch.randn(*s, generator=gen).cuda().requires_grad_()  # noqa: E731
+    tokens = torch.randint(0, 7, (2, 5), generator=gen).cuda()
+    cfg = dict(batch=2, seqlen=5, d_inner=8, d_state=16, n_heads=8, n_groups=1, d_conv=4, io="f32", a_kind=dn.bd.A_PER_HEAD_STATE,
+               d_kind=dn.bd.D_PER_CHANNEL, dt_softplus=1, conv_bc=0, combine=dn.bd.COMBINE_ADD)
+    side = lambda: dict(conv_w=r(8, 4), conv_b=r(8), A=(-torch.rand(8, 16, generator=gen)).cuda().requires_grad_(), D=r(8), dt_bias=r(8))  # noqa: E731
+    sides = side(), side()
+    mixed = [r(2, 5, 8) for _ in range(3)] + [r(2, 5, 16) for _ in range(2)]
+    logits = r(2, 5, 7)
+    for n, (leaves, call) in enumerate((([r(7, 12)], lambda t: dn.embed(t, tokens, 2.0, torch.float32)), ([r(2, 5, 12), r(2, 12), r(2, 12)], dn.layer_norm),
+                         (mixed + [p for s in sides for p in s.values()],
+                          lambda *a: dn.mixer(cfg, *a[:5], *(dict(zip(dn.PARAMS, a[5 + 5 * k:10 + 5 * k])) for k in (0, 1)))),
+                         ([logits], lambda x: dn.log_probs(x, tokens)[0]), ([logits], lambda x: sum(dn.log_probs(x, tokens, True))))):
+        other, linear = r(3), {0: 0, 1: 2}.get(n)   # (the place of what no first derivative depends on: a table, a bias)
+        # (the first is linear in what comes out, so that the gradient that comes in is a constant; the leaves' cubes have second derivatives)
+        losses = (lambda: call(*leaves).sum(), lambda: call(*leaves).square().sum())
+        for loss in losses:
+            total = lambda: loss() + sum((t ** 3).sum() for t in leaves) + (other ** 3).sum()  # noqa: E731
+            want = torch.autograd.grad(total(), leaves)
+            got = torch.autograd.grad(total(), leaves + [other], create_graph=True)
+            assert all(torch.equal(a, b) for a, b in zip(want, got))
+            second, = torch.autograd.grad(got[-1].sum(), other, retain_graph=True)
+            assert torch.allclose(second, 6 * other)
+            for k, leaf in enumerate(leaves):
+                if k == linear and loss is losses[0]:   # (nothing is missing: there is none)
+                    assert torch.allclose(torch.autograd.grad(got[k].sum(), leaf, retain_graph=True)[0], 6 * leaf)
+                    continue
+                with pytest.raises(RuntimeError, match="second derivative"):
+                    torch.autograd.grad(got[k].sum(), leaf, retain_graph=True)
