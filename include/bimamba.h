@@ -407,7 +407,8 @@ int bimamba_log_probs_bwd(const bimamba_logits_desc* desc, const bimamba_tensor*
                           const bimamba_tensor* dlogits, void* hip_stream);
 
 /* One gradient tensor of a clipping call: count elements at `from`, contiguous; the scaled ones go to `to`, which is `from`
- * itself or memory apart from every tensor. */
+ * itself or memory apart from it, and in either case apart from what every other entry reads or writes: a tensor that is scaled
+ * in place is listed once. */
 typedef struct bimamba_grad {
     const void* from;
     void* to;
@@ -417,7 +418,8 @@ typedef struct bimamba_grad {
     int32_t reserved;       /* 0 */
 } bimamba_grad;
 
-/* Fills `first` of a host table of n tensors.  BIMAMBA_OK or an error (a table that bimamba_clip_grads would refuse). */
+/* Fills `first` of a host table of n tensors.  BIMAMBA_OK, or an error: a table that bimamba_clip_grads would refuse, or one whose
+ * entries meet (BIMAMBA_ERR_ALIAS; looked at here, once for a table, and not again in each bimamba_clip_grads). */
 int bimamba_clip_layout(bimamba_grad* table, int n);
 
 /*

@@ -188,6 +188,51 @@ int clip_pieces(const bimamba_grad* table, bimamba_grad* fill, int n, long long*
     return BIMAMBA_OK;
 }
 
+Bytes read_of(const bimamba_grad& g) { return bytes_of(g.from, g.count, dtype_bytes(g.dtype)); }
+Bytes written_of(const bimamba_grad& g) { return bytes_of(g.to, g.count, dtype_bytes(g.dtype)); }
+
+// Whether what each entry writes is apart from what all others read or write, entries being fine by themselves.  The numbers of those
+// that are not empty are sorted by where they write, in the table's own `first` (which is filled afterwards): no memory is asked for.
+bool clip_apart(bimamba_grad* table, int n)
+{
+    long long m = 0;
+    for (int i = 0; i < n; i++)
+        if (table[i].count > 0) table[m++].first = i;
+    const auto entry = [&](long long k) -> const bimamba_grad& { return table[table[k].first]; };
+    const auto before = [&](long long k, long long l) { return written_of(entry(k)).lo < written_of(entry(l)).lo; };
+    const auto swap = [&](long long k, long long l) {
+        const int64_t i = table[k].first;
+        table[k].first = table[l].first;
+        table[l].first = i;
+    };
+    const auto sift = [&](long long k, long long size) {   // of a heap whose root writes last
+        for (long long c; (c = 2 * k + 1) < size; k = c) {
+            if (c + 1 < size && before(c, c + 1)) c++;
+            if (!before(k, c)) return;
+            swap(k, c);
+        }
+    };
+    for (long long k = m / 2 - 1; k >= 0; k--) sift(k, m);
+    for (long long size = m - 1; size > 0; size--) {
+        swap(0, size);
+        sift(0, size);
+    }
+    for (long long k = 0; k + 1 < m; k++)
+        if (written_of(entry(k)).hi > written_of(entry(k + 1)).lo) return false;
+    // (what is written is apart now, so the last of it that starts before the end of what an entry reads reaches farthest)
+    for (long long k = 0; k < m; k++) {
+        const Bytes from = read_of(entry(k));
+        long long lo = 0, hi = m;
+        while (lo < hi) {
+            const long long mid = (lo + hi) / 2;
+            if (written_of(entry(mid)).lo < from.hi) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo > 0 && table[lo - 1].first != table[k].first && written_of(entry(lo - 1)).hi > from.lo) return false;
+    }
+    return true;
+}
+
 unsigned clip_groups(long long pieces)
 {
     const long long most = 8ll * cu_count();   // what the chip holds at once
@@ -204,7 +249,9 @@ extern "C" {
 int bimamba_clip_layout(bimamba_grad* table, int n)
 {
     long long pieces;
-    return clip_pieces(table, table, n, &pieces);
+    const int rc = clip_pieces(table, table, n, &pieces);
+    if (rc) return rc;
+    return clip_apart(table, n) ? clip_pieces(table, table, n, &pieces) : BIMAMBA_ERR_ALIAS;
 }
 
 size_t bimamba_clip_grads_workspace_bytes(const bimamba_grad* table, int n)
@@ -224,6 +271,13 @@ int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, 
     if (!aligned_to(table_dev, 8) || !aligned_to(norm, 4)) return BIMAMBA_ERR_MISALIGNED;
     const unsigned groups = clip_groups(pieces);
     if ((rc = check_workspace(workspace, workspace_bytes, groups * sizeof(double)))) return rc;
+    const Bytes value = bytes_of(norm, 1, 4), ws = bytes_of(workspace, groups, sizeof(double)), dev = bytes_of(table_dev, n, sizeof(bimamba_grad));
+    if (meet(value, ws) || meet(value, dev) || meet(ws, dev)) return BIMAMBA_ERR_ALIAS;
+    for (int i = 0; i < n; i++) {
+        if (table[i].count == 0) continue;
+        const Bytes from = read_of(table[i]), to = written_of(table[i]);
+        if (meet(value, from) || meet(value, to) || meet(ws, from) || meet(ws, to) || meet(dev, to)) return BIMAMBA_ERR_ALIAS;
+    }
     const long long past = past_caches(2.0 * bytes) && bytes > kKept ? (long long)((double)pieces * (bytes - kKept) / bytes) : 0;
     const ClipArgs a{static_cast<const bimamba_grad*>(table_dev), pieces, past, n, max_norm, norm, static_cast<double*>(workspace)};
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);

@@ -57,7 +57,6 @@ def workspace(n):
 
 # ---- token table ----
 
-
 @pytest.mark.parametrize("table", ["f32", "bf16"])
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("batch,seqlen,d,vocab,extra", [
@@ -614,7 +613,6 @@ def test_clip_leaves_gradients_of_a_norm_that_is_not_finite(bd, value):
 
 
 # ---- all of them ----
-
 
 def test_rows_far_apart(bd):
     """Rows more than 2^31 elements apart: offsets pass 32 bits."""

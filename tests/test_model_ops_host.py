@@ -216,6 +216,49 @@ def test_clip_refusals():
     assert L.bimamba_clip_layout(t, n) == OK
 
 
+def test_clip_refuses_tensors_that_meet():
+    """What one entry writes must be apart from what every other entry reads or writes: two workgroups would race on it."""
+    L = bd.lib()
+    KB = 1 << 10
+
+    def layout(*entries):
+        return L.bimamba_clip_layout(*grads(*[(f, t, n, 0, k, 0) for f, t, n, k in entries]))
+    f32, bf16 = bd.F32, bd.BF16
+    apart = [(A + k * KB, A + k * KB, 256, f32) for k in (3, 0, 2, 1)]                      # in place, side by side, in any order
+    assert layout(*apart) == OK and layout(*apart, (Z, A + 4 * KB, 100, bf16)) == OK
+    assert layout((A, A, 5, f32), (A, A, 5, f32)) == ALIAS                                  # a tensor twice
+    assert layout((A, A, 5, f32), (Z, Z, 5, f32), (A + 16, A + 16, 5, f32)) == ALIAS        # its last value once more
+    assert layout((A, A, 5, f32), (Z, Z, 5, f32), (A + 20, A + 20, 5, f32)) == OK
+    assert layout((A, B, 5, f32), (Z, B, 5, f32)) == ALIAS and layout((A, B, 5, f32), (Z, B + 18, 1, bf16)) == ALIAS   # one place for two
+    assert layout((A, B, 5, f32), (B, Z, 5, f32)) == ALIAS and layout((B, Z, 5, f32), (A, B, 5, f32)) == ALIAS         # crosswise
+    assert layout((A, B, 5, f32), (B, A, 5, f32)) == ALIAS and layout((A, B, 5, f32), (B + 16, D, 1 << 20, f32)) == ALIAS
+    assert layout((B - KB, Z, KB, f32), *[(D, B + k * KB, 5, f32) for k in range(9)]) == ALIAS                         # the first of many
+    assert layout((B + KB // 2, Z, KB, f32), *[(D, B + k * KB, 5, f32) for k in range(9)]) == ALIAS                    # in the midst of them
+    assert layout((B + 20, Z, 251, f32), *[(D, B + k * KB, 5, f32) for k in range(9)]) == OK                           # between two
+    assert layout((A, B, 5, f32), (A, Z, 5, f32)) == OK                                     # read twice, scaled to two places
+    assert layout((A, A, 5, f32), (A, A, 0, f32), (A + 4, None, 0, f32), (None, A + 8, 0, bf16)) == OK                 # (empty ones are nowhere)
+    many = [(A + k * KB, A + k * KB, 256, f32) for k in range(1000)]
+    t, n = grads(*[(f, to, c, 0, k, 0) for f, to, c, k in many])
+    assert L.bimamba_clip_layout(t, n) == OK and [g.first for g in t] == list(range(n))
+    for at in (0, 500, 999):
+        assert layout(*many[:at], (A + 700 * KB + 4, Z, 1, f32), *many[at:]) == ALIAS
+        assert layout(*many[:at], (Z, A + 700 * KB + 1020, 1, f32), *many[at:]) == ALIAS
+
+
+def test_clip_refuses_what_it_writes_on_its_tensors():
+    L = bd.lib()
+    t, n = grads((A, B, 10000, 0, bd.F32, 0), (Z, Z, 5, 0, bd.BF16, 0), (None, None, 0, 0, 0, 0))
+    assert L.bimamba_clip_layout(t, n) == OK
+    call = lambda dev=D, norm=E, ws=F: L.bimamba_clip_grads(t, n, dev, 1.0, norm, ws, 1 << 20, None)  # noqa: E731
+    for on in (A, A + 39996, B, B + 39996, Z + 8):
+        assert call(norm=on) == ALIAS, on
+    for on in (A, B + 39984, Z, B - 16):
+        assert call(ws=on) == ALIAS, on
+    for on in (B, B + 39992, Z):
+        assert call(dev=on) == ALIAS, on
+    assert call(norm=F) == ALIAS and call(norm=D + 100) == ALIAS and call(ws=D) == ALIAS and call(ws=D - 16) == ALIAS
+
+
 def test_the_binding_checks_tensors_against_the_descriptor():
     """Host tensors, other shapes and types, descriptors of another call and what is no tensor never reach the library."""
     x = torch.zeros(2, 10, 64, dtype=torch.bfloat16)
