@@ -222,7 +222,7 @@ class Denoiser:
 
     def train_step(self, tokens, gen, lr=0.05, max_norm=1.0):
         """One step of gradient descent with clipping on clean tokens [batch, L].  Returns the loss and the gradients' norm (on the device).
-        Each parameter's .grad is the model's own tensor, the same in every step, and afterwards holds the clipped gradient."""
+        Where the norm is not finite the parameters stay as they are.  Each parameter's .grad is the model's own tensor, the same in every step, and afterwards holds the clipped gradient."""
         params = list(self.params.values())
         if self._clip is None:
             for p in params:
@@ -239,8 +239,9 @@ class Denoiser:
             if p.grad is not g:
                 raise RuntimeError("the gradient of %s was replaced within the step" % name)
         bd.bimamba_clip_grads(table, max_norm, norm, ws)
-        with torch.no_grad():
-            torch._foreach_add_(params, table.grads, alpha=-lr)
+        with torch.no_grad():   # (a norm that is not finite: nothing moves; told on the device, so that nothing is waited for)
+            torch._fused_sgd_(params, table.grads, [], weight_decay=0.0, momentum=0.0, lr=lr, dampening=0.0, nesterov=False, maximize=False,
+                              is_first_step=False, found_inf=(~torch.isfinite(norm)).float())
         return loss.detach(), norm
 
     @torch.no_grad()

@@ -216,3 +216,22 @@ def test_second_derivatives_are_refused(dn):
                     continue
                 with pytest.raises(RuntimeError, match="second derivative"):
                     torch.autograd.grad(got[k].sum(), leaf, retain_graph=True)
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_a_step_whose_norm_is_not_finite_leaves_the_parameters(dn, value):
+    model = dn.Denoiser(33, 32, 2, io="f32", seed=3)
+    tokens, _ = batch(dn, model, 5)
+    step = lambda seed: model.train_step(tokens, torch.Generator(device="cuda").manual_seed(seed), lr=0.5, max_norm=0.01)  # noqa: E731
+    step(1)
+    weight = model.params["0.in"]
+    with torch.no_grad():
+        kept = float(weight[3, 5])
+        weight[3, 5] = value
+    before = {k: p.detach().clone() for k, p in model.params.items()}
+    assert not math.isfinite(float(step(2)[1]))
+    assert all(torch.equal(p.detach().view(torch.int32), before[k].view(torch.int32)) for k, p in model.params.items())
+    with torch.no_grad():
+        weight[3, 5] = kept
+    assert math.isfinite(float(step(3)[1])) and not torch.equal(weight, before["0.in"])
+    assert all(bool(torch.isfinite(p).all()) for p in model.params.values())
