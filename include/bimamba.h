@@ -290,10 +290,11 @@ int bimamba_time_chunks(const bimamba_desc* desc);
 /* ---- What stands around the mixers of a denoiser: token table, layer norm, log probabilities, clipped gradients ----
  *
  * The calls below share the rules above (host validation, caller's memory and stream, nothing allocated or kept) and these:
- * rows are (batch, token) pairs, batch * seqlen < 2^31; views read have any non-negative strides (0 repeats a row), rows of a
- * view written must lie apart from each other and from everything read (BIMAMBA_ERR_ALIAS), but where a call allows the very
- * same view; all sums, statistics and parameter gradients are fp32 or wider and formed in a fixed order: the same inputs give
- * the same bits.  Activations need be aligned to their element only.  No call records a memset node. */
+ * rows are (batch, token) pairs, batch * seqlen < 2^31 or what a call states (beyond it BIMAMBA_ERR_UNSUPPORTED); views read have
+ * any non-negative strides (0 repeats a row), rows of a view written must lie apart from each other and from everything read
+ * (BIMAMBA_ERR_ALIAS), but where a call allows the very same view; all sums, statistics and parameter gradients are fp32 or
+ * wider and formed in a fixed order: the same inputs give the same bits.  Activations need be aligned to their element only.
+ * No call records a memset node. */
 
 /* Token ids [batch, seqlen] in device memory: id (b, t) at ptr + b*stride_batch + t*stride_token, 8-byte aligned. */
 typedef struct bimamba_tokens {
@@ -321,6 +322,7 @@ int bimamba_embed(const bimamba_embed_desc* desc, const bimamba_tokens* tokens, 
 
 /* dtable[v, :] = scale * sum of dout[b, t, :] over the places with id v; fp32 [vocab, d_model] contiguous, every row is written
  * (rows of ids that do not occur: zeros).  Ids outside [0, vocab) count nowhere.
+ * ceil(batch * seqlen / 64) * ceil(d_model / 512) < 2^25.
  *   workspace   at least bimamba_embed_bwd_workspace_bytes(desc) bytes, 16-byte aligned. */
 int bimamba_embed_bwd(const bimamba_embed_desc* desc, const bimamba_tokens* tokens, const bimamba_tensor* dout, float* dtable,
                       void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -384,6 +386,7 @@ typedef struct bimamba_scores {
 
 /*
  * Log probabilities of given tokens under softmax(logits), with the entropy and the most probable tokens of every row.
+ * batch * seqlen < 2^24.
  *   logits   [batch, seqlen, vocab].  -inf is a mask: probability 0; so, beside others, is the type's lowest value, which is a number:
  *            a row of nothing but it is uniform.  A row of nothing but -inf has lse -inf, logp -inf, entropy 0, alternatives
  *            0, 1, ... with -inf.  A NaN or +inf makes a row's values NaN and its alternatives -1.
@@ -401,7 +404,8 @@ size_t bimamba_log_probs_workspace_bytes(const bimamba_logits_desc* desc);
  *   dlogp, dentropy   fp32 [batch, seqlen] contiguous; either may be NULL (0), dlogp is taken as 0 where there is no target.
  *   dlogits           may be the very view of the logits (same pointer and strides): the gradient takes their place.
  * Rows whose two gradients are 0, and rows of nothing but -inf, get zeros and are not read.  With desc's targets_only so do rows
- * without a target, whose scores are constants, whatever their dentropy (targets must then be given).  (top_k is not used.) */
+ * without a target, whose scores are constants, whatever their dentropy (targets must then be given).  (top_k is not used.)
+ * batch * seqlen * ceil(vocab / 8192) < 2^31. */
 int bimamba_log_probs_bwd(const bimamba_logits_desc* desc, const bimamba_tensor* logits, const bimamba_tokens* targets,
                           const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                           const bimamba_tensor* dlogits, void* hip_stream);

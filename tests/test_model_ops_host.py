@@ -175,6 +175,17 @@ def test_log_probs_with_the_rest_of_a_log_sum():
         assert call() == rc, at
 
 
+def test_sizes_up_to_the_limits_that_the_header_states():
+    """Below a limit the next check refuses, at it the size does."""
+    for rows, rc in (((1 << 24) - 1, ALIGN), (1 << 24, UNSUPPORTED)):
+        assert scores(batch=1, seqlen=rows, logits=view(A + 1, 100), targets=bd.Tokens(1 << 50, 0, 1)) == rc
+    for seqlen, d, rc in (((1 << 31) - 64, 512, SMALL), ((1 << 31) - 63, 512, UNSUPPORTED), ((1 << 30) - 64, 513, SMALL), ((1 << 30) - 63, 513, UNSUPPORTED),
+                          ((1 << 20) - 64, 1 << 20, SMALL), ((1 << 20) - 63, 1 << 20, UNSUPPORTED)):
+        assert embed_bwd(batch=1, seqlen=seqlen, d_model=d, tok=bd.Tokens(1 << 50, 0, 1), dout=bd.Tensor(B, 0, 0), ws_bytes=16) == rc, (seqlen, d)
+    assert scores_bwd(batch=1, seqlen=1 << 30, vocab=8193, logits=bd.Tensor(A, 0, 0), targets=bd.Tokens(1 << 50, 0, 1), dlogits=view(1 << 52, 8193),
+                      lse=1 << 51, entropy=3 << 50, dlogp=5 << 50, dentropy=6 << 50) == UNSUPPORTED
+
+
 def test_views_side_by_side_in_one_buffer_do_not_meet():
     """Column slices of one buffer whose rows both step alike are apart, others are not.  (A misaligned pointer elsewhere ends the call
     on the host in either case: the order of the checks tells which was found.)"""
