@@ -349,7 +349,7 @@ int bimamba_layer_norm(const bimamba_norm_desc* desc, const bimamba_tensor* x, c
  * dweight = sum of dy * xh and dbias = sum of dy over the rows that share the vector: fp32 [batch, d_model] contiguous, or
  * [d_model] with weight_stride 0; NULL: not wanted.
  *   workspace   at least bimamba_layer_norm_bwd_workspace_bytes(desc, weight_stride != 0) bytes, 16-byte aligned; may be NULL if
- *               neither dweight nor dbias is wanted. */
+ *               that is 0 or neither dweight nor dbias is wanted. */
 int bimamba_layer_norm_bwd(const bimamba_norm_desc* desc, const bimamba_tensor* x, const float* weight, int64_t weight_stride,
                            const float* mean, const float* rstd, const bimamba_tensor* dy, const bimamba_tensor* dx,
                            float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -222,13 +222,14 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(const NormArgs 
 //
 // A row is held as in the forward call.  A group of waves takes `per_group` rows of one batch element after the other and keeps the
 // sums of dy * xh and dy over them in registers; it leaves them in a slot of its own, and a second launch adds the slots of a vector in
-// a fixed order.  What bounds it are the bytes: 65536 rows of 2048 bf16 162 us (5.0 TB/s with the slots), the second launch 6 of them;
+// a fixed order.  Where one workgroup takes all rows of a vector its sums are the gradients, and there is neither slot nor second launch.  What bounds it are the bytes: 65536 rows of 2048 bf16 162 us (5.0 TB/s with the slots), the second launch 6 of them;
 // 3711 rows of 740 fp32 12.8 us, two launches and two rows a wave one after the other.
 struct NormBwdArgs {
     RowView x, dy, dx;
     const float *weight, *mean, *rstd;
     long long weight_stride;
-    float* slots;   // [vectors][workgroups][2][d], or null: neither dweight nor dbias is wanted
+    float *dw, *db;   // sums of a workgroup, null: not wanted; in slots [vectors][workgroups][2][d], or the vectors' gradients themselves
+    long long slot;   // from one workgroup's to the next one's
     NormRows n;
     int d;
 };
@@ -290,25 +291,26 @@ __device__ __forceinline__ void norm_bwd_rows(const NormBwdArgs& a)
             store_piece_of<IO, kPast>(dx, at(k), a.d, f);
         }
     }
-    if (!a.slots) return;
-    float* const slot = a.slots + ((long long)vector * gridDim.x + blockIdx.x) * 2 * a.d;
+    const long long slot = ((long long)vector * gridDim.x + blockIdx.x) * a.slot;
     if constexpr (kWaves > 1) {
 #pragma unroll
         for (int k = 0; k < kPieces; k++) {
-            store_piece_of<IoF32>(slot, at(k), a.d, dw[k]);
-            store_piece_of<IoF32>(slot + a.d, at(k), a.d, db[k]);
+            if (a.dw) store_piece_of<IoF32>(a.dw + slot, at(k), a.d, dw[k]);
+            if (a.db) store_piece_of<IoF32>(a.db + slot, at(k), a.d, db[k]);
         }
     } else {   // four waves' sums of the same channels: one of the two at a time through shared memory
         __shared__ float sum[4][64 * kPieces * kPiece];
 #pragma unroll
         for (int which = 0; which < 2; which++) {
+            float* const to = which ? a.db : a.dw;
+            if (!to) continue;   // (all threads)
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kPieces; k++)
 #pragma unroll
                 for (int i = 0; i < kPiece; i++) sum[wave][(k * 64 + lane) * kPiece + i] = which ? db[k][i] : dw[k][i];
             __syncthreads();
-            for (int c = threadIdx.x; c < a.d; c += 256) slot[which * a.d + c] = (sum[0][c] + sum[1][c]) + (sum[2][c] + sum[3][c]);
+            for (int c = threadIdx.x; c < a.d; c += 256) to[slot + c] = (sum[0][c] + sum[1][c]) + (sum[2][c] + sum[3][c]);
         }
     }
 }
@@ -384,9 +386,9 @@ __global__ __launch_bounds__(256) void norm_long_cols_kernel(const NormBwdArgs a
             db[i] += pd[i];
         }
     }
-    float* const slot = a.slots + ((long long)vector * gridDim.x + blockIdx.x) * 2 * a.d;
-    store_piece_of<IoF32>(slot, at, a.d, dw);
-    store_piece_of<IoF32>(slot + a.d, at, a.d, db);
+    const long long slot = ((long long)vector * gridDim.x + blockIdx.x) * a.slot;
+    if (a.dw) store_piece_of<IoF32>(a.dw + slot, at, a.d, dw);
+    if (a.db) store_piece_of<IoF32>(a.db + slot, at, a.d, db);
 }
 
 // dweight and dbias: the slots of a vector, added up 32 channels to a workgroup, each of its rows of threads a share of the slots.
@@ -496,7 +498,7 @@ void launch_norm_bwd(const NormPlan& p, const NormBwdArgs& a, hipStream_t st)
         case 32 * 8 + 4: hipLaunchKernelGGL((norm_bwd_kernel<IO, 4, 32, kPast>), grid, wg, 0, st, a); break;
         default:
             hipLaunchKernelGGL(norm_bwd_long_kernel<IO>, dim3(long_groups(a.n), p.vectors), dim3(kLongThreads), 0, st, a);
-            if (a.slots)
+            if (a.dw || a.db)
                 hipLaunchKernelGGL(norm_long_cols_kernel<IO>, dim3(p.groups, p.vectors, (a.d + 256 * kPieceOf<IO> - 1) / (256 * kPieceOf<IO>)), wg, 0, st, a);
     }
 }
@@ -555,7 +557,7 @@ size_t bimamba_layer_norm_bwd_workspace_bytes(const bimamba_norm_desc* d, int pe
 {
     if (check_norm(d) || d->batch == 0 || d->seqlen == 0) return 0;
     const NormPlan p = plan_norm(d, per_batch != 0, true);
-    return (size_t)p.groups * p.vectors * 2 * d->d_model * sizeof(float);
+    return p.groups > 1 ? (size_t)p.groups * p.vectors * 2 * d->d_model * sizeof(float) : 0;
 }
 
 int bimamba_layer_norm_bwd(const bimamba_norm_desc* d, const bimamba_tensor* x, const float* weight, int64_t weight_stride,
@@ -596,18 +598,21 @@ int bimamba_layer_norm_bwd(const bimamba_norm_desc* d, const bimamba_tensor* x, 
         }
     }
     if (vectors == 0 || (!rows && !sums)) return BIMAMBA_OK;
+    const bool direct = rows && p.groups == 1;   // (one workgroup a vector)
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
     if (rows) {
+        float* const slots = sums ? static_cast<float*>(workspace) : nullptr;
         const NormBwdArgs a{row_view(x), row_view(dy), row_view(dx), weight, mean, rstd, weight_stride,
-                            sums ? static_cast<float*>(workspace) : nullptr, p.n, d->d_model};
+                            direct ? dweight : slots, direct ? dbias : slots ? slots + d->d_model : nullptr,
+                            (direct ? 1ll : 2ll) * d->d_model, p.n, d->d_model};
         const bool past = past_caches(3.0 * rows * d->d_model * dtype_bytes(d->io_dtype)), bf16 = d->io_dtype == BIMAMBA_BF16;
         if (bf16 && past) launch_norm_bwd<IoBF16, true>(p, a, st);
         else if (bf16) launch_norm_bwd<IoBF16, false>(p, a, st);
         else if (past) launch_norm_bwd<IoF32, true>(p, a, st);
         else launch_norm_bwd<IoF32, false>(p, a, st);
     }
-    if (sums) {   // (no rows: sums of nothing)
+    if (sums && !direct) {   // (no rows: sums of nothing)
         const long long count = rows ? p.groups : 0;
         const NormSumArgs a{static_cast<const float*>(workspace), dweight, dbias, count, d->d_model};
         const dim3 grid((d->d_model + kSumChannels - 1) / kSumChannels, vectors, 2);

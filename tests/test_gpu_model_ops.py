@@ -250,6 +250,35 @@ def test_layer_norm_gradient(bd, batch, seqlen, d, vectors, io):
         assert all(torch.equal(o[0], dx) for o in only) and torch.equal(only[0][1], dw) and torch.equal(only[1][2], db)
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,seqlen,d", [(1, 1, 9000), (1100, 1, 5), (1100, 2, 72), (340, 7, 600), (1030, 9, 1000), (600, 3, 2050), (520, 2, 5000), (260, 3, 8200)])
+def test_layer_norm_gradient_of_a_workgroup_a_vector(bd, batch, seqlen, d, io):
+    """As many vectors as workgroups: their gradients need no workspace, and those that are not wanted are not written."""
+    g = gen(13 * d + batch)
+    x, w, _ = norm_inputs(g, batch, seqlen, d, "batch", io, 1.0)
+    dy = normal(g, batch, seqlen, d, io=io)
+    _, mean, rstd, _, _, _ = norm_ref(x, w, None, 1e-5)
+    mean, rstd = mean[..., 0].float(), rstd[..., 0].float()
+    desc = bd.make_norm_desc(batch, seqlen, d, io=io)
+    assert bd.bimamba_layer_norm_bwd_workspace_bytes(desc, True) == 0
+    args = x.cuda(), w.cuda(), mean.cuda(), rstd.cuda(), dy.cuda()
+
+    def call(want):
+        dx, around = torch.empty_like(args[0]), nans(2, 2 + batch, d)   # (with a row before and after that stays as it is)
+        dw, db = (around[k, 1:-1] if want[k] else None for k in range(2))
+        bd.bimamba_layer_norm_bwd(desc, *args, dx, dw, db, None)
+        assert all(bool(torch.isnan(a[::batch + 1] if k else a).all()) for a, k in zip(around, want))
+        return dx, dw, db
+
+    dx, dw, db = call((True, True))
+    rdx, size, tw, tb = norm_bwd_ref(x, w, mean, rstd, dy)
+    within(dx, rdx, (64 + d / 1024) * U32 * size, io)
+    within(dw, tw.sum(1), (seqlen + 12) * U32 * tw.abs().sum(1))
+    within(db, tb.sum(1), (seqlen + 8) * U32 * tb.abs().sum(1))
+    for want in ((True, False), (False, True), (False, False)):
+        assert all(a is None or torch.equal(a, b) for a, b in zip(call(want), (dx, dw, db)))
+
+
 @pytest.mark.parametrize("d", [5, 700, 2048, 9000])
 def test_layer_norm_keeps_what_is_not_a_number_in_its_row(bd, d):
     """A row with a NaN or an infinity is NaN; the others, and the gradients of theirs, are what they are without it."""

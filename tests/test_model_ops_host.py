@@ -306,3 +306,13 @@ def test_workspaces_stay_small():
     assert bd.bimamba_layer_norm_bwd_workspace_bytes(bd.make_norm_desc(8, 8192, 2048), True) < 64 << 20
     assert bd.bimamba_layer_norm_bwd_workspace_bytes(bd.make_norm_desc(65535, 1, 2048), False) < 64 << 20
     assert bd.bimamba_log_probs_workspace_bytes(bd.make_logits_desc(8, 8192, 50304, top_k=8)) == 0
+
+
+def test_workspaces_stay_small_with_vectors_of_their_own():
+    """Slots for as many workgroups as the chip holds, however many batch elements have vectors of their own."""
+    need = lambda b, L, d: bd.bimamba_layer_norm_bwd_workspace_bytes(bd.make_norm_desc(b, L, d), True)  # noqa: E731
+    assert need(65535, 1, 2048) == 0 and need(65535, 3, 64) == 0 and need(2000, 40, 1000) == 0
+    assert need(1000, 100, 2048) < 64 << 20 and need(300, 7, 2048) < 64 << 20
+    # what goes without one is still refused where the results are wrong
+    one = dict(batch=2000, seqlen=1, x=view(A, 64, L=1), dy=view(E, 64, L=1), dx=view(F, 64, L=1), stride=64, ws=None)
+    assert norm_bwd(**dict(one, dw=8 << 40)) == ALIAS and norm_bwd(**dict(one, db=E)) == ALIAS and norm_bwd(**dict(one, dw=B + 64)) == ALIAS
