@@ -1,5 +1,6 @@
 """Compile the HIP library for gfx950 into paper_2511_15927_amd/libbimamba.so (in-tree, hipcc), and _calls.so beside it (g++)."""
 import os
+import re
 import subprocess
 from concurrent.futures import ThreadPoolExecutor
 
@@ -32,14 +33,22 @@ def sources():
     return [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC))] + [os.path.join(ROOT, "include", "bimamba.h")]
 
 
-def newest_dep(src, newest_all):
-    """Modification time an object must beat: its source and the headers that source includes."""
-    text = open(src).read()
-    deps = [src, os.path.join(ROOT, "include", "bimamba.h")]
-    for h in ("kernels.h", "short_kernels.h", "launch.h", "ssd_kernels.h", "ssd_wide.h", "ssd_block.h", "bwd_kernels.h", "row_kernels.h", "stack_kernels.h", "stack_quad.h", "model_ops.h"):
-        if h in text or (h == "kernels.h"):
-            deps.append(os.path.join(CSRC, h))
-    return max(os.path.getmtime(p) for p in deps)
+def includes_of(src):
+    """A source and all that it includes, headers through headers among them."""
+    found, todo = set(), [src]
+    while todo:
+        path = todo.pop()
+        if path in found:
+            continue
+        found.add(path)
+        for name in re.findall(r'^#include "([^"]+)"', open(path).read(), re.M):
+            todo += [p for p in (os.path.join(CSRC, name), os.path.join(ROOT, "include", name)) if os.path.exists(p)]
+    return found
+
+
+def newest_dep(src):
+    """Modification time that an object must beat."""
+    return max(os.path.getmtime(p) for p in includes_of(src))
 
 
 def compile_calls(force):
@@ -49,7 +58,7 @@ def compile_calls(force):
     import torch
     from torch.utils import cpp_extension
     src, obj = os.path.join(CSRC, "torch_calls.cpp"), os.path.join(OBJ, "torch_calls.o")
-    if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src), os.path.getmtime(os.path.join(ROOT, "include", "bimamba.h"))):
+    if not force and os.path.exists(obj) and os.path.getmtime(obj) >= newest_dep(src):
         return ""
     includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
     return _run(["g++", "-O2", "-std=c++17", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] +
@@ -81,8 +90,7 @@ def build(force: bool = True, jobs: int = 8):
     units.append((os.path.join(CSRC, "stack_inst.hip"), os.path.join(OBJ, "stack_inst.o"), []))
     for name in ("embed", "norm", "scores", "clip"):
         units.append((os.path.join(CSRC, name + ".hip"), os.path.join(OBJ, name + ".o"), []))
-    newest = max(os.path.getmtime(p) for p in sources())
-    todo = [u for u in units if force or not os.path.exists(u[1]) or os.path.getmtime(u[1]) < newest_dep(u[0], newest)]
+    todo = [u for u in units if force or not os.path.exists(u[1]) or os.path.getmtime(u[1]) < newest_dep(u[0])]
     cmds = [["hipcc"] + FLAGS + extra + ["-c", src, "-o", obj] for src, obj, extra in todo]
     with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds) + 1))) as ex:
         calls = ex.submit(compile_calls, force)
