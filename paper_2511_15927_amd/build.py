@@ -94,8 +94,9 @@ def build(force: bool = True, jobs: int = 8):
     cmds = [["hipcc"] + FLAGS + extra + ["-c", src, "-o", obj] for src, obj, extra in todo]
     with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds) + 1))) as ex:
         calls = ex.submit(compile_calls, force)
-        logs = list(ex.map(_run, cmds)) + [calls.result()]
+        logs = list(ex.map(_run, cmds))
     logs.append(_run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [u[1] for u in units]))
+    logs.append(calls.result())   # (the library is there by now: it needs neither g++ nor the headers of Python and torch)
     logs.append(link_calls())
     out = "\n".join(l for l in logs if l.strip())
     if out.strip():

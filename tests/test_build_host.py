@@ -1,6 +1,8 @@
 """CPU-only checks of what the build rebuilds and of what it needs for what."""
 import os
 
+import pytest
+
 from paper_2511_15927_amd import build
 
 
@@ -16,3 +18,18 @@ def test_an_object_is_as_old_as_all_that_its_source_includes():
     # every header is reached by some source
     every = set().union(*(names(f) for f in os.listdir(build.CSRC) if not f.endswith(".h")))
     assert {f for f in os.listdir(build.CSRC) if f.endswith(".h")} <= every
+
+
+def test_the_library_is_linked_without_what_the_extension_module_needs(monkeypatch, tmp_path):
+    """A machine without g++ or the headers of Python and torch gets the C library, and an error that names what is missing."""
+    ran = []
+    monkeypatch.setattr(build, "_run", lambda cmd: ran.append(cmd) or "")
+    monkeypatch.setattr(build, "OBJ", str(tmp_path))
+
+    def missing(force):
+        raise RuntimeError("no torch headers")
+    monkeypatch.setattr(build, "compile_calls", missing)
+    with pytest.raises(RuntimeError, match="no torch headers"):
+        build.build(force=True)
+    assert all(cmd[0] == "hipcc" for cmd in ran)
+    assert sum("-shared" in cmd and build.LIB in cmd for cmd in ran) == 1 and "-shared" in ran[-1]
