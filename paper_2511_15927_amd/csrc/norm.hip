@@ -480,7 +480,7 @@ void launch_norm(const NormPlan& p, const NormArgs& a, hipStream_t st)
         case 8 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 8, kPast>), grid, wg, 0, st, a); break;
         case 16 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 16, kPast>), grid, wg, 0, st, a); break;
         case 32 * 8 + 1: hipLaunchKernelGGL((norm_kernel<IO, 1, 32, kPast>), grid, wg, 0, st, a); break;
-        case 8 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 8, kPast>), grid, wg, 0, st, a); break;
+        case 8 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 8, false>), grid, wg, 0, st, a); break;   // (few rows, of 2048 at most: 16 MB)
         case 16 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 16, kPast>), grid, wg, 0, st, a); break;
         case 32 * 8 + 4: hipLaunchKernelGGL((norm_kernel<IO, 4, 32, kPast>), grid, wg, 0, st, a); break;
         default: hipLaunchKernelGGL(norm_long_kernel<IO>, dim3(long_groups(a.n), p.vectors), dim3(kLongThreads), 0, st, a);

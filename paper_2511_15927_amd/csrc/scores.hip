@@ -272,7 +272,7 @@ __device__ __forceinline__ void scores_row(const ScoresArgs& a)
 template <typename IO, bool kEntropy, bool kTop, int kThreads, bool kPast>
 __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresArgs a)
 {
-    if constexpr (kThreads == kManyRowsThreads) {   // (rows shorter than a piece: a logit a lane)
+    if constexpr (kThreads == kManyRowsThreads && !kPast) {   // (rows shorter than a piece, a logit a lane: 2^24 of them are less than the caches hold)
         if (a.vocab < kPieceOf<IO>) return scores_row<IO, kEntropy, kTop, 1, kThreads, kPast>(a);
     }
     scores_row<IO, kEntropy, kTop, kPieceOf<IO>, kThreads, kPast>(a);
