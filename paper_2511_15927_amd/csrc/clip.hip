@@ -7,7 +7,7 @@ namespace bm {
 // search.  Two launches: the squares' sums, 64 bits each, one a workgroup; then every workgroup adds up all of these in the same
 // order, which gives it the norm, and scales its pieces.  What bounds it are the bytes: two reads, one write.  The second launch
 // goes from the last piece to the first, so that it starts with what the first has left in the caches; where the gradients are larger
-// than these, the first reads all but the last 192 MB past them, and the second goes past them altogether.  604 M values, 1.2 GB: 611 us
+// than these, the first reads all but the last 192 MB past them, and the second goes past them altogether.  609 M values, 1.2 GB: 609 us
 // (each workgroup a run of pieces of its own, walked backwards, everything through the caches: 761; the pieces in turn 692; stores past
 // the caches 640; nothing kept for the second launch 629).  40 tensors, 94208 values: 7.7 us, two launches and their chains of loads.
 constexpr int kClipThreads = 256, kClipPiece = 8192;

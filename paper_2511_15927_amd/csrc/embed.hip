@@ -58,8 +58,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a)
 // place counting by binary search what precedes it in the other seven.  It moves 8 bytes a place and occupies few CUs for 10 to 20 us;
 // meanwhile the other workgroups of its launches clear the table, half of it each, so that only rows of ids that occur are left to
 // write.  (Looking up which rows are absent instead, after the sort, writes those rows once and not twice, but hides nothing.)
-// What bounds it are the bytes, 412 MB of zeros, 135 MB of dout and 53 MB of rows at 8 x 4096 tokens of 2048 channels and 50304 ids: 129 us
-// (sort 37 and merge 38 with the clearing in them, sums 46, join 7; 4.6 TB/s); for few tokens the four launches.
+// What bounds it are the bytes, 412 MB of zeros, 135 MB of dout and 53 MB of rows at 8 x 4096 tokens of 2048 channels and 50304 ids: 126 us
+// (sort 38 and merge 36 with the clearing in them, sums 46, join 7; 4.8 TB/s); for few tokens the four launches.
 
 // Places sorted by one workgroup, 2048 or 4096 by the bits that the ids leave of a 32-bit key, four neighbouring ones a lane.
 constexpr int kChunkBits = 11, kLargeChunkBits = 12, kSortKeys = 4;

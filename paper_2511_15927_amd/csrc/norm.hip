@@ -8,7 +8,7 @@ namespace bm {
 // four waves share a row each takes both of its own part, and one exchange joins them (the squares around the common mean are the
 // parts' own plus what their means are off by).  A wave takes many rows one after the other, the next one on its way, with weight and
 // bias in registers: read again for each row they would be twice the row's own bytes.  What bounds it are the bytes: 65536 rows of
-// 2048 bf16 96 us (5.6 TB/s).  Few rows, one to four waves each: 512 rows 4.2 us, the launch and one load's time.
+// 2048 bf16 95 us (5.6 TB/s).  Few rows, one to four waves each: 512 rows 4.2 us, the launch and one load's time.
 struct NormRows {
     unsigned L, rows;      // tokens of a batch element; rows that share a vector: all, or (per_batch) those of a batch element
     unsigned per_group;    // rows that a group of waves takes, one after the other
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(const NormArgs 
 //
 // A row is held as in the forward call.  A group of waves takes `per_group` rows of one batch element after the other and keeps the
 // sums of dy * xh and dy over them in registers; it leaves them in a slot of its own, and a second launch adds the slots of a vector in
-// a fixed order.  Where one workgroup takes all rows of a vector its sums are the gradients, and there is neither slot nor second launch.  What bounds it are the bytes: 65536 rows of 2048 bf16 162 us (5.0 TB/s with the slots), the second launch 6 of them;
+// a fixed order.  Where one workgroup takes all rows of a vector its sums are the gradients, and there is neither slot nor second launch.  What bounds it are the bytes: 65536 rows of 2048 bf16 156 to 162 us (5.2 to 5.0 TB/s with the slots), the second launch 6 of them;
 // 3711 rows of 740 fp32 12.8 us, two launches and two rows a wave one after the other.
 struct NormBwdArgs {
     RowView x, dy, dx;

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64) void scores_join_kernel(const ScoresArgs a)
 // fp32 value and what rounding left of it: 2^-24 |lse|, by which every p of the row would be off, relatively (by e^0.001 at logits near
 // 30000; a row of equal logits from 2^28 on, the type's lowest value among them, would have p = 1 throughout).  A logit is read and its
 // gradient written by the same lane, so the gradient may take the logits' place.  16384 rows of 50304 bf16, half of them without a target
-// and so only written: 403 us (2.47 GB, 6.1 TB/s), bound by the bytes.
+// and so only written: 402 to 425 us (2.47 GB, 6.1 to 5.8 TB/s), bound by the bytes.
 constexpr int kGradThreads = 256, kGradPart = kGradThreads * 32;
 struct ScoresBwdArgs {
     RowView logits, dlogits;

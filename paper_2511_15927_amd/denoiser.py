@@ -246,8 +246,8 @@ class Denoiser:
 
     @torch.no_grad()
     def fill(self, tokens, per_step=8):
-        """Masked places of tokens [batch, L] are filled, in every step the `per_step` of each sequence whose most probable token is the
-        most probable, and of those with equal ones the least uncertain."""
+        """Masked places of tokens [batch, L] are filled, in every step the `per_step` of each sequence whose most probable token has the
+        largest log probability, less a millionth of the entropy: of equal ones the least uncertain come first."""
         tokens = tokens.clone()
         Bt, L = tokens.shape
         desc = bd.make_logits_desc(Bt, L, self.vocab, io=NAME[self.io], top_k=1)
