@@ -439,6 +439,138 @@ int bimamba_clip_grads(const bimamba_grad* table, int n, const void* table_dev, 
                        size_t workspace_bytes, void* hip_stream);
 size_t bimamba_clip_grads_workspace_bytes(const bimamba_grad* table, int n);
 
+/* ---- The block of a gated linear recurrence: the recurrence, the norm of its gated output, dropout into the residual stream ----
+ *
+ * The calls below keep the rules of the section above. */
+
+enum bimamba_gate {
+    BIMAMBA_GATE_LOG = 0,      /* g is the logarithm of the factor: a = exp(min(g, 0)), u = x */
+    BIMAMBA_GATE_SIGMOID = 1   /* a = sigmoid(g + bias), u = (1 - a) * x */
+};
+
+/* Host struct. */
+typedef struct bimamba_recurrence_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_recurrence_desc), checked */
+    int32_t batch;          /* >= 0, <= 65535 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t d_inner;        /* <= 65536 */
+    int32_t io_dtype;       /* bimamba_dtype of x, g, add, y and of dy, dx, dg */
+    int32_t gate;           /* bimamba_gate */
+    int32_t reverse;        /* 0: tokens 0, 1, ...; 1: from a sequence's last token to its first */
+} bimamba_recurrence_desc;
+
+#define BIMAMBA_RECURRENCE_KEEP 64
+
+/*
+ * h = a h + u for every channel along the sequence, y = h + add, a mixer without state expansion: of two calls, one with `reverse`
+ * that adds the other's y, comes a bidirectional one.  With h_in and h_out it goes on where an earlier call stopped: blocks, single tokens.
+ *   bias      fp32 [d_inner] or NULL (0); sigmoid gates only (else BIMAMBA_ERR_UNSUPPORTED).
+ *   add       [batch, seqlen, d_inner] or NULL; may be the very view y.
+ *   lengths   int64 [batch] on the device or NULL: sequence b has the first lengths[b] tokens (taken into [0, seqlen]).  Tokens behind
+ *             them are read into nothing; their y are zeros.
+ *   h_in      fp32 [batch, d_inner], the state before a sequence's first step, or NULL (0).
+ *   h_out     the same after its last step, or NULL.  May be h_in.
+ *   states    fp32 [batch, ceil(seqlen / 64), d_inner] or NULL: the state before every 64th step (BIMAMBA_RECURRENCE_KEEP), counted in
+ *             the order of the walk; the gradients take them.  Behind a sequence's end: its last state.
+ *   workspace at least bimamba_recurrence_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL if that is 0.
+ * A value that is not finite makes everything not finite that its channel's walk reaches after it.
+ */
+int bimamba_recurrence(const bimamba_recurrence_desc* desc, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
+                       const bimamba_tensor* add, const int64_t* lengths, const float* h_in, const bimamba_tensor* y, float* h_out,
+                       float* states, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t bimamba_recurrence_workspace_bytes(const bimamba_recurrence_desc* desc);
+
+/*
+ * Its gradients (that of add is dy).  With the step's dh = dy + (a dh of the next step), the last one's from dh_out:
+ *   log       dx = dh, dg = dh h' a (0 where g > 0), h' the state before the step
+ *   sigmoid   dx = dh (1 - a), dg = dh (h' - x) a (1 - a)
+ *   states    what bimamba_recurrence left.  bias, lengths: as there.
+ *   dh_out    fp32 [batch, d_inner], the gradient of h_out, or NULL (0).
+ *   dx, dg    zeros behind a sequence's end.
+ *   dbias     fp32 [d_inner], the sum of dg over all tokens, or NULL; sigmoid gates only.
+ *   dh_in     fp32 [batch, d_inner] or NULL.  May be dh_out.
+ *   workspace at least bimamba_recurrence_bwd_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL if that is 0.
+ */
+int bimamba_recurrence_bwd(const bimamba_recurrence_desc* desc, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
+                           const int64_t* lengths, const float* states, const bimamba_tensor* dy, const float* dh_out,
+                           const bimamba_tensor* dx, const bimamba_tensor* dg, float* dbias, float* dh_in,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t bimamba_recurrence_bwd_workspace_bytes(const bimamba_recurrence_desc* desc);
+
+enum bimamba_norm_act {
+    BIMAMBA_ACT_NONE = 0,
+    BIMAMBA_ACT_SILU = 1,          /* y = SiLU(norm(x)) */
+    BIMAMBA_ACT_GATE_BEFORE = 2,   /* y = norm(x * SiLU(z)) */
+    BIMAMBA_ACT_GATE_AFTER = 3     /* y = norm(x) * SiLU(z) */
+};
+
+/* Host struct.  d_inner is a multiple of groups; at most 8192 channels a group. */
+typedef struct bimamba_group_norm_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_group_norm_desc), checked */
+    int32_t batch;          /* >= 0 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t d_inner;        /* <= 65536 */
+    int32_t groups;         /* >= 1 */
+    int32_t io_dtype;       /* bimamba_dtype of x, z, y and of dy, dx, dz */
+    int32_t act;            /* bimamba_norm_act */
+    int32_t centred;        /* 0: root mean square; 1: the mean is taken off first */
+    float eps;              /* > 0 */
+} bimamba_group_norm_desc;
+
+/* The norm of every token's groups of channels (neighbours each): with u = x, or x * SiLU(z), v = (u - mean) * rstd * weight + bias,
+ * rstd = 1 / sqrt(mean((u - mean)^2) + eps), mean 0 unless centred; y = v, SiLU(v) or v * SiLU(z).
+ *   z               the gate's input; gates only (else it must be NULL: BIMAMBA_ERR_UNSUPPORTED).
+ *   weight, bias    fp32 [d_inner] or NULL (1 and 0).
+ *   mean, rstd      fp32 [batch, seqlen, groups] or NULL (not wanted; the gradients take them); mean: centred only. */
+int bimamba_group_norm(const bimamba_group_norm_desc* desc, const bimamba_tensor* x, const bimamba_tensor* z, const float* weight,
+                       const float* bias, const bimamba_tensor* y, float* mean, float* rstd, void* hip_stream);
+
+/* Its gradients.  With xh = (u - mean) * rstd and dv = dy, dy * SiLU'(v) or dy * SiLU(z): dweight = sum of dv * xh and dbias = sum of dv
+ * over all tokens, fp32 [d_inner], NULL: not wanted; with k = dv * weight, du = rstd * (k - mean(k) - xh * mean(k * xh)) (mean(k):
+ * centred only); dx = du or du * SiLU(z); dz = dy * v * SiLU'(z) or du * x * SiLU'(z).
+ *   workspace   at least bimamba_group_norm_bwd_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL if that is 0 or neither dweight
+ *               nor dbias is wanted. */
+int bimamba_group_norm_bwd(const bimamba_group_norm_desc* desc, const bimamba_tensor* x, const bimamba_tensor* z, const float* weight,
+                           const float* bias, const float* mean, const float* rstd, const bimamba_tensor* dy, const bimamba_tensor* dx,
+                           const bimamba_tensor* dz, float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+size_t bimamba_group_norm_bwd_workspace_bytes(const bimamba_group_norm_desc* desc);
+
+/* Host struct.  d_model <= 2^20, 0 <= site < 2^15. */
+typedef struct bimamba_dropout_desc {
+    uint32_t struct_size;   /* sizeof(bimamba_dropout_desc), checked */
+    int32_t batch;          /* >= 0, <= 65535 */
+    int32_t seqlen;         /* >= 0 */
+    int32_t d_model;
+    int32_t io_dtype;       /* bimamba_dtype of x, residual, out and of dout, dx */
+    int32_t site;           /* which of a model's dropouts it is: sites have masks of their own under one key */
+    float p;                /* share that is dropped, in [0, 1]; taken as round(65536 p) / 65536 */
+} bimamba_dropout_desc;
+
+/*
+ * out = residual + gate * dropout(x).  No mask is stored: value (b, t, c) is kept where its 16 random bits are at least T = round(65536 p),
+ * and multiplied by 65536 / (65536 - T); T = 65536 keeps nothing.  Its bits are half c % 8 (the low half of a word first) of the
+ * four words that Philox4x32 with ten rounds (Salmon et al., 2011) makes of the counter (b * seqlen + t, c / 8 + site * 2^17, low and
+ * high word of the offset) under the seed as its key.
+ *   key        int64 [2] on the device: seed, offset.  A program moves the offset between steps, in a captured graph too.
+ *   gate       fp32, unit stride, or NULL (1).  gate_stride 0: one vector [d_model]; >= d_model: batch element b has its own at
+ *              gate + b * gate_stride.
+ *   residual   or NULL (0); may be the very view out.
+ * What is dropped is not read into the result: a NaN there leaves the residual as it is.
+ */
+int bimamba_dropout_add(const bimamba_dropout_desc* desc, const int64_t* key, const bimamba_tensor* x, const float* gate,
+                        int64_t gate_stride, const bimamba_tensor* residual, const bimamba_tensor* out, void* hip_stream);
+
+/* Its gradients (the residual's is dout): dx = gate * keep * dout / (1 - p), and dgate = the sum of keep * x * dout / (1 - p) over the
+ * tokens that share the vector, fp32 [batch, d_model] contiguous, or [d_model] with gate_stride 0; NULL: not wanted, x may then be NULL too.
+ *   dx          may be the very view dout.
+ *   workspace   at least bimamba_dropout_add_bwd_workspace_bytes(desc, gate_stride != 0) bytes, 16-byte aligned; may be NULL if that is 0
+ *               or dgate is not wanted. */
+int bimamba_dropout_add_bwd(const bimamba_dropout_desc* desc, const int64_t* key, const bimamba_tensor* x, const float* gate,
+                            int64_t gate_stride, const bimamba_tensor* dout, const bimamba_tensor* dx, float* dgate, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+size_t bimamba_dropout_add_bwd_workspace_bytes(const bimamba_dropout_desc* desc, int per_batch);
+
 /* Benchmark diagnostics: arm a one-shot probe on the calling host thread.  The next bimamba_fwd or
  * bimamba_block_fwd made by this thread records ev_start immediately before and ev_stop immediately after its
  * scan-and-combine kernel (on the chunked matrix-core path: around its two launches, one per direction; never the

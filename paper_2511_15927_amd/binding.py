@@ -27,7 +27,10 @@ EXPORTS = ("bimamba_fwd", "bimamba_block_fwd", "bimamba_block_fwd_static", "bima
            "bimamba_bwd_workspace_bytes", "bimamba_time_chunks", "bimamba_profile_next_call", "bimamba_status_string", "bimamba_version",
            "bimamba_embed", "bimamba_embed_bwd", "bimamba_embed_bwd_workspace_bytes", "bimamba_layer_norm", "bimamba_layer_norm_bwd",
            "bimamba_layer_norm_bwd_workspace_bytes", "bimamba_log_probs", "bimamba_log_probs_bwd", "bimamba_log_probs_workspace_bytes",
-           "bimamba_clip_layout", "bimamba_clip_grads", "bimamba_clip_grads_workspace_bytes")
+           "bimamba_clip_layout", "bimamba_clip_grads", "bimamba_clip_grads_workspace_bytes",
+           "bimamba_recurrence", "bimamba_recurrence_workspace_bytes", "bimamba_recurrence_bwd", "bimamba_recurrence_bwd_workspace_bytes",
+           "bimamba_group_norm", "bimamba_group_norm_bwd", "bimamba_group_norm_bwd_workspace_bytes",
+           "bimamba_dropout_add", "bimamba_dropout_add_bwd", "bimamba_dropout_add_bwd_workspace_bytes")
 
 
 class Desc(C.Structure):
@@ -87,6 +90,19 @@ class Grad(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class RecurrenceDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("batch", "seqlen", "d_inner", "io_dtype", "gate", "reverse")]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "batch", "seqlen", "d_inner", "groups", "io_dtype", "act", "centred")] + [("eps", C.c_float)]
+
+
+class DropoutDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("batch", "seqlen", "d_model", "io_dtype", "site")] + [("p", C.c_float)]
+
+
 class BimambaError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -140,7 +156,18 @@ def lib():
         L.bimamba_profile_next_call.restype = None
         L.bimamba_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
         P, V, Z, I = C.POINTER, C.c_void_p, C.c_size_t, C.c_int
+        T, I64 = P(Tensor), C.c_int64
         for name, res, args in (
+                ("bimamba_recurrence", I, [P(RecurrenceDesc), T, T, V, T, V, V, T, V, V, V, Z, V]),
+                ("bimamba_recurrence_workspace_bytes", Z, [P(RecurrenceDesc)]),
+                ("bimamba_recurrence_bwd", I, [P(RecurrenceDesc), T, T, V, V, V, T, V, T, T, V, V, V, Z, V]),
+                ("bimamba_recurrence_bwd_workspace_bytes", Z, [P(RecurrenceDesc)]),
+                ("bimamba_group_norm", I, [P(GroupNormDesc), T, T, V, V, T, V, V, V]),
+                ("bimamba_group_norm_bwd", I, [P(GroupNormDesc), T, T, V, V, V, V, T, T, T, V, V, V, Z, V]),
+                ("bimamba_group_norm_bwd_workspace_bytes", Z, [P(GroupNormDesc)]),
+                ("bimamba_dropout_add", I, [P(DropoutDesc), V, T, V, I64, T, T, V]),
+                ("bimamba_dropout_add_bwd", I, [P(DropoutDesc), V, T, V, I64, T, T, V, V, Z, V]),
+                ("bimamba_dropout_add_bwd_workspace_bytes", Z, [P(DropoutDesc), I]),
                 ("bimamba_embed", I, [P(EmbedDesc), P(Tokens), V, P(Tensor), V]),
                 ("bimamba_embed_bwd", I, [P(EmbedDesc), P(Tokens), P(Tensor), V, V, Z, V]),
                 ("bimamba_embed_bwd_workspace_bytes", Z, [P(EmbedDesc)]),
@@ -468,6 +495,83 @@ def bimamba_clip_grads_workspace_bytes(table):
 def bimamba_clip_grads(table, max_norm, norm, workspace, stream=None, check=True):
     """Enqueue the norm of a GradTable's gradients (norm: float32 [1], or None) and their scaling to at most max_norm."""
     return _checked((_calls_module or _calls()).clip_grads(table.host, table.dev, max_norm, norm, workspace, _stream(stream)), "bimamba_clip_grads", check)
+
+
+# ---- the block of a gated linear recurrence: the recurrence, the norm of its gated output, dropout into the residual stream ----
+
+RECURRENCE_KEEP = 64   # steps between two kept states
+_GATES = {"log": 0, "sigmoid": 1}
+_ACTS = {"none": 0, "silu": 1, "gate_before": 2, "gate_after": 3}
+
+
+def make_recurrence_desc(batch, seqlen, d_inner, io="bf16", gate="sigmoid", reverse=0):
+    """gate: "log" (a = exp(min(g, 0)), u = x) or "sigmoid" (a = sigmoid(g + bias), u = (1 - a) x); reverse: from the last token to the first."""
+    return RecurrenceDesc(C.sizeof(RecurrenceDesc), batch, seqlen, d_inner, _NAMES[io], _GATES[gate], int(reverse))
+
+
+def bimamba_recurrence_workspace_bytes(desc):
+    return int(lib().bimamba_recurrence_workspace_bytes(C.byref(desc)))
+
+
+def bimamba_recurrence(desc, x, g, bias, y, add=None, lengths=None, h_in=None, h_out=None, states=None, workspace=None, stream=None, check=True):
+    """Enqueue h = a h + u along the sequence, y = h + add (add may be y).  x, g, add, y [batch, L, d]; bias float32 [d] or None; lengths int64
+    [batch] or None; h_in, h_out float32 [batch, d] or None, the state before the first and after the last step; states float32
+    [batch, ceil(L / 64), d] or None, that before every 64th (bimamba_recurrence_bwd takes them)."""
+    return _checked((_calls_module or _calls()).recurrence(desc, x, g, bias, add, lengths, h_in, y, h_out, states, workspace, _stream(stream)),
+                    "bimamba_recurrence", check)
+
+
+def bimamba_recurrence_bwd_workspace_bytes(desc):
+    return int(lib().bimamba_recurrence_bwd_workspace_bytes(C.byref(desc)))
+
+
+def bimamba_recurrence_bwd(desc, x, g, bias, states, dy, dx, dg, dbias=None, lengths=None, dh_out=None, dh_in=None, workspace=None, stream=None,
+                           check=True):
+    """Enqueue the gradients of bimamba_recurrence (add's is dy).  dbias float32 [d] or None; dh_out, dh_in float32 [batch, d] or None."""
+    return _checked((_calls_module or _calls()).recurrence_bwd(desc, x, g, bias, lengths, states, dy, dh_out, dx, dg, dbias, dh_in, workspace,
+                                                               _stream(stream)), "bimamba_recurrence_bwd", check)
+
+
+def make_group_norm_desc(batch, seqlen, d_inner, groups, io="bf16", act="none", centred=0, eps=1e-5):
+    """act: "none", "silu", "gate_before" (the norm of x * SiLU(z)) or "gate_after" (times SiLU(z)); centred: the mean is taken off."""
+    return GroupNormDesc(C.sizeof(GroupNormDesc), batch, seqlen, d_inner, groups, _NAMES[io], _ACTS[act], int(centred), eps)
+
+
+def bimamba_group_norm(desc, x, z, weight, bias, y, mean=None, rstd=None, stream=None, check=True):
+    """Enqueue the norm of every token's groups of channels.  z: the gate's input, or None without one; weight, bias float32 [d] or None;
+    mean (centred only), rstd float32 [batch, L, groups] or None (bimamba_group_norm_bwd takes them)."""
+    return _checked((_calls_module or _calls()).group_norm(desc, x, z, weight, bias, y, mean, rstd, _stream(stream)), "bimamba_group_norm", check)
+
+
+def bimamba_group_norm_bwd_workspace_bytes(desc):
+    return int(lib().bimamba_group_norm_bwd_workspace_bytes(C.byref(desc)))
+
+
+def bimamba_group_norm_bwd(desc, x, z, weight, bias, mean, rstd, dy, dx, dz, dweight, dbias, workspace, stream=None, check=True):
+    """Enqueue the gradients of bimamba_group_norm.  dz: None without a gate; dweight, dbias float32 [d] or None; overwritten."""
+    return _checked((_calls_module or _calls()).group_norm_bwd(desc, x, z, weight, bias, mean, rstd, dy, dx, dz, dweight, dbias, workspace,
+                                                               _stream(stream)), "bimamba_group_norm_bwd", check)
+
+
+def make_dropout_desc(batch, seqlen, d_model, io="bf16", p=0.1, site=0):
+    return DropoutDesc(C.sizeof(DropoutDesc), batch, seqlen, d_model, _NAMES[io], site, p)
+
+
+def bimamba_dropout_add(desc, key, x, gate, residual, out, stream=None, check=True):
+    """Enqueue out = residual + gate * dropout(x).  key: int64 [2], seed and offset; gate: float32 [d], or [batch, d] with a vector for each
+    batch element, or None; residual: None, or like x; it may be out."""
+    return _checked((_calls_module or _calls()).dropout_add(desc, key, x, gate, residual, out, _stream(stream)), "bimamba_dropout_add", check)
+
+
+def bimamba_dropout_add_bwd_workspace_bytes(desc, per_batch):
+    return int(lib().bimamba_dropout_add_bwd_workspace_bytes(C.byref(desc), int(per_batch)))
+
+
+def bimamba_dropout_add_bwd(desc, key, x, gate, dout, dx, dgate=None, workspace=None, stream=None, check=True):
+    """Enqueue the gradients of bimamba_dropout_add (the residual's is dout; dx may be dout).  dgate: float32 like gate, contiguous, or None
+    (x may then be None); without a gate its shape says whether each batch element has a vector of its own."""
+    return _checked((_calls_module or _calls()).dropout_add_bwd(desc, key, x, gate, dout, dx, dgate, workspace, _stream(stream)),
+                    "bimamba_dropout_add_bwd", check)
 
 
 # ---- conveniences used by tests and the benchmark (allocation through torch, no arithmetic) ----

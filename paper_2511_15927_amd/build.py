@@ -88,7 +88,7 @@ def build(force: bool = True, jobs: int = 8):
     units.append((os.path.join(CSRC, "bwd_inst.hip"), os.path.join(OBJ, "bwd_inst.o"), []))
     units.append((os.path.join(CSRC, "row_inst.hip"), os.path.join(OBJ, "row_inst.o"), []))
     units.append((os.path.join(CSRC, "stack_inst.hip"), os.path.join(OBJ, "stack_inst.o"), []))
-    for name in ("embed", "norm", "scores", "clip"):
+    for name in ("embed", "norm", "scores", "clip", "recurrence", "group_norm", "dropout", "slot_sums"):
         units.append((os.path.join(CSRC, name + ".hip"), os.path.join(OBJ, name + ".o"), []))
     todo = [u for u in units if force or not os.path.exists(u[1]) or os.path.getmtime(u[1]) < newest_dep(u[0])]
     cmds = [["hipcc"] + FLAGS + extra + ["-c", src, "-o", obj] for src, obj, extra in todo]

@@ -282,10 +282,126 @@ PyObject* clip_grads(PyObject* const* a)   // the host table's bytes, its copy o
     return rc;
 }
 
+// A view, or None: a null pointer then.
+struct Maybe {
+    bimamba_tensor t;
+    bool has;
+    const bimamba_tensor* operator()() const { return has ? &t : nullptr; }
+};
+template <typename Desc>
+Maybe maybe_rows(Reader& r, PyObject* o, const char* what, const Desc& d, int64_t width)
+{
+    const bool has = o != Py_None;
+    return {has ? r.rows(o, what, d.io_dtype, d.batch, d.seqlen, width) : bimamba_tensor{}, has};
+}
+
+PyObject* recurrence(PyObject* const* a)   // desc, x, g, bias, add, lengths, h_in, y, h_out, states, workspace, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_recurrence_desc>(a[0]);
+    const int64_t D = d.d_inner, kept = (d.seqlen + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
+    const auto x = r.rows(a[1], "x", d.io_dtype, d.batch, d.seqlen, D), g = r.rows(a[2], "g", d.io_dtype, d.batch, d.seqlen, D);
+    const float* const bias = r.flat(a[3], "bias", {D});
+    const auto add = maybe_rows(r, a[4], "add", d, D);
+    const int64_t* const lengths = r.flat<int64_t>(a[5], "lengths", {d.batch}, at::kLong);
+    const float* const h_in = r.flat(a[6], "h_in", {d.batch, D});
+    const auto y = r.rows(a[7], "y", d.io_dtype, d.batch, d.seqlen, D);
+    float* const h_out = r.flat(a[8], "h_out", {d.batch, D});
+    float* const states = r.flat(a[9], "states", {d.batch, kept, D});
+    const auto ws = r.workspace(a[10]);
+    void* const st = r.stream(a[11]);
+    return status_of(r, [&] { return bimamba_recurrence(&d, &x, &g, bias, add(), lengths, h_in, &y, h_out, states, ws.p, ws.n, st); });
+}
+PyObject* recurrence_bwd(PyObject* const* a)   // desc, x, g, bias, lengths, states, dy, dh_out, dx, dg, dbias, dh_in, workspace, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_recurrence_desc>(a[0]);
+    const int64_t D = d.d_inner, kept = (d.seqlen + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
+    const auto view = [&](PyObject* o, const char* what) { return r.rows(o, what, d.io_dtype, d.batch, d.seqlen, D); };
+    const auto x = view(a[1], "x"), g = view(a[2], "g");
+    const float* const bias = r.flat(a[3], "bias", {D});
+    const int64_t* const lengths = r.flat<int64_t>(a[4], "lengths", {d.batch}, at::kLong);
+    const float* const states = r.flat(a[5], "states", {d.batch, kept, D});
+    const auto dy = view(a[6], "dy");
+    const float* const dh_out = r.flat(a[7], "dh_out", {d.batch, D});
+    const auto dx = view(a[8], "dx"), dg = view(a[9], "dg");
+    float* const dbias = r.flat(a[10], "dbias", {D});
+    float* const dh_in = r.flat(a[11], "dh_in", {d.batch, D});
+    const auto ws = r.workspace(a[12]);
+    void* const st = r.stream(a[13]);
+    return status_of(r, [&] {
+        return bimamba_recurrence_bwd(&d, &x, &g, bias, lengths, states, &dy, dh_out, &dx, &dg, dbias, dh_in, ws.p, ws.n, st);
+    });
+}
+PyObject* group_norm(PyObject* const* a)   // desc, x, z, weight, bias, y, mean, rstd, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_group_norm_desc>(a[0]);
+    const int64_t D = d.d_inner;
+    const auto x = r.rows(a[1], "x", d.io_dtype, d.batch, d.seqlen, D);
+    const auto z = maybe_rows(r, a[2], "z", d, D);
+    const float *const weight = r.flat(a[3], "weight", {D}), *const bias = r.flat(a[4], "bias", {D});
+    const auto y = r.rows(a[5], "y", d.io_dtype, d.batch, d.seqlen, D);
+    float* const mean = r.flat(a[6], "mean", {d.batch, d.seqlen, d.groups});
+    float* const rstd = r.flat(a[7], "rstd", {d.batch, d.seqlen, d.groups});
+    void* const st = r.stream(a[8]);
+    return status_of(r, [&] { return bimamba_group_norm(&d, &x, z(), weight, bias, &y, mean, rstd, st); });
+}
+PyObject* group_norm_bwd(PyObject* const* a)   // desc, x, z, weight, bias, mean, rstd, dy, dx, dz, dweight, dbias, workspace, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_group_norm_desc>(a[0]);
+    const int64_t D = d.d_inner;
+    const auto x = r.rows(a[1], "x", d.io_dtype, d.batch, d.seqlen, D);
+    const auto z = maybe_rows(r, a[2], "z", d, D);
+    const float *const weight = r.flat(a[3], "weight", {D}), *const bias = r.flat(a[4], "bias", {D});
+    const float* const mean = r.flat(a[5], "mean", {d.batch, d.seqlen, d.groups});
+    const float* const rstd = r.flat(a[6], "rstd", {d.batch, d.seqlen, d.groups});
+    const auto dy = r.rows(a[7], "dy", d.io_dtype, d.batch, d.seqlen, D), dx = r.rows(a[8], "dx", d.io_dtype, d.batch, d.seqlen, D);
+    const auto dz = maybe_rows(r, a[9], "dz", d, D);
+    float *const dweight = r.flat(a[10], "dweight", {D}), *const dbias = r.flat(a[11], "dbias", {D});
+    const auto ws = r.workspace(a[12]);
+    void* const st = r.stream(a[13]);
+    return status_of(r, [&] { return bimamba_group_norm_bwd(&d, &x, z(), weight, bias, mean, rstd, &dy, &dx, dz(), dweight, dbias, ws.p, ws.n, st); });
+}
+const int64_t* key_of(Reader& r, PyObject* o)
+{
+    if (o == Py_None) r.fail("key: not a tensor");
+    return r.flat<int64_t>(o, "key", {2}, at::kLong);
+}
+PyObject* dropout_add(PyObject* const* a)   // desc, key, x, gate, residual, out, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_dropout_desc>(a[0]);
+    const int64_t* const key = key_of(r, a[1]);
+    const auto x = r.rows(a[2], "x", d.io_dtype, d.batch, d.seqlen, d.d_model);
+    const auto gate = r.vector(a[3], "gate", d.batch, d.d_model);
+    const auto residual = maybe_rows(r, a[4], "residual", d, d.d_model);
+    const auto out = r.rows(a[5], "out", d.io_dtype, d.batch, d.seqlen, d.d_model);
+    void* const st = r.stream(a[6]);
+    return status_of(r, [&] { return bimamba_dropout_add(&d, key, &x, gate.p, gate.stride < 0 ? 0 : gate.stride, residual(), &out, st); });
+}
+PyObject* dropout_add_bwd(PyObject* const* a)   // desc, key, x, gate, dout, dx, dgate, workspace, stream
+{
+    Reader r;
+    const auto d = r.desc<bimamba_dropout_desc>(a[0]);
+    const int64_t* const key = key_of(r, a[1]);
+    const auto x = maybe_rows(r, a[2], "x", d, d.d_model);
+    auto gate = r.vector(a[3], "gate", d.batch, d.d_model);
+    const auto dout = r.rows(a[4], "dout", d.io_dtype, d.batch, d.seqlen, d.d_model), dx = r.rows(a[5], "dx", d.io_dtype, d.batch, d.seqlen, d.d_model);
+    if (gate.stride < 0) gate.stride = a[6] != Py_None && THPVariable_Check(a[6]) && THPVariable_Unpack(a[6]).dim() == 2 ? d.d_model : 0;
+    float* const dgate = gate.stride ? r.flat(a[6], "dgate", {d.batch, d.d_model}) : r.flat(a[6], "dgate", {d.d_model});
+    const auto ws = r.workspace(a[7]);
+    void* const st = r.stream(a[8]);
+    return status_of(r, [&] { return bimamba_dropout_add_bwd(&d, key, x(), gate.p, gate.stride, &dout, &dx, dgate, ws.p, ws.n, st); });
+}
+
 #define BM_METHOD(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&method<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BM_METHOD(embed, 5),      BM_METHOD(embed_bwd, 6),      BM_METHOD(layer_norm, 8),
                          BM_METHOD(layer_norm_bwd, 11), BM_METHOD(log_probs, 11), BM_METHOD(log_probs_bwd, 10),
-                         BM_METHOD(clip_grads, 6), {nullptr, nullptr, 0, nullptr}};
+                         BM_METHOD(clip_grads, 6), BM_METHOD(recurrence, 12), BM_METHOD(recurrence_bwd, 14),
+                         BM_METHOD(group_norm, 9), BM_METHOD(group_norm_bwd, 14), BM_METHOD(dropout_add, 7),
+                         BM_METHOD(dropout_add_bwd, 9), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "The library's calls as functions of torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
