@@ -35,7 +35,7 @@ template <typename IO, int N = kPieceOf<IO>, bool kPast = false>
 __device__ __forceinline__ Piece<IO, N> load_piece(const typename IO::T* p)
 {
     Piece<IO, N> r;
-    if constexpr (kPast && sizeof r >= 8) {
+    if constexpr (kPast && sizeof r >= 4) {
         typedef PastCaches<sizeof r> Past;
         const typename Past::Bits bits = __builtin_nontemporal_load(reinterpret_cast<const typename Past::Place*>(p));
         __builtin_memcpy(&r, &bits, sizeof r);
@@ -50,7 +50,7 @@ __device__ __forceinline__ void store_piece(typename IO::T* p, const float (&f)[
     Piece<IO, N> r;
 #pragma unroll
     for (int i = 0; i < N; i++) r.v[i] = io_value<IO>(f[i]);
-    if constexpr (kPast && sizeof r >= 8) {
+    if constexpr (kPast && sizeof r >= 4) {
         typedef PastCaches<sizeof r> Past;
         __builtin_nontemporal_store(__builtin_bit_cast(typename Past::Bits, r), reinterpret_cast<typename Past::Place*>(p));
     } else {

@@ -3,17 +3,18 @@
 
 namespace bm {
 
-// A workgroup walks a segment of the sequence for the channels of one wave: in each step its kW waves take kT tokens each, which stay in
+// The sequence is cut into pieces of kW waves times kT tokens, a workgroup each for the channels of one wave, whose tokens stay in
 // registers.  A wave first runs its tokens from a state of zero, which gives the state E that they add and the factor P that they put
-// on what enters; the pairs are exchanged through shared memory, each wave folds those before it onto the state that entered the step
-// and runs its tokens again from there.  So the activations are read once, one barrier a step.  Where there are too few channels for
-// the chip the sequence is cut into segments: a launch before this one leaves every segment's (P, E), and a segment starts from the fold
-// of those before it; that reads the activations twice.  (The state that enters goes through the links too: it may be replaced by the one
-// that leaves while other segments start.)
+// on what enters; the pairs are exchanged through shared memory, folded onto the state that enters the piece, and the tokens run again
+// from there: the activations are read once.  What enters a piece comes from those before it.  A workgroup publishes its piece's (P, E),
+// looks back, and then publishes what leaves the piece as (0, h).  A pair is one word of 64
+// bits, written and read whole, so that no fence is needed; a word of ones says that nothing is there yet.  Pieces are handed out by a
+// counter in the order of the walk, all channels and sequences of a step before the next step: a workgroup waits for pieces that were
+// handed out before its own only, by workgroups that run, so every wait ends.
 //
 // Everything is in fp32: a, u, the states; y is rounded once.  1 - a is formed beside a from the same exponential, not as a difference, so
 // that neither loses digits where the other is near 1: with e = exp(-|v|), sigmoid(|v|) = 1 - e / (1 + e) and sigmoid(-|v|) = e / (1 + e).
-constexpr int kKeep = 64;   // tokens between two kept states
+constexpr int kKeep = BIMAMBA_RECURRENCE_KEEP;   // steps between two kept states
 
 enum Gate { kLog, kSigmoid };
 
@@ -22,20 +23,21 @@ struct RecurArgs {
     RowView dy, dx, dg;      // gradients
     const float* bias;       // null: 0
     const int64_t* lengths;  // null: L
-    const float* enter;      // [batch][d], null: 0; the state before the first token (gradients: that of the state after the last)
+    const float* enter;      // [batch][d], null: 0; the state before the first step (gradients: that of the state after the last)
     float* leave;            // [batch][d] or null: the state after the last (gradients: that of the state before the first)
     float* states;           // [batch][ceil(L / kKeep)][d] or null
-    float* dbias;            // [batch * nseg][d] or null
-    float* links;            // [batch][nseg][2][d] with several segments: 0 and `enter`, then P, E of the segments in walking order (gradients: P, Q)
-    int L, d, nseg, seg_len, reverse;
+    float* dbias;            // [batch * pieces][d] or null
+    unsigned long long* slots;   // [batch][pieces][d], with several pieces: what enters the first one, then what each leaves, in the order of the walk
+    unsigned* ticket;
+    int L, d, pieces, reverse, batch, look;   // look: pieces before its own that a workgroup looks at
 };
 
-// The tokens that the steps of a scan take.
+// The tokens that the steps of a walk take.
 struct Places {
     int len, reverse;
     __device__ __forceinline__ Places(const RecurArgs& a, int b) : len(a.L), reverse(a.reverse)
     {
-        if (a.lengths) len = (int)max(0ll, min((long long)a.L, (long long)a.lengths[b]));
+        if (a.lengths) len = __builtin_amdgcn_readfirstlane((int)max(0ll, min((long long)a.L, (long long)a.lengths[b])));
     }
     // One that may be read for step s: beyond the end some other one.
     __device__ __forceinline__ int readable(int s) const
@@ -47,36 +49,70 @@ struct Places {
     __device__ __forceinline__ int written(int s) const { return reverse && s < len ? len - 1 - s : s; }
 };
 
-template <typename IO, int kC>
-struct Channels {
-    int at, d;
-    bool whole;   // (wave-uniform) all lanes' channels exist
-    __device__ __forceinline__ Channels(int first, int lane, int d) : at(first + lane * kC), d(d), whole(first + 64 * kC <= d) {}
+// A lane's channels of the rows that a wave's steps take.  kWhole: all of them exist and lie within the sequence; nothing is clamped, and there
+// is no branch.  Rows are wave-uniform pointers and lanes unsigned 32-bit offsets, kept narrow where they are used, so that the
+// accesses take a scalar base: sixteen tokens of two tensors in flight otherwise hold sixty registers of addresses.
+template <typename IO, int kC, int kT, bool kPast, bool kWhole>
+struct Steps {
+    typedef typename IO::T T;
     typedef Piece<IO, kC> Raw;
-    __device__ __forceinline__ Raw load(const RowView& v, int b, int t) const
+    const Places& places;
+    int b, s0, L, at, d;
+    unsigned off;   // bytes; the last channels of a row are loaded whole and moved into place
+    __device__ __forceinline__ Steps(const Places& places, int b, int s0, int L, int first, int lane, int d)
+        : places(places), b(b), s0(s0), L(L), at(first + lane * kC), d(d), off((unsigned)min(at, d - kC) * (unsigned)sizeof(T)) {}
+    static __device__ __forceinline__ char* row(const RowView& v, int b, int t) { return static_cast<char*>(v.p) + row_offset(v, b, t) * (long long)sizeof(T); }
+    __device__ __forceinline__ unsigned narrow() const
     {
-        return load_clamped<IO, kC>(static_cast<const typename IO::T*>(v.p) + row_offset(v, b, t), at, d);
+        unsigned o = off;
+        asm volatile("" : "+v"(o));
+        return o;
     }
-    __device__ __forceinline__ void settled(Raw& r) const
+    __device__ __forceinline__ bool inside(int i) const { return kWhole || s0 + i < places.len; }
+    __device__ __forceinline__ void load(Raw (&r)[kT], const RowView& v) const
     {
-        if (!whole) settle(r, at, d, typename IO::T(0));
+        const char* p = row(v, b, places.readable(s0));
+        const long long step = (places.reverse ? -v.st : v.st) * (long long)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kT; i++) {
+            if constexpr (kWhole) {
+                r[i] = load_piece<IO, kC, kPast>(reinterpret_cast<const T*>(p + narrow()));
+                p += step;
+            } else {
+                r[i] = load_piece<IO, kC, kPast>(reinterpret_cast<const T*>(row(v, b, places.readable(s0 + i)) + off));
+            }
+        }
+        if constexpr (!kWhole) {
+#pragma unroll
+            for (int i = 0; i < kT; i++) settle(r[i], at, d, T(0));
+        }
     }
-    __device__ __forceinline__ void store(const RowView& v, int b, int t, const float (&f)[kC]) const
+    __device__ __forceinline__ void store(const RowView& v, int i, const float (&f)[kC]) const
     {
-        typename IO::T* const row = static_cast<typename IO::T*>(v.p) + row_offset(v, b, t);
-        if (whole) store_piece<IO>(row + at, f);
-        else store_piece_of<IO>(row, at, d, f);
+        if constexpr (kWhole) {
+            store_piece<IO, kPast>(reinterpret_cast<T*>(row(v, b, places.written(s0)) + (places.reverse ? -i : i) * v.st * (long long)sizeof(T) + narrow()), f);
+        } else if (s0 + i < L) {
+            store_piece_of<IO>(reinterpret_cast<T*>(row(v, b, places.written(s0 + i))), at, d, f);
+        }
     }
     __device__ __forceinline__ void load_params(float (&f)[kC], const float* p) const
     {
+        if (p) {
+            Piece<IoF32, kC> v = load_piece<IoF32, kC>(p + min(at, d - kC));
+            if constexpr (!kWhole) settle(v, at, d, 0.0f);
 #pragma unroll
-        for (int k = 0; k < kC; k++) f[k] = p && at + k < d ? p[at + k] : 0.0f;
+            for (int j = 0; j < kC; j++) f[j] = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kC; j++) f[j] = 0.0f;
+        }
     }
+    __device__ __forceinline__ bool has(int j) const { return kWhole || at + j < d; }
     __device__ __forceinline__ void store_params(float* p, const float (&f)[kC]) const
     {
 #pragma unroll
-        for (int k = 0; k < kC; k++)
-            if (at + k < d) p[at + k] = f[k];
+        for (int j = 0; j < kC; j++)
+            if (has(j)) p[at + j] = f[j];
     }
 };
 
@@ -94,321 +130,341 @@ __device__ __forceinline__ void gate_of(float g, float bias, float& a, float& q)
     }
 }
 
+// Keeps a raw piece as it is: what was made of it before is not kept in registers for later.
+template <typename Raw>
+__device__ __forceinline__ void hold(Raw& r)
+{
+    if constexpr (sizeof r == 4) {
+        unsigned bits = __builtin_bit_cast(unsigned, r);
+        asm volatile("" : "+v"(bits));
+        r = __builtin_bit_cast(Raw, bits);
+    }
+}
+
 template <int kC>
 struct Link {
     float p[kC], e[kC];
 };
 
-// What enters the segment that comes `turn` segments after the first one walked.
-template <typename IO, int kC>
-__device__ __forceinline__ void enter(float (&carry)[kC], const Channels<IO, kC>& ch, const RecurArgs& r, int b, int turn)
+constexpr unsigned kNothing = ~0u;
+__device__ __forceinline__ void publish(unsigned long long* to, float p, float e)
 {
-    if (r.nseg == 1) {
-        ch.load_params(carry, r.enter ? r.enter + (long long)b * r.d : nullptr);
-        return;
-    }
-    const float* link = r.links + (long long)b * r.nseg * 2 * r.d;
+    const unsigned hi = p != p ? 0x7fc00000u : __float_as_uint(p);
+    __hip_atomic_store(to, (unsigned long long)hi << 32 | __float_as_uint(e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// What a link makes of the state that enters it.  (One that nothing passes ends there, so that the word (0, h) stands for the state h itself.)
+__device__ __forceinline__ float through(float p, float e, float h) { return p == 0.0f ? e : p * h + e; }
+
+// Waits for a piece's words, `end`: for those of the state that it leaves.  (Were they not to come, which would be a mistake here, the walk
+// would go on with a NaN, not stand still.)
+template <int kC, typename At>
+__device__ __forceinline__ Link<kC> await(const unsigned long long* from, const At& steps, bool end)
+{
+    Link<kC> link;
+    unsigned long long word[kC];
+    const auto there = [&](int j) {
+        const unsigned hi = (unsigned)(word[j] >> 32);
+        return end ? hi == 0 : hi != kNothing;
+    };
+    int tries = 1 << 22;
+    for (;;) {
+        bool all = true;
 #pragma unroll
-    for (int j = 0; j < kC; j++) carry[j] = 0.0f;
-#pragma unroll 4
-    for (int k = 0; k <= turn; k++, link += 2 * r.d) {
-        float p[kC], e[kC];
-        ch.load_params(p, link);
-        ch.load_params(e, link + r.d);
-#pragma unroll
-        for (int j = 0; j < kC; j++) carry[j] = p[j] * carry[j] + e[j];
+        for (int j = 0; j < kC; j++) {
+            word[j] = steps.has(j) ? __hip_atomic_load(from + steps.at + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+            all &= there(j);
+        }
+        if (__all(all) || --tries == 0) break;
+        __builtin_amdgcn_s_sleep(1);
     }
+#pragma unroll
+    for (int j = 0; j < kC; j++) {
+        link.p[j] = there(j) ? __uint_as_float((unsigned)(word[j] >> 32)) : 0.0f;
+        link.e[j] = there(j) ? __uint_as_float((unsigned)word[j]) : __builtin_nanf("");
+    }
+    return link;
+}
+// Before the pieces: nothing is there but what enters the first one.  (The state that enters is read here only: it may be the one that the
+// last piece replaces.)
+__global__ __launch_bounds__(256) void recur_clear_kernel(const RecurArgs r)
+{
+    const long long n = (long long)r.pieces * r.d, i = blockIdx.x * 256ll + threadIdx.x;
+    const int b = blockIdx.y;
+    if (i == 0 && b == 0) *r.ticket = 0;
+    if (i >= n) return;
+    r.slots[b * n + i] = i < r.d ? (r.enter ? __float_as_uint(r.enter[(long long)b * r.d + i]) : 0) : ~0ull;
 }
 
-template <typename IO, int kGate, int kC, int kT, int kW, int kV>
-__global__ __launch_bounds__(64 * kW * kV) void recur_kernel(const RecurArgs r)
-{
-    __shared__ Link<kC> part[2][kW][kV * 64];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % kW, v = wave / kW;
-    const int tiles = (r.d + 64 * kC * kV - 1) / (64 * kC * kV), tile = blockIdx.x % tiles, seg = blockIdx.x / tiles, b = blockIdx.y;
-    const Channels<IO, kC> ch((tile * kV + v) * 64 * kC, lane, r.d);
-    const Places places(r, b);
-    const int p0 = seg * r.seg_len, p1 = min(p0 + r.seg_len, r.L), column = v * 64 + lane;
-    float bias[kC], carry[kC];
-    ch.load_params(bias, r.bias);
-    enter(carry, ch, r, b, seg);
-    Piece<IO, kC> nx[kT], ng[kT], nadd[kT];
-    const auto request = [&](int base) {
-#pragma unroll
-        for (int i = 0; i < kT; i++) {
-            const int t = places.readable(base + w * kT + i);
-            nx[i] = ch.load(r.x, b, t);
-            ng[i] = ch.load(r.g, b, t);
-        }
-    };
-    request(p0);
-    int turn = 0;
-    for (int base = p0; base < p1; base += kW * kT, turn ^= 1) {
-        const int s0 = base + w * kT;
-        float a[kT][kC], u[kT][kC];
-        Link<kC> mine;
-#pragma unroll
-        for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = 0.0f;
-        if (r.add.p)
-#pragma unroll
-            for (int i = 0; i < kT; i++) nadd[i] = ch.load(r.add, b, places.readable(s0 + i));
-#pragma unroll
-        for (int i = 0; i < kT; i++) {
-            ch.settled(nx[i]);
-            ch.settled(ng[i]);
-            const bool inside = s0 + i < places.len;
-#pragma unroll
-            for (int j = 0; j < kC; j++) {
-                float q;
-                gate_of<kGate>(ng[i][j], bias[j], a[i][j], q);
-                u[i][j] = kGate == kSigmoid ? q * nx[i][j] : nx[i][j];
-                if (!inside) a[i][j] = 1.0f, u[i][j] = 0.0f;
-                mine.e[j] = a[i][j] * mine.e[j] + u[i][j];
-                mine.p[j] *= a[i][j];
-            }
-        }
-        if (base + kW * kT < p1) request(base + kW * kT);
-        float h[kC];
-#pragma unroll
-        for (int j = 0; j < kC; j++) h[j] = carry[j];
-        if constexpr (kW > 1) {
-            part[turn][w][column] = mine;
+// What a workgroup's waves share.
+constexpr int kMostLooked = 8;
+template <int kC, int kW>
+struct PieceShared {
+    Link<kC> part[kW][64], seen[kMostLooked][64];
+    float before[kW][kC][64];   // (gradients)
+    unsigned ticket;
+};
+// Which piece it is, of how many channels and where.
+struct PieceOf {
+    int turn, b, first;
+    template <typename Shared>
+    __device__ __forceinline__ PieceOf(const RecurArgs& r, int channels, Shared& sh)
+    {
+        unsigned n = blockIdx.x;
+        if (r.pieces > 1) {
+            if (threadIdx.x == 0) sh.ticket = atomicAdd(r.ticket, 1u);
             __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kW; k++) {
-                const Link<kC> link = part[turn][k][column];
-#pragma unroll
-                for (int j = 0; j < kC; j++) {
-                    carry[j] = link.p[j] * carry[j] + link.e[j];
-                    if (k + 1 == w) h[j] = carry[j];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kC; j++) carry[j] = mine.p[j] * carry[j] + mine.e[j];
+            n = __builtin_amdgcn_readfirstlane(sh.ticket);
         }
-        if (r.states && s0 % kKeep == 0 && s0 < p1) ch.store_params(r.states + ((long long)b * ((r.L + kKeep - 1) / kKeep) + s0 / kKeep) * r.d, h);
+        const unsigned tiles = (r.d + channels - 1) / channels, chains = tiles * r.batch;
+        turn = n / chains;
+        b = n % chains / tiles;
+        first = n % tiles * channels;
+    }
+};
+// What enters the piece: the state that the r.look-th piece before it leaves, and the links of those between, folded in the order of the walk.
+// The state that a piece leaves is this same fold, one link further, so its bits do not depend on how far back the look went or on
+// which of the words were there.  A sequence of one piece has read what enters it beside its tokens, before a barrier: the same memory may
+// be written at its end.
+template <int kC, int kW, typename At>
+__device__ __forceinline__ void look_back(float (&carry)[kC], const At& steps, const RecurArgs& r, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
+{
+    const unsigned long long* const slots = r.slots + (long long)piece.b * r.pieces * r.d;
+    const int look = min(r.look, piece.turn + 1);   // (slot `turn` is what the piece before this one leaves, slot 0 what enters the first one)
+    for (int k = w; k < look; k += kW) sh.seen[k][lane] = await<kC>(slots + (long long)(piece.turn - k) * r.d, steps, k == look - 1);
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kT; i++) {
-            const int s = s0 + i;
-            float f[kC];
-            if (r.add.p) ch.settled(nadd[i]);
+    for (int j = 0; j < kC; j++) carry[j] = sh.seen[look - 1][lane].e[j];
+#pragma unroll 1
+    for (int k = look - 2; k >= 0; k--) {
+        const Link<kC> link = sh.seen[k][lane];
+#pragma unroll
+        for (int j = 0; j < kC; j++) carry[j] = through(link.p[j], link.e[j], carry[j]);
+    }
+}
+// What the piece leaves: to those after it, or, from the last one, to the caller.
+template <int kC, typename At>
+__device__ __forceinline__ void leave(const Link<kC>& all, const float (&carry)[kC], const At& steps, const RecurArgs& r, const PieceOf& piece)
+{
+    float end[kC];
+#pragma unroll
+    for (int j = 0; j < kC; j++) end[j] = through(all.p[j], all.e[j], carry[j]);
+    if (piece.turn == r.pieces - 1) {
+        if (r.leave) steps.store_params(r.leave + (long long)piece.b * r.d, end);
+        return;
+    }
+    unsigned long long* const to = r.slots + ((long long)piece.b * r.pieces + piece.turn + 1) * r.d + steps.at;
+#pragma unroll
+    for (int j = 0; j < kC; j++)
+        if (steps.has(j)) publish(to + j, 0.0f, end[j]);
+}
+template <int kC, typename At>
+__device__ __forceinline__ void announce(const Link<kC>& all, const At& steps, const RecurArgs& r, const PieceOf& piece)
+{
+    if (r.look < 2 || piece.turn == 0 || piece.turn == r.pieces - 1) return;   // (the first one's end is known at once, the last one's no piece asks for)
+    unsigned long long* const to = r.slots + ((long long)piece.b * r.pieces + piece.turn + 1) * r.d + steps.at;
+#pragma unroll
+    for (int j = 0; j < kC; j++)
+        if (steps.has(j)) publish(to + j, all.p[j], all.e[j]);
+}
+
+template <typename IO, int kGate, int kC, int kT, int kW, bool kPast, bool kWhole>
+__device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
+{
+    const int s0 = (piece.turn * kW + w) * kT;
+    const Steps<IO, kC, kT, kPast, kWhole> steps(places, piece.b, s0, r.L, piece.first, lane, r.d);
+    Piece<IO, kC> x[kT], g[kT], add[kT];
+    steps.load(x, r.x);
+    steps.load(g, r.g);
+    float bias[kC], a[kT][kC], u[kT][kC], h[kC];
+    steps.load_params(bias, r.bias);
+    if (r.pieces == 1) steps.load_params(h, r.enter ? r.enter + (long long)piece.b * r.d : nullptr);
+    if (r.add.p) {
+        steps.load(add, r.add);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kT; i++) add[i] = Piece<IO, kC>{};
+    }
+    Link<kC> mine;
+#pragma unroll
+    for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kT; i++)
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            float q;
+            gate_of<kGate>(g[i][j], bias[j], a[i][j], q);
+            u[i][j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
+            if (!steps.inside(i)) a[i][j] = 1.0f, u[i][j] = 0.0f;
+            mine.e[j] = a[i][j] * mine.e[j] + u[i][j];
+            mine.p[j] *= a[i][j];
+        }
+    Link<kC> all = mine, before;
+    if constexpr (kW > 1) {
+        sh.part[w][lane] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kC; j++) all.p[j] = before.p[j] = 1.0f, all.e[j] = before.e[j] = 0.0f;
+#pragma unroll 2
+        for (int k = 0; k < kW; k++) {   // (all of it unrolled: the links' registers cost a quarter of the waves)
+            const Link<kC> link = sh.part[k][lane];
 #pragma unroll
             for (int j = 0; j < kC; j++) {
-                h[j] = a[i][j] * h[j] + u[i][j];
-                f[j] = s < places.len ? h[j] + (r.add.p ? nadd[i][j] : 0.0f) : 0.0f;
+                all.e[j] = link.p[j] * all.e[j] + link.e[j];
+                all.p[j] *= link.p[j];
+                if (k + 1 == w) before.p[j] = all.p[j], before.e[j] = all.e[j];
             }
-            if (s < p1) ch.store(r.y, b, places.written(s), f);
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kC; j++) before.p[j] = 1.0f, before.e[j] = 0.0f;
     }
-    if (r.leave && seg == r.nseg - 1 && w == 0) ch.store_params(r.leave + (long long)b * r.d, carry);
+    if (w == 0) announce(all, steps, r, piece);
+    if (r.pieces > 1) look_back<kC, kW>(h, steps, r, piece, w, lane, sh);
+    if (w == 0) leave(all, h, steps, r, piece);
+#pragma unroll
+    for (int j = 0; j < kC; j++) h[j] = before.p[j] * h[j] + before.e[j];
+    if (r.states && s0 % kKeep == 0 && s0 < r.L) steps.store_params(r.states + ((long long)piece.b * ((r.L + kKeep - 1) / kKeep) + s0 / kKeep) * r.d, h);
+#pragma unroll
+    for (int i = 0; i < kT; i++) {
+        float f[kC];
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            h[j] = a[i][j] * h[j] + u[i][j];
+            f[j] = steps.inside(i) ? h[j] + add[i][j] : 0.0f;
+        }
+        steps.store(r.y, i, f);
+    }
+}
+template <typename IO, int kGate, int kC, int kT, int kW, bool kPast>
+__global__ __launch_bounds__(64 * kW, 4) void recur_kernel(const RecurArgs r)
+{
+    __shared__ PieceShared<kC, kW> sh;
+    const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const PieceOf piece(r, 64 * kC, sh);
+    const Places places(r, piece.b);
+    if (piece.first + 64 * kC <= r.d && (piece.turn + 1) * kW * kT <= places.len) recur_piece<IO, kGate, kC, kT, kW, kPast, true>(r, places, piece, w, lane, sh);
+    else recur_piece<IO, kGate, kC, kT, kW, kPast, false>(r, places, piece, w, lane, sh);
 }
 
 // dh_s = dy_s + a_{s+1} dh_{s+1} is the same recurrence from the other end: what enters a wave's tokens is q = a dh of the token after
-// them, and they leave Q + P q.  The states in front of a wave's tokens are folded from the kept one before them, so the walk reads x, g
-// and dy once and writes dx and dg.  dbias is summed by lane over the segment, then over the waves and the slots in a fixed order.
-template <typename IO, int kGate, int kC, int kT, int kW, int kV>
-__global__ __launch_bounds__(64 * kW * kV) void recur_bwd_kernel(const RecurArgs r)
+// them, and they leave Q + P q; the pieces go from the last one to the first.  The states in front of a wave's tokens are folded from the kept
+// one before them, so that x, g and dy are read once and dx and dg written.  Between the two runs a token keeps a, the factors that dx
+// and dg are of dh, and dy as it was read, not the states.  dbias is summed by lane over the wave's tokens, then over the waves and the
+// pieces in a fixed order.
+template <typename IO, int kGate, int kC, int kT, int kW, bool kPast, bool kWhole>
+__device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
 {
-    static_assert((kW * kT) % kKeep == 0, "every step starts at a kept state");
-    struct Links {
-        float p[kC], e[kC], q[kC];
-    };
-    __shared__ Links part[2][kW][kV * 64];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % kW, v = wave / kW;
-    const int tiles = (r.d + 64 * kC * kV - 1) / (64 * kC * kV), tile = blockIdx.x % tiles, seg = blockIdx.x / tiles, b = blockIdx.y;
-    const Channels<IO, kC> ch((tile * kV + v) * 64 * kC, lane, r.d);
-    const Places places(r, b);
-    const int p0 = seg * r.seg_len, p1 = min(p0 + r.seg_len, r.L), column = v * 64 + lane, kept = (r.L + kKeep - 1) / kKeep;
-    float bias[kC], carry[kC], dbias[kC];
-    ch.load_params(bias, r.bias);
-    enter(carry, ch, r, b, r.nseg - 1 - seg);
+    const int seg = r.pieces - 1 - piece.turn, base = seg * kW * kT, s0 = base + w * kT, kept = (r.L + kKeep - 1) / kKeep, first = min(s0 / kKeep, kept - 1);
+    const Steps<IO, kC, kT, kPast, kWhole> steps(places, piece.b, s0, r.L, piece.first, lane, r.d);
+    Piece<IO, kC> x[kT], g[kT], dy[kT];
+    steps.load(x, r.x);
+    steps.load(g, r.g);
+    steps.load(dy, r.dy);
+    float bias[kC], dbias[kC], h[kC], dh[kC], a[kT][kC], q[kT][kC];
+    steps.load_params(bias, r.bias);
+    steps.load_params(h, r.states + ((long long)piece.b * kept + first) * r.d);
+    if (r.pieces == 1) steps.load_params(dh, r.enter ? r.enter + (long long)piece.b * r.d : nullptr);
+    Link<kC> mine;   // (P, Q)
+    float e[kC];
 #pragma unroll
-    for (int j = 0; j < kC; j++) dbias[j] = 0.0f;
-    Piece<IO, kC> nx[kT], ng[kT], nd[kT];
-    const auto request = [&](int base) {
+    for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = e[j] = dbias[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kT; i++) {
-            const int t = places.readable(base + w * kT + i);
-            nx[i] = ch.load(r.x, b, t);
-            ng[i] = ch.load(r.g, b, t);
-            nd[i] = ch.load(r.dy, b, t);
-        }
-    };
-    const int steps = (p1 - p0 + kW * kT - 1) / (kW * kT);
-    request(p0 + (steps - 1) * kW * kT);
-    int turn = 0;
-    for (int base = p0 + (steps - 1) * kW * kT; base >= p0; base -= kW * kT, turn ^= 1) {
-        const int s0 = base + w * kT;
-        float a[kT][kC], q[kT][kC], x[kT][kC], dy[kT][kC], h[kC];
-        const int first = min(s0 / kKeep, kept - 1);   // (waves beyond the end: any)
-        ch.load_params(h, r.states + ((long long)b * kept + first) * r.d);
-        Links mine;
+    for (int i = 0; i < kT; i++)
 #pragma unroll
-        for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = mine.q[j] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kT; i++) {
-            ch.settled(nx[i]);
-            ch.settled(ng[i]);
-            ch.settled(nd[i]);
-            const bool inside = s0 + i < places.len;
-#pragma unroll
-            for (int j = 0; j < kC; j++) {
-                gate_of<kGate>(ng[i][j], bias[j], a[i][j], q[i][j]);
-                x[i][j] = nx[i][j], dy[i][j] = nd[i][j];
-                if (!inside) a[i][j] = 1.0f, q[i][j] = x[i][j] = dy[i][j] = 0.0f;
-                mine.e[j] = a[i][j] * mine.e[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
-                mine.p[j] *= a[i][j];
-            }
+        for (int j = 0; j < kC; j++) {
+            gate_of<kGate>(g[i][j], bias[j], a[i][j], q[i][j]);
+            if (!steps.inside(i)) a[i][j] = 1.0f, q[i][j] = 0.0f, x[i].v[j] = dy[i].v[j] = 0;
+            e[j] = a[i][j] * e[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
+            mine.p[j] *= a[i][j];
         }
 #pragma unroll
-        for (int i = kT - 1; i >= 0; i--)
+    for (int i = kT - 1; i >= 0; i--)
 #pragma unroll
-            for (int j = 0; j < kC; j++) mine.q[j] = a[i][j] * (dy[i][j] + mine.q[j]);
-        if (base > p0) request(base - kW * kT);
-        float dh[kC];   // (q of the tokens behind)
+        for (int j = 0; j < kC; j++) mine.e[j] = a[i][j] * (dy[i][j] + mine.e[j]);
+    Link<kC> all = mine, behind;
 #pragma unroll
-        for (int j = 0; j < kC; j++) dh[j] = carry[j];
-        if constexpr (kW > 1) {
-            part[turn][w][column] = mine;
-            __syncthreads();
-            const int w0 = (first * kKeep - base) / kT;   // (the wave that starts at the kept state)
+    for (int j = 0; j < kC; j++) behind.p[j] = 1.0f, behind.e[j] = 0.0f;
+    if constexpr (kW > 1) {
+        sh.part[w][lane] = mine;
 #pragma unroll
-            for (int k = 0; k < kW; k++)
-                if (k >= w0 && k < w) {
-                    const Links link = part[turn][k][column];
+        for (int j = 0; j < kC; j++) sh.before[w][j][lane] = e[j];
+        __syncthreads();
+        const int w0 = (first * kKeep - base) / kT;   // (the wave that starts at the kept state)
+#pragma unroll 1
+        for (int k = w0; k < w; k++) {
+            const Link<kC> link = sh.part[k][lane];
 #pragma unroll
-                    for (int j = 0; j < kC; j++) h[j] = link.p[j] * h[j] + link.e[j];
-                }
-#pragma unroll
-            for (int k = kW - 1; k >= 0; k--) {
-                const Links link = part[turn][k][column];
-#pragma unroll
-                for (int j = 0; j < kC; j++) {
-                    carry[j] = link.p[j] * carry[j] + link.q[j];
-                    if (k - 1 == w) dh[j] = carry[j];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kC; j++) carry[j] = mine.p[j] * carry[j] + mine.q[j];
+            for (int j = 0; j < kC; j++) h[j] = link.p[j] * h[j] + sh.before[k][j][lane];
         }
-        float before[kT][kC];
 #pragma unroll
-        for (int i = 0; i < kT; i++)
-#pragma unroll
-            for (int j = 0; j < kC; j++) {
-                before[i][j] = h[j];
-                h[j] = a[i][j] * h[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
-            }
-#pragma unroll
-        for (int i = kT - 1; i >= 0; i--) {
-            const int s = s0 + i;
-            float dx[kC], dg[kC];
+        for (int j = 0; j < kC; j++) all.p[j] = 1.0f, all.e[j] = 0.0f;
+#pragma unroll 2
+        for (int k = kW - 1; k >= 0; k--) {
+            const Link<kC> link = sh.part[k][lane];
 #pragma unroll
             for (int j = 0; j < kC; j++) {
-                const float d = dy[i][j] + dh[j];
-                dh[j] = a[i][j] * d;
-                if (kGate == kSigmoid) {
-                    dx[j] = d * q[i][j];
-                    dg[j] = dx[j] * (before[i][j] - x[i][j]) * a[i][j];
-                } else {
-                    dx[j] = d;
-                    dg[j] = d * before[i][j] * q[i][j];
-                }
-                if (s >= places.len) dx[j] = dg[j] = 0.0f;
-                dbias[j] += dg[j];
-            }
-            if (s < p1) {
-                const int t = places.written(s);
-                ch.store(r.dx, b, t, dx);
-                ch.store(r.dg, b, t, dg);
+                all.e[j] = link.p[j] * all.e[j] + link.e[j];
+                all.p[j] *= link.p[j];
+                if (k - 1 == w) behind.p[j] = all.p[j], behind.e[j] = all.e[j];
             }
         }
     }
-    if (r.leave && seg == 0 && w == 0) ch.store_params(r.leave + (long long)b * r.d, carry);
-    if (r.dbias) {
-        float* const slot = r.dbias + ((long long)b * r.nseg + seg) * r.d;
-        if constexpr (kW > 1) {
-            __syncthreads();
+    if (w == 0) announce(all, steps, r, piece);
+    float c[kT][kC];
 #pragma unroll
-            for (int j = 0; j < kC; j++) part[0][w][column].p[j] = dbias[j];
+    for (int i = 0; i < kT; i++) {
+        hold(x[i]);
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            const float v = x[i][j];
+            c[i][j] = kGate == kSigmoid ? q[i][j] * (h[j] - v) * a[i][j] : h[j] * q[i][j];
+            h[j] = a[i][j] * h[j] + (kGate == kSigmoid ? q[i][j] * v : v);
+        }
+    }
+    if (r.pieces > 1) look_back<kC, kW>(dh, steps, r, piece, w, lane, sh);
+    if (w == 0) leave(all, dh, steps, r, piece);
+#pragma unroll
+    for (int j = 0; j < kC; j++) dh[j] = behind.p[j] * dh[j] + behind.e[j];
+#pragma unroll
+    for (int i = kT - 1; i >= 0; i--) {
+        float dx[kC], dg[kC];
+        hold(dy[i]);
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            const float d = dy[i][j] + dh[j];
+            dh[j] = a[i][j] * d;
+            dx[j] = kGate == kSigmoid ? d * q[i][j] : d;
+            dg[j] = d * c[i][j];
+            if (!steps.inside(i)) dx[j] = dg[j] = 0.0f;
+            dbias[j] += dg[j];
+        }
+        steps.store(r.dx, i, dx);
+        steps.store(r.dg, i, dg);
+    }
+    if (r.dbias) {
+        if constexpr (kW > 1) {
+            __syncthreads();   // (`before` has been read)
+#pragma unroll
+            for (int j = 0; j < kC; j++) sh.before[w][j][lane] = dbias[j];
             __syncthreads();
             if (w == 0)
 #pragma unroll
                 for (int k = 1; k < kW; k++)
 #pragma unroll
-                    for (int j = 0; j < kC; j++) dbias[j] += part[0][k][column].p[j];
+                    for (int j = 0; j < kC; j++) dbias[j] += sh.before[k][j][lane];
         }
-        if (w == 0) ch.store_params(slot, dbias);
+        if (w == 0) steps.store_params(r.dbias + ((long long)piece.b * r.pieces + seg) * r.d, dbias);
     }
 }
-
-// The (P, E) of a segment, or with kBack its (P, Q): each wave takes a run of it, the runs are joined at the end.
-template <typename IO, int kGate, int kC, int kT, int kW, bool kBack>
-__global__ __launch_bounds__(64 * kW) void recur_ends_kernel(const RecurArgs r)
+template <typename IO, int kGate, int kC, int kT, int kW, bool kPast>
+__global__ __launch_bounds__(64 * kW) void recur_bwd_kernel(const RecurArgs r)
 {
-    __shared__ Link<kC> part[kW][64];
+    __shared__ PieceShared<kC, kW> sh;
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int tiles = (r.d + 64 * kC - 1) / (64 * kC), tile = blockIdx.x % tiles, turn = blockIdx.x / tiles, b = blockIdx.y;
-    const int seg = kBack ? r.nseg - 1 - turn : turn;   // (the last one walked leaves nothing that is wanted)
-    const Channels<IO, kC> ch(tile * 64 * kC, lane, r.d);
-    const Places places(r, b);
-    const int run = r.seg_len / kW, p0 = seg * r.seg_len + w * run, p1 = min(p0 + run, r.L), steps = max(0, (p1 - p0 + kT - 1) / kT);
-    float bias[kC];
-    ch.load_params(bias, r.bias);
-    Link<kC> mine;
-#pragma unroll
-    for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = 0.0f;
-    for (int k = 0; k < steps; k++) {
-        const int s0 = p0 + (kBack ? steps - 1 - k : k) * kT;
-        Piece<IO, kC> x[kT], g[kT];
-#pragma unroll
-        for (int i = 0; i < kT; i++) {
-            const int t = places.readable(s0 + i);
-            x[i] = ch.load(kBack ? r.dy : r.x, b, t);
-            g[i] = ch.load(r.g, b, t);
-        }
-#pragma unroll
-        for (int n = 0; n < kT; n++) {
-            const int i = kBack ? kT - 1 - n : n;
-            ch.settled(x[i]);
-            ch.settled(g[i]);
-            const bool inside = s0 + i < min(p1, places.len);
-#pragma unroll
-            for (int j = 0; j < kC; j++) {
-                float a, q, u = x[i][j];
-                gate_of<kGate>(g[i][j], bias[j], a, q);
-                if (!inside) a = 1.0f, q = u = 0.0f;
-                if constexpr (kBack) mine.e[j] = a * (u + mine.e[j]);
-                else mine.e[j] = a * mine.e[j] + (kGate == kSigmoid ? q * u : u);
-                mine.p[j] *= a;
-            }
-        }
-    }
-    part[w][lane] = mine;
-    __syncthreads();
-    if (w != 0) return;
-    mine = part[kBack ? kW - 1 : 0][lane];
-#pragma unroll
-    for (int n = 1; n < kW; n++) {
-        const Link<kC> link = part[kBack ? kW - 1 - n : n][lane];
-#pragma unroll
-        for (int j = 0; j < kC; j++) {
-            mine.e[j] = link.p[j] * mine.e[j] + link.e[j];
-            mine.p[j] *= link.p[j];
-        }
-    }
-    float* const to = r.links + ((long long)b * r.nseg + turn + 1) * 2 * r.d;
-    ch.store_params(to, mine.p);
-    ch.store_params(to + r.d, mine.e);
-    if (turn == 0) {
-        ch.load_params(mine.e, r.enter ? r.enter + (long long)b * r.d : nullptr);
-#pragma unroll
-        for (int j = 0; j < kC; j++) mine.p[j] = 0.0f;
-        ch.store_params(to - 2 * r.d, mine.p);
-        ch.store_params(to - r.d, mine.e);
-    }
+    const PieceOf piece(r, 64 * kC, sh);
+    const Places places(r, piece.b);
+    if (piece.first + 64 * kC <= r.d && (r.pieces - piece.turn) * kW * kT <= places.len) recur_bwd_piece<IO, kGate, kC, kT, kW, kPast, true>(r, places, piece, w, lane, sh);
+    else recur_bwd_piece<IO, kGate, kC, kT, kW, kPast, false>(r, places, piece, w, lane, sh);
 }
 
 namespace {
@@ -422,56 +478,71 @@ int check_recurrence(const bimamba_recurrence_desc* d)
     if (const int rc = check_rows(d->batch, d->seqlen)) return rc;
     if (!known_dtype(d->io_dtype) || (d->gate != BIMAMBA_GATE_LOG && d->gate != BIMAMBA_GATE_SIGMOID)) return BIMAMBA_ERR_UNSUPPORTED;
     if (d->batch > 65535 || d->d_inner > kMaxWidth) return BIMAMBA_ERR_UNSUPPORTED;
-    return BIMAMBA_OK;
+    // (a grid holds 2^32 threads; pieces have 64 steps or more, or there is one)
+    const long long pieces = ((d->seqlen + 63) / 64) * (long long)d->batch * ((d->d_inner + 63) / 64);
+    return d->seqlen > 64 && pieces >= 1ll << 23 ? BIMAMBA_ERR_UNSUPPORTED : BIMAMBA_OK;
 }
 
-constexpr int kTokens = 16, kWaves = 4;   // of a wave in a step; of a workgroup
-
+// Tokens of a wave in a piece, waves of one.  Short sequences go in one piece of as few registers as hold it, since its time is that of one
+// load after the other (512 x 32 tokens of 4096 channels: 8 x 4 4.6 us, 16 x 8 11.0).  Long ones: 16 x 8 forward, 8 x 65536 tokens of 4096
+// channels 388 us (16 x 4 465, 8 x 8 467, 16 x 16 485).  The gradients hold half as much again, so two workgroups of eight waves no
+// longer fit a CU: 16 x 4 476 us (16 x 8 643, 8 x 8 475) where there are more pieces than the chip holds at once, 16 x 8 below (4096 tokens
+// of 2048 channels 26 us, 16 x 4 33: half the pieces to look back at).
 struct RecurPlan {
-    int channels, nseg, seg_len;   // channels a lane
+    int tokens, waves, pieces;
+    int channels;   // a lane
     unsigned tiles;
 };
-RecurPlan plan_recurrence(const bimamba_recurrence_desc* d)
+RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
 {
     RecurPlan p{};
     p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 1 ? 2 : 1;
     p.tiles = (d->d_inner + 64 * p.channels - 1) / (64 * p.channels);
-    const int step = kTokens * kWaves;
-    const long long have = (long long)p.tiles * d->batch, want = 4 * cu_count();
-    const int steps = (d->seqlen + step - 1) / step;
-    p.nseg = (int)(have >= want || steps < 8 ? 1 : (want + have - 1) / have);
-    if (p.nseg > steps / 4) p.nseg = steps / 4 > 0 ? steps / 4 : 1;
-    const int per = (steps + p.nseg - 1) / p.nseg;
-    p.seg_len = per * step;
-    p.nseg = (steps + per - 1) / per;
+    const int L = d->seqlen;
+    const auto pieces = [&](int steps) { return (L + steps - 1) / steps; };
+    if (L == 1 && !back) p.tokens = 1, p.waves = 1;
+    else if (L <= 4) p.tokens = 4, p.waves = 1;
+    else if (L <= 32) p.tokens = 8, p.waves = 4;
+    else if (L <= 64 || (back && (long long)p.tiles * d->batch * pieces(128) > 2 * cu_count())) p.tokens = 16, p.waves = 4;
+    else p.tokens = 16, p.waves = 8;
+    p.pieces = pieces(p.tokens * p.waves);
     return p;
 }
 
-size_t links_bytes(const bimamba_recurrence_desc* d, const RecurPlan& p)
+size_t slots_bytes(const bimamba_recurrence_desc* d, const RecurPlan& p)   // (and the ticket)
 {
-    return p.nseg > 1 ? (size_t)d->batch * p.nseg * 2 * d->d_inner * sizeof(float) : 0;
+    return p.pieces > 1 ? (size_t)d->batch * p.pieces * d->d_inner * 8 + 16 : 0;
 }
 
-template <typename IO, int kGate, int kC>
-void launch_forward(const RecurPlan& p, const RecurArgs& a, int batch, hipStream_t st)
+template <typename IO, int kGate, int kC, bool kPast>
+void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
 {
-    const dim3 grid(p.tiles * p.nseg, batch), wg(64 * kWaves);
-    if (p.nseg > 1) hipLaunchKernelGGL((recur_ends_kernel<IO, kGate, kC, kTokens, kWaves, false>), dim3(p.tiles * (p.nseg - 1), batch), wg, 0, st, a);
-    hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kTokens, kWaves, 1>), grid, wg, 0, st, a);
-}
-template <typename IO, int kGate, int kC>
-void launch_backward(const RecurPlan& p, const RecurArgs& a, int batch, hipStream_t st)
-{
-    const dim3 grid(p.tiles * p.nseg, batch), wg(64 * kWaves);
-    if (p.nseg > 1) hipLaunchKernelGGL((recur_ends_kernel<IO, kGate, kC, kTokens, kWaves, true>), dim3(p.tiles * (p.nseg - 1), batch), wg, 0, st, a);
-    hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kTokens, kWaves, 1>), grid, wg, 0, st, a);
+    // How far a workgroup looks back: what a hop from one state to the next takes has to pass over as many pieces of a sequence as are done
+    // meanwhile, the more the fewer sequences and channels there are; each piece looked at costs words to read.  65536 tokens of 2048
+    // channels: 8 pieces 188 us, 4 199, 2 266; 8 x 8192 of 4096: 1 piece 381 us, 8 395.
+    const int look = (int)(cu_count() / (2u * p.tiles * (unsigned)a.batch));
+    a.look = look < 1 ? 1 : look > kMostLooked ? kMostLooked : look;
+    if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 255) / 256), a.batch), dim3(256), 0, st, a);
+    const dim3 grid(p.tiles * (unsigned)a.batch * p.pieces), wg(64 * p.waves);
+    if (back) {
+        if (p.tokens == 4) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 4, 1, kPast>), grid, wg, 0, st, a);
+        else if (p.tokens == 8) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 8, 4, kPast>), grid, wg, 0, st, a);
+        else if (p.waves == 4) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 16, 4, kPast>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 16, 8, false>), grid, wg, 0, st, a);   // (a few pieces: within the caches)
+    } else {
+        if (p.tokens == 1) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 1, 1, kPast>), grid, wg, 0, st, a);
+        else if (p.tokens == 4) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 4, 1, kPast>), grid, wg, 0, st, a);
+        else if (p.tokens == 8) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 8, 4, kPast>), grid, wg, 0, st, a);
+        else if (p.waves == 4) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 16, 4, kPast>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 16, 8, kPast>), grid, wg, 0, st, a);
+    }
 }
 template <typename IO, int kC>
 void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool back, hipStream_t st)
 {
-    const bool sigmoid = d->gate == BIMAMBA_GATE_SIGMOID;
-    if (back) sigmoid ? launch_backward<IO, kSigmoid, kC>(p, a, d->batch, st) : launch_backward<IO, kLog, kC>(p, a, d->batch, st);
-    else sigmoid ? launch_forward<IO, kSigmoid, kC>(p, a, d->batch, st) : launch_forward<IO, kLog, kC>(p, a, d->batch, st);
+    const bool past = past_caches((back ? 5.0 : 3.0) * d->batch * d->seqlen * d->d_inner * sizeof(typename IO::T));
+    if (d->gate == BIMAMBA_GATE_SIGMOID) past ? launch_pieces<IO, kSigmoid, kC, true>(p, a, back, st) : launch_pieces<IO, kSigmoid, kC, false>(p, a, back, st);
+    else past ? launch_pieces<IO, kLog, kC, true>(p, a, back, st) : launch_pieces<IO, kLog, kC, false>(p, a, back, st);
 }
 void launch(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool back, hipStream_t st)
 {
@@ -498,7 +569,7 @@ extern "C" {
 size_t bimamba_recurrence_workspace_bytes(const bimamba_recurrence_desc* d)
 {
     if (check_recurrence(d) || d->batch == 0 || d->seqlen == 0) return 0;
-    return links_bytes(d, plan_recurrence(d));
+    return slots_bytes(d, plan_recurrence(d, false));
 }
 
 int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
@@ -512,7 +583,7 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
     if (d->batch == 0) return BIMAMBA_OK;
     const int Bt = d->batch, L = d->seqlen, D = d->d_inner, io = d->io_dtype;
     const size_t elem = dtype_bytes(io);
-    const RecurPlan p = L ? plan_recurrence(d) : RecurPlan{};
+    const RecurPlan p = L ? plan_recurrence(d, false) : RecurPlan{};
     const size_t need = bimamba_recurrence_workspace_bytes(d);
     Bytes bx{}, bg{}, badd{}, by{}, bbias, blen, bin, bout, bkept;
     if (L) {
@@ -540,8 +611,9 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
     RecurArgs a{};
     a.x = row_view(x), a.g = row_view(g), a.y = row_view(y);
     if (add) a.add = row_view(add);
-    a.bias = bias, a.lengths = lengths, a.enter = h_in, a.leave = h_out, a.states = states, a.links = static_cast<float*>(workspace);
-    a.L = L, a.d = D, a.nseg = p.nseg, a.seg_len = p.seg_len, a.reverse = d->reverse;
+    a.bias = bias, a.lengths = lengths, a.enter = h_in, a.leave = h_out, a.states = states;
+    a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 2;
+    a.L = L, a.d = D, a.pieces = p.pieces, a.reverse = d->reverse, a.batch = Bt;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
     if (L) {
@@ -556,10 +628,10 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
 size_t bimamba_recurrence_bwd_workspace_bytes(const bimamba_recurrence_desc* d)
 {
     if (check_recurrence(d) || d->batch == 0 || d->seqlen == 0) return 0;
-    const RecurPlan p = plan_recurrence(d);
-    const long long slots = (long long)d->batch * p.nseg;
+    const RecurPlan p = plan_recurrence(d, true);
+    const long long slots = (long long)d->batch * p.pieces;
     const size_t sums = d->gate == BIMAMBA_GATE_SIGMOID && slots > 1 ? (size_t)slots * d->d_inner * sizeof(float) : 0;
-    return links_bytes(d, p) + sums;
+    return slots_bytes(d, p) + sums;
 }
 
 int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
@@ -574,7 +646,7 @@ int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tenso
     const int Bt = d->batch, L = d->seqlen, D = d->d_inner, io = d->io_dtype;
     const bool rows = Bt && L;
     const size_t elem = dtype_bytes(io);
-    const RecurPlan p = rows ? plan_recurrence(d) : RecurPlan{};
+    const RecurPlan p = rows ? plan_recurrence(d, true) : RecurPlan{};
     const size_t need = bimamba_recurrence_bwd_workspace_bytes(d);
     Bytes bx{}, bg{}, by{}, bdx{}, bdg{}, bbias, blen, bkept, bout, bdb, bin;
     if (rows) {
@@ -607,15 +679,15 @@ int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tenso
     }
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
-    const long long slots = rows ? (long long)Bt * p.nseg : 0;
+    const long long slots = rows ? (long long)Bt * p.pieces : 0;
     if (rows) {
         RecurArgs a{};
         a.x = row_view(x), a.g = row_view(g), a.dy = row_view(dy), a.dx = row_view(dx), a.dg = row_view(dg);
         a.bias = bias, a.lengths = lengths, a.enter = dh_out, a.leave = dh_in, a.states = const_cast<float*>(states);
-        a.links = static_cast<float*>(workspace);
-        float* const sums = static_cast<float*>(workspace) + links_bytes(d, p) / sizeof(float);
+        a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 2;
+        float* const sums = static_cast<float*>(workspace) + slots_bytes(d, p) / sizeof(float);
         a.dbias = dbias ? slots > 1 ? sums : dbias : nullptr;
-        a.L = L, a.d = D, a.nseg = p.nseg, a.seg_len = p.seg_len, a.reverse = d->reverse;
+        a.L = L, a.d = D, a.pieces = p.pieces, a.reverse = d->reverse, a.batch = Bt;
         launch(d, p, a, true, st);
         if (dbias && slots > 1) launch_slot_sum(SlotSumArgs{{sums, nullptr}, {dbias, nullptr}, slots, D, D}, 1, st);
     } else {
