@@ -90,6 +90,8 @@ def build(force: bool = True, jobs: int = 8):
     units.append((os.path.join(CSRC, "stack_inst.hip"), os.path.join(OBJ, "stack_inst.o"), []))
     for name in ("embed", "norm", "scores", "clip", "recurrence", "group_norm", "dropout", "slot_sums"):
         units.append((os.path.join(CSRC, name + ".hip"), os.path.join(OBJ, name + ".o"), []))
+    for act in range(4):   # (of the group norm)
+        units.append((os.path.join(CSRC, "group_norm_inst.hip"), os.path.join(OBJ, "group_norm_a%d.o" % act), ["-DBM_ACT=%d" % act]))
     todo = [u for u in units if force or not os.path.exists(u[1]) or os.path.getmtime(u[1]) < newest_dep(u[0])]
     cmds = [["hipcc"] + FLAGS + extra + ["-c", src, "-o", obj] for src, obj, extra in todo]
     with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds) + 1))) as ex:

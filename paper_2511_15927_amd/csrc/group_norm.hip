@@ -1,319 +1,12 @@
-// The norm of groups of channels with an activation or a gate, and its gradients.
+// The norm of groups of channels with an activation or a gate, and its gradients: checks, plan and entry points.
+#include "group_norm.h"
 #include "slot_sums.h"
 
 namespace bm {
-
-// A token's group stays in registers: 2^k lanes hold it in pieces of 16 bytes, up to 32 elements a lane, so a wave has 64 / lanes
-// neighbouring groups of a row in hand (one, with four waves to it, beyond 2048 channels).  It takes rows one after the other with weight
-// and bias in registers; the gradients' sums for these two stay there as well and are left in a slot at the end.  The statistics are taken
-// over the registers, the mean before the squares around it, so that a large mean costs no digits.  All arithmetic is fp32, each
-// output is rounded once.
-struct GroupNormArgs {
-    RowView x, z, y, dy, dx, dz;
-    const float *weight, *bias;   // null: 1, 0
-    float *mean, *rstd;           // [rows][G]; forward: null, not wanted
-    float *dw, *db;               // sums of a row group, null: not wanted
-    long long slot;               // from one row group's to the next one's
-    unsigned L, rows, per_wave;   // rows that a wave (or the four of a wide group) takes
-    int G, n, d, lanes;           // groups, channels of one; lanes that hold one
-    int centred;
-    float eps;
-};
-enum Act { kPlain = BIMAMBA_ACT_NONE, kSilu = BIMAMBA_ACT_SILU, kBefore = BIMAMBA_ACT_GATE_BEFORE, kAfter = BIMAMBA_ACT_GATE_AFTER };
-
-__device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
-
-// Two values summed over each run of `lanes` lanes, the same in all of a run.
-__device__ __forceinline__ void run_sum(float& u, float& v, int lanes)
-{
-#define BM_DPP(x, ctrl) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xf, 0xf, true))
-    if (lanes < 2) return;
-    u += BM_DPP(u, 0xB1), v += BM_DPP(v, 0xB1);     // quad_perm 1 0 3 2
-    if (lanes < 4) return;
-    u += BM_DPP(u, 0x4E), v += BM_DPP(v, 0x4E);     // quad_perm 2 3 0 1
-    if (lanes < 8) return;
-    u += BM_DPP(u, 0x141), v += BM_DPP(v, 0x141);   // row_half_mirror
-    if (lanes < 16) return;
-    u += BM_DPP(u, 0x140), v += BM_DPP(v, 0x140);   // row_mirror
-#undef BM_DPP
-    if (lanes < 32) return;
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(u), false, false);
-    u = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    if (lanes < 64) return;
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(u), __float_as_uint(u), false, false);
-    u = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// The sums of a group from those of its lanes; kWaves 4: over the waves as well, two barriers apart from the next use of the same turn.
-template <int kWaves>
-struct GroupSum {
-    float2 part[2][kWaves];
-    __device__ __forceinline__ void operator()(float& u, float& v, int lanes, int wave, int turn)
-    {
-        run_sum(u, v, lanes);
-        if constexpr (kWaves > 1) {
-            part[turn][wave] = make_float2(u, v);
-            __syncthreads();
-            u = part[turn][0].x, v = part[turn][0].y;
-#pragma unroll
-            for (int k = 1; k < kWaves; k++) u += part[turn][k].x, v += part[turn][k].y;
-        }
-    }
-};
-
-// Where a lane's elements lie and which rows its wave takes.
-template <int kWaves, int kPieces, int kPiece>
-struct GroupPlace {
-    int g, in, n, stride;
-    bool real, whole;   // whether the lane's group exists; (wave-uniform) every piece of every lane lies within its group
-    unsigned r0, r1;
-    __device__ __forceinline__ GroupPlace(const GroupNormArgs& a, int lane, int wave) : n(a.n)
-    {
-        const int runs = 64 / a.lanes, first = blockIdx.x * runs;
-        g = first + lane / a.lanes;
-        real = g < a.G;
-        g = min(g, a.G - 1);
-        in = (lane % a.lanes + (kWaves > 1 ? wave * kPieces * 64 : 0)) * kPiece;
-        stride = a.lanes * kPiece;
-        whole = first + runs <= a.G && a.n == kWaves * kPieces * stride;
-        const unsigned group = kWaves == 1 ? blockIdx.y * 4 + wave : blockIdx.y;
-        r0 = min(group * a.per_wave, a.rows);
-        r1 = min(r0 + a.per_wave, a.rows);
-    }
-    __device__ __forceinline__ int at(int k) const { return in + k * stride; }
-    __device__ __forceinline__ int channel() const { return g * n; }
-    template <typename IO>
-    __device__ __forceinline__ void load(Piece<IO, kPiece> (&p)[kPieces], const RowView& v, unsigned b, unsigned t) const
-    {
-        const typename IO::T* const row = static_cast<const typename IO::T*>(v.p) + row_offset(v, b, t) + channel();
-#pragma unroll
-        for (int k = 0; k < kPieces; k++) p[k] = load_clamped<IO, kPiece>(row, at(k), n);
-    }
-    template <typename IO>
-    __device__ __forceinline__ void settled(Piece<IO, kPiece> (&p)[kPieces]) const
-    {
-        if (whole) return;
-#pragma unroll
-        for (int k = 0; k < kPieces; k++) settle(p[k], at(k), n, typename IO::T(0));
-    }
-    template <typename IO>
-    __device__ __forceinline__ void store(const RowView& v, unsigned b, unsigned t, const float (&f)[kPieces][kPiece]) const
-    {
-        typename IO::T* const row = static_cast<typename IO::T*>(v.p) + row_offset(v, b, t) + channel();
-#pragma unroll
-        for (int k = 0; k < kPieces; k++) {
-            if (whole) store_piece<IO>(row + at(k), f[k]);
-            else if (real) store_piece_of<IO>(row, at(k), n, f[k]);
-        }
-    }
-    __device__ __forceinline__ void params(float (&f)[kPieces][kPiece], const float* p, float missing) const
-    {
-#pragma unroll
-        for (int k = 0; k < kPieces; k++) {
-            if (p) load_floats(f[k], p + channel(), at(k), n, 0.0f);
-            else
-#pragma unroll
-                for (int i = 0; i < kPiece; i++) f[k][i] = missing;
-        }
-    }
-};
-
-template <typename IO, int kAct, int kWaves, int kPieces, int kPiece>
-__device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
-{
-    __shared__ GroupSum<kWaves> sum;
-    constexpr bool kGated = kAct == kBefore || kAct == kAfter;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const GroupPlace<kWaves, kPieces, kPiece> place(a, lane, wave);
-    if (place.r0 >= place.r1) return;   // (with four waves to a group: the whole workgroup)
-    float w[kPieces][kPiece], c[kPieces][kPiece];
-    place.params(w, a.weight, 1.0f);
-    place.params(c, a.bias, 0.0f);
-    const float inv = 1.0f / a.n;
-    unsigned b = place.r0 / a.L, t = place.r0 - b * a.L;
-    Piece<IO, kPiece> px[kPieces], pz[kPieces];
-    place.template load<IO>(px, a.x, b, t);
-    if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
-    for (unsigned r = place.r0; r < place.r1; r++) {
-        float u[kPieces][kPiece], gate[kPieces][kPiece], s0 = 0.0f, s1 = 0.0f;
-        place.template settled<IO>(px);
-        if constexpr (kGated) place.template settled<IO>(pz);
-#pragma unroll
-        for (int k = 0; k < kPieces; k++)
-#pragma unroll
-            for (int i = 0; i < kPiece; i++) {
-                u[k][i] = px[k][i];
-                if constexpr (kGated) gate[k][i] = pz[k][i] * sigmoid_of(pz[k][i]);
-                if constexpr (kAct == kBefore) u[k][i] *= gate[k][i];
-                s0 += u[k][i];
-                s1 += u[k][i] * u[k][i];
-            }
-        const unsigned b0 = b, t0 = t;
-        if (++t == a.L) t = 0, b++;
-        if (r + 1 < place.r1) {
-            place.template load<IO>(px, a.x, b, t);
-            if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
-        }
-        sum(s0, s1, a.lanes, wave, 0);
-        float mean = 0.0f;
-        if (a.centred) {
-            mean = s0 * inv;
-            s0 = s1 = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kPieces; k++)
-#pragma unroll
-                for (int i = 0; i < kPiece; i++) {
-                    u[k][i] -= mean;
-                    s1 += place.whole || place.at(k) + i < a.n ? u[k][i] * u[k][i] : 0.0f;
-                }
-            sum(s0, s1, a.lanes, wave, 1);
-        } else if constexpr (kWaves > 1) {
-            __syncthreads();
-        }
-        const float rstd = 1.0f / sqrtf(s1 * inv + a.eps);
-#pragma unroll
-        for (int k = 0; k < kPieces; k++)
-#pragma unroll
-            for (int i = 0; i < kPiece; i++) {
-                const float v = u[k][i] * rstd * w[k][i] + c[k][i];
-                u[k][i] = kAct == kSilu ? v * sigmoid_of(v) : kAct == kAfter ? v * gate[k][i] : v;
-            }
-        place.template store<IO>(a.y, b0, t0, u);
-        if (place.real && lane % a.lanes == 0 && (kWaves == 1 || wave == 0)) {
-            if (a.mean) a.mean[(long long)r * a.G + place.g] = mean;
-            if (a.rstd) a.rstd[(long long)r * a.G + place.g] = rstd;
-        }
-    }
-}
-
-template <typename IO, int kAct, int kWaves, int kPieces, int kPiece>
-__device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
-{
-    __shared__ GroupSum<kWaves> sum;
-    constexpr bool kGated = kAct == kBefore || kAct == kAfter;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const GroupPlace<kWaves, kPieces, kPiece> place(a, lane, wave);   // (r0 >= r1: a wave without rows, which leaves zeros)
-    float w[kPieces][kPiece], c[kPieces][kPiece], dw[kPieces][kPiece], db[kPieces][kPiece];
-    place.params(w, a.weight, 1.0f);
-    if constexpr (kAct == kSilu || kAct == kAfter) place.params(c, a.bias, 0.0f);
-#pragma unroll
-    for (int k = 0; k < kPieces; k++)
-#pragma unroll
-        for (int i = 0; i < kPiece; i++) dw[k][i] = db[k][i] = 0.0f;
-    const float inv = 1.0f / a.n;
-    unsigned b = place.r0 / a.L, t = place.r0 - b * a.L;
-    for (unsigned r = place.r0; r < place.r1; r++) {
-        Piece<IO, kPiece> px[kPieces], pz[kPieces], pd[kPieces];
-        place.template load<IO>(px, a.x, b, t);
-        if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
-        place.template load<IO>(pd, a.dy, b, t);
-        const float mean = a.centred ? a.mean[(long long)r * a.G + place.g] : 0.0f, rstd = a.rstd[(long long)r * a.G + place.g];
-        place.template settled<IO>(px);
-        if constexpr (kGated) place.template settled<IO>(pz);
-        place.template settled<IO>(pd);
-        // xh, and k = dv * weight; what dz needs beside them
-        float xh[kPieces][kPiece], g[kPieces][kPiece], dz[kPieces][kPiece], gate[kPieces][kPiece], s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kPieces; k++)
-#pragma unroll
-            for (int i = 0; i < kPiece; i++) {
-                float u = px[k][i], dv = pd[k][i];
-                if constexpr (kGated) {
-                    const float z = pz[k][i], s = sigmoid_of(z);
-                    gate[k][i] = z * s;
-                    dz[k][i] = s * (1.0f + z * (1.0f - s));
-                    if constexpr (kAct == kBefore) u *= gate[k][i];
-                }
-                xh[k][i] = (u - mean) * rstd;
-                if constexpr (kAct == kSilu || kAct == kAfter) {
-                    const float v = xh[k][i] * w[k][i] + c[k][i];
-                    if constexpr (kAct == kSilu) {
-                        const float s = sigmoid_of(v);
-                        dv *= s * (1.0f + v * (1.0f - s));
-                    } else {
-                        dz[k][i] *= dv * v;
-                        dv *= gate[k][i];
-                    }
-                }
-                dw[k][i] += dv * xh[k][i];
-                db[k][i] += dv;
-                g[k][i] = dv * w[k][i];
-                s0 += g[k][i];
-                s1 += g[k][i] * xh[k][i];
-            }
-        sum(s0, s1, a.lanes, wave, (r - place.r0) & 1);
-        const float c0 = a.centred ? s0 * inv : 0.0f, c1 = s1 * inv;
-#pragma unroll
-        for (int k = 0; k < kPieces; k++)
-#pragma unroll
-            for (int i = 0; i < kPiece; i++) {
-                const float du = rstd * (g[k][i] - c0 - xh[k][i] * c1);
-                if constexpr (kAct == kBefore) {
-                    dz[k][i] *= du * px[k][i];
-                    g[k][i] = du * gate[k][i];
-                } else {
-                    g[k][i] = du;
-                }
-            }
-        place.template store<IO>(a.dx, b, t, g);
-        if constexpr (kGated) place.template store<IO>(a.dz, b, t, dz);
-        if (++t == a.L) t = 0, b++;
-    }
-    const long long slot = (long long)blockIdx.y * a.slot + place.channel();
-    if constexpr (kWaves > 1) {
-#pragma unroll
-        for (int k = 0; k < kPieces; k++) {
-            if (a.dw) store_piece_of<IoF32>(a.dw + slot, place.at(k), a.n, dw[k]);
-            if (a.db) store_piece_of<IoF32>(a.db + slot, place.at(k), a.n, db[k]);
-        }
-    } else {   // four waves' sums of the same channels: one of the two at a time through shared memory
-        __shared__ float all[4][kPieces * kPiece][64];
-#pragma unroll
-        for (int which = 0; which < 2; which++) {
-            float* const to = which ? a.db : a.dw;
-            if (!to) continue;   // (all threads)
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kPieces; k++)
-#pragma unroll
-                for (int i = 0; i < kPiece; i++) all[wave][k * kPiece + i][lane] = which ? db[k][i] : dw[k][i];
-            __syncthreads();
-            if (wave != 0 || !place.real) continue;
-#pragma unroll
-            for (int k = 0; k < kPieces; k++) {
-                float f[kPiece];
-#pragma unroll
-                for (int i = 0; i < kPiece; i++) {
-                    const int e = k * kPiece + i;
-                    f[i] = (all[0][e][lane] + all[1][e][lane]) + (all[2][e][lane] + all[3][e][lane]);
-                }
-                store_piece_of<IoF32>(to + slot, place.at(k), a.n, f);
-            }
-        }
-    }
-}
-
-template <typename IO, int kAct, int kWaves, int kPieces>
-__global__ __launch_bounds__(256) void group_norm_kernel(const GroupNormArgs a)
-{
-    if constexpr (kWaves == 1 && kPieces == 1) {   // (groups smaller than a piece: an element a lane)
-        if (a.n < kPieceOf<IO>) return group_norm_rows<IO, kAct, 1, 1, 1>(a);
-    }
-    group_norm_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>>(a);
-}
-template <typename IO, int kAct, int kWaves, int kPieces>
-__global__ __launch_bounds__(256) void group_norm_bwd_kernel(const GroupNormArgs a)
-{
-    if constexpr (kWaves == 1 && kPieces == 1) {
-        if (a.n < kPieceOf<IO>) return group_norm_bwd_rows<IO, kAct, 1, 1, 1>(a);
-    }
-    group_norm_bwd_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>>(a);
-}
-
+template <> void launch_group_norm<BIMAMBA_ACT_NONE>(const GroupPlan&, const GroupNormArgs&, bool, bool, bool, hipStream_t);
+template <> void launch_group_norm<BIMAMBA_ACT_SILU>(const GroupPlan&, const GroupNormArgs&, bool, bool, bool, hipStream_t);
+template <> void launch_group_norm<BIMAMBA_ACT_GATE_BEFORE>(const GroupPlan&, const GroupNormArgs&, bool, bool, bool, hipStream_t);
+template <> void launch_group_norm<BIMAMBA_ACT_GATE_AFTER>(const GroupPlan&, const GroupNormArgs&, bool, bool, bool, hipStream_t);
 namespace {
 
 constexpr int kMaxWidth = 65536, kMaxGroup = 8192;
@@ -329,71 +22,45 @@ int check_group_norm(const bimamba_group_norm_desc* d)
 }
 bool gated(const bimamba_group_norm_desc* d) { return d->act == BIMAMBA_ACT_GATE_BEFORE || d->act == BIMAMBA_ACT_GATE_AFTER; }
 
-struct GroupPlan {
-    int waves, pieces, lanes;
-    unsigned tiles, row_groups, per_wave;
-};
 GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
 {
     GroupPlan p{};
     const int n = d->d_inner / d->groups, piece = d->io_dtype == BIMAMBA_BF16 ? 8 : 4;
     const int pieces = n < piece ? n : (n + piece - 1) / piece;   // (of one element in small groups)
-    p.waves = n > 64 * 32 ? 4 : 1;
+    // 16 elements a lane at most: 32 of them and the gradients' sums take the registers of half the waves (32768 x 2 groups of 2048, gated: four
+    // waves to a group 130 us, one 139; gradients 234, 265; groups of 8192: eight waves 279, four 296; gradients 496, 605)
+    p.waves = n <= 1024 ? 1 : n <= 2048 ? 4 : 8;
     p.lanes = 1;
     while (p.lanes < 64 && p.lanes < pieces) p.lanes *= 2;
     p.pieces = 1;
     while (p.pieces * p.lanes * p.waves < pieces) p.pieces *= 2;
     const int runs = 64 / p.lanes;
     p.tiles = (d->groups + runs - 1) / runs;
-    const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = p.waves == 1 ? 4 : 1, want = (bwd ? 8u : 16u) * cu_count();
-    unsigned groups = (want + p.tiles - 1) / p.tiles;
-    if (bwd && groups > rows / 8) groups = rows / 8 ? rows / 8 : 1;   // (each leaves a slot as long as two rows)
-    p.per_wave = (rows + groups * together - 1) / (groups * together);
-    if (p.per_wave < 1) p.per_wave = 1;
+    p.team = p.waves > 1 ? p.waves : bwd && p.pieces == 1 ? 8 : 4;
+    // Rows: as many as are in hand at once go to one wave each, up to four where there are more (sixteen for the gradients of shared groups, which
+    // otherwise leave a slot as long as two rows for every few of them).
+    const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = p.waves == 1 ? p.team : 1;
+    const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 8u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 16 : 4;
+    p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);
+    // (a grid's second axis ends at 65535)
+    const unsigned long long least = (rows + 65535ull * together - 1) / (65535ull * together);
+    if (p.per_wave < least) p.per_wave = (unsigned)least;
     const unsigned long long step = (unsigned long long)p.per_wave * together;
     p.row_groups = (unsigned)((rows + step - 1) / step);
     return p;
 }
 
-template <typename IO, int kAct, int kWaves, int kPieces>
-void launch_one(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
-{
-    const dim3 grid(p.tiles, p.row_groups), wg(256);
-    if (bwd) hipLaunchKernelGGL((group_norm_bwd_kernel<IO, kAct, kWaves, kPieces>), grid, wg, 0, st, a);
-    else hipLaunchKernelGGL((group_norm_kernel<IO, kAct, kWaves, kPieces>), grid, wg, 0, st, a);
-}
-template <typename IO, int kAct>
-void launch_act(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
-{
-    constexpr bool kWide = sizeof(typename IO::T) == 4;   // (twice the pieces for as many elements)
-    if (p.waves == 4) {
-        if (kWide ? p.pieces <= 4 : p.pieces <= 2) launch_one<IO, kAct, 4, kWide ? 4 : 2>(p, a, bwd, st);
-        else launch_one<IO, kAct, 4, kWide ? 8 : 4>(p, a, bwd, st);
-        return;
-    }
-    switch (p.pieces) {
-        case 1: launch_one<IO, kAct, 1, 1>(p, a, bwd, st); break;
-        case 2: launch_one<IO, kAct, 1, 2>(p, a, bwd, st); break;
-        case 4: launch_one<IO, kAct, 1, 4>(p, a, bwd, st); break;
-        default: if constexpr (kWide) launch_one<IO, kAct, 1, 8>(p, a, bwd, st);
-    }
-}
-template <typename IO>
-void launch_io(const bimamba_group_norm_desc* d, const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
-{
-    switch (d->act) {
-        case BIMAMBA_ACT_NONE: launch_act<IO, kPlain>(p, a, bwd, st); break;
-        case BIMAMBA_ACT_SILU: launch_act<IO, kSilu>(p, a, bwd, st); break;
-        case BIMAMBA_ACT_GATE_BEFORE: launch_act<IO, kBefore>(p, a, bwd, st); break;
-        default: launch_act<IO, kAfter>(p, a, bwd, st);
-    }
-}
 void launch(const bimamba_group_norm_desc* d, const GroupPlan& p, GroupNormArgs& a, bool bwd, hipStream_t st)
 {
     a.L = d->seqlen, a.rows = (unsigned)((long long)d->batch * d->seqlen), a.per_wave = p.per_wave;
     a.G = d->groups, a.n = d->d_inner / d->groups, a.d = d->d_inner, a.lanes = p.lanes, a.centred = d->centred, a.eps = d->eps;
-    if (d->io_dtype == BIMAMBA_BF16) launch_io<IoBF16>(d, p, a, bwd, st);
-    else launch_io<IoF32>(d, p, a, bwd, st);
+    const bool bf16 = d->io_dtype == BIMAMBA_BF16, past = past_caches((bwd ? 3.0 : 2.0) * a.rows * a.d * dtype_bytes(d->io_dtype));
+    switch (d->act) {
+        case BIMAMBA_ACT_NONE: launch_group_norm<BIMAMBA_ACT_NONE>(p, a, bf16, past, bwd, st); break;
+        case BIMAMBA_ACT_SILU: launch_group_norm<BIMAMBA_ACT_SILU>(p, a, bf16, past, bwd, st); break;
+        case BIMAMBA_ACT_GATE_BEFORE: launch_group_norm<BIMAMBA_ACT_GATE_BEFORE>(p, a, bf16, past, bwd, st); break;
+        default: launch_group_norm<BIMAMBA_ACT_GATE_AFTER>(p, a, bf16, past, bwd, st);
+    }
 }
 
 int check_params(const float* p, long long count, Bytes* r)

@@ -620,7 +620,7 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
         launch(d, p, a, false, st);
     } else if (h_out && h_out != h_in) {
         // (no token: the state goes through; a sum of one slot, or of none)
-        launch_slot_sum(SlotSumArgs{{h_in, nullptr}, {h_out, nullptr}, h_in ? 1 : 0, D, D}, Bt, st);
+        launch_slot_sum(SlotSumArgs{{const_cast<float*>(h_in), nullptr}, {h_out, nullptr}, h_in ? 1 : 0, D, D}, Bt, st);
     }
     return launches.status();
 }
@@ -691,7 +691,7 @@ int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tenso
         launch(d, p, a, true, st);
         if (dbias && slots > 1) launch_slot_sum(SlotSumArgs{{sums, nullptr}, {dbias, nullptr}, slots, D, D}, 1, st);
     } else {
-        if (Bt && dh_in && dh_in != dh_out) launch_slot_sum(SlotSumArgs{{dh_out, nullptr}, {dh_in, nullptr}, dh_out ? 1 : 0, D, D}, Bt, st);
+        if (Bt && dh_in && dh_in != dh_out) launch_slot_sum(SlotSumArgs{{const_cast<float*>(dh_out), nullptr}, {dh_in, nullptr}, dh_out ? 1 : 0, D, D}, Bt, st);
         if (dbias) launch_slot_sum(SlotSumArgs{{nullptr, nullptr}, {dbias, nullptr}, 0, D, D}, 1, st);
     }
     return launches.status();
