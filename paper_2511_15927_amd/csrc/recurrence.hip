@@ -28,8 +28,8 @@ struct RecurArgs {
     float* states;           // [batch][ceil(L / kKeep)][d] or null
     float* dbias;            // [batch * pieces][d] or null
     unsigned long long* slots;   // [batch][pieces][d], with several pieces: what enters the first one, then what each leaves, in the order of the walk
-    unsigned* ticket;
-    int L, d, pieces, reverse, batch, look;   // look: pieces before its own that a workgroup looks at
+    unsigned* ticket;        // [kXcds]
+    int L, d, pieces, reverse, batch, queues, look;   // look: pieces before its own that a workgroup looks at
 };
 
 // The tokens that the steps of a walk take.
@@ -49,18 +49,20 @@ struct Places {
     __device__ __forceinline__ int written(int s) const { return reverse && s < len ? len - 1 - s : s; }
 };
 
-// A lane's channels of the rows that a wave's steps take.  kWhole: all of them exist and lie within the sequence; nothing is clamped, and there
-// is no branch.  Rows are wave-uniform pointers and lanes unsigned 32-bit offsets, kept narrow where they are used, so that the
-// accesses take a scalar base: sixteen tokens of two tensors in flight otherwise hold sixty registers of addresses.
+// A lane's channels of the rows that a wave's steps take.  Lanes beyond the last channels take those along with their owner, and store nothing;
+// where the last lane's channels would reach beyond the row it takes the row's last ones and stores those that are its own.
+// kWhole: every lane owns all of its channels and all steps lie within the sequence; nothing is clamped, and there is no branch.  Rows are
+// wave-uniform pointers and lanes unsigned 32-bit offsets, kept narrow where they are used, so that the accesses take a scalar base:
+// sixteen tokens of two tensors in flight otherwise hold sixty registers of addresses.
 template <typename IO, int kC, int kT, bool kPast, bool kWhole>
 struct Steps {
     typedef typename IO::T T;
     typedef Piece<IO, kC> Raw;
     const Places& places;
-    int b, s0, L, at, d;
-    unsigned off;   // bytes; the last channels of a row are loaded whole and moved into place
+    int b, s0, L, at, own;   // own: the first channel that is the lane's, at + kC if none is
+    unsigned off;            // bytes
     __device__ __forceinline__ Steps(const Places& places, int b, int s0, int L, int first, int lane, int d)
-        : places(places), b(b), s0(s0), L(L), at(first + lane * kC), d(d), off((unsigned)min(at, d - kC) * (unsigned)sizeof(T)) {}
+        : places(places), b(b), s0(s0), L(L), at(min(first + lane * kC, d - kC)), own(min(first + lane * kC, d)), off((unsigned)at * (unsigned)sizeof(T)) {}
     static __device__ __forceinline__ char* row(const RowView& v, int b, int t) { return static_cast<char*>(v.p) + row_offset(v, b, t) * (long long)sizeof(T); }
     __device__ __forceinline__ unsigned narrow() const
     {
@@ -69,22 +71,16 @@ struct Steps {
         return o;
     }
     __device__ __forceinline__ bool inside(int i) const { return kWhole || s0 + i < places.len; }
+    __device__ __forceinline__ bool idle() const { return !kWhole && s0 >= places.len; }   // (the whole wave)
     __device__ __forceinline__ void load(Raw (&r)[kT], const RowView& v) const
     {
         const char* p = row(v, b, places.readable(s0));
         const long long step = (places.reverse ? -v.st : v.st) * (long long)sizeof(T);
 #pragma unroll
         for (int i = 0; i < kT; i++) {
-            if constexpr (kWhole) {
-                r[i] = load_piece<IO, kC, kPast>(reinterpret_cast<const T*>(p + narrow()));
-                p += step;
-            } else {
-                r[i] = load_piece<IO, kC, kPast>(reinterpret_cast<const T*>(row(v, b, places.readable(s0 + i)) + off));
-            }
-        }
-        if constexpr (!kWhole) {
-#pragma unroll
-            for (int i = 0; i < kT; i++) settle(r[i], at, d, T(0));
+            if constexpr (!kWhole) p = row(v, b, places.readable(s0 + i));
+            r[i] = load_piece<IO, kC, kPast>(reinterpret_cast<const T*>(p + narrow()));
+            if constexpr (kWhole) p += step;
         }
     }
     __device__ __forceinline__ void store(const RowView& v, int i, const float (&f)[kC]) const
@@ -92,22 +88,22 @@ struct Steps {
         if constexpr (kWhole) {
             store_piece<IO, kPast>(reinterpret_cast<T*>(row(v, b, places.written(s0)) + (places.reverse ? -i : i) * v.st * (long long)sizeof(T) + narrow()), f);
         } else if (s0 + i < L) {
-            store_piece_of<IO>(reinterpret_cast<T*>(row(v, b, places.written(s0 + i))), at, d, f);
+            T* const to = reinterpret_cast<T*>(row(v, b, places.written(s0 + i)) + narrow());
+            if (own == at) store_piece<IO, kPast>(to, f);
+            else if (kC == 2 && own == at + 1) to[kC - 1] = io_value<IO>(f[kC - 1]);
         }
     }
     __device__ __forceinline__ void load_params(float (&f)[kC], const float* p) const
     {
+#pragma unroll
+        for (int j = 0; j < kC; j++) f[j] = 0.0f;
         if (p) {
-            Piece<IoF32, kC> v = load_piece<IoF32, kC>(p + min(at, d - kC));
-            if constexpr (!kWhole) settle(v, at, d, 0.0f);
+            const Piece<IoF32, kC> v = load_piece<IoF32, kC>(p + at);
 #pragma unroll
             for (int j = 0; j < kC; j++) f[j] = v[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < kC; j++) f[j] = 0.0f;
         }
     }
-    __device__ __forceinline__ bool has(int j) const { return kWhole || at + j < d; }
+    __device__ __forceinline__ bool has(int j) const { return kWhole || at + j >= own; }
     __device__ __forceinline__ void store_params(float* p, const float (&f)[kC]) const
     {
 #pragma unroll
@@ -155,53 +151,63 @@ __device__ __forceinline__ void publish(unsigned long long* to, float p, float e
 // What a link makes of the state that enters it.  (One that nothing passes ends there, so that the word (0, h) stands for the state h itself.)
 __device__ __forceinline__ float through(float p, float e, float h) { return p == 0.0f ? e : p * h + e; }
 
-// Waits for a piece's words, `end`: for those of the state that it leaves.  (Were they not to come, which would be a mistake here, the walk
-// would go on with a NaN, not stand still.)
-template <int kC, typename At>
-__device__ __forceinline__ Link<kC> await(const unsigned long long* from, const At& steps, bool end)
+// Waits for the words of pieces that lie `stride` slots apart, of `end`'s for those of the state that it leaves.  (Were they not to come, which
+// would be a mistake here, the walk would go on with a NaN, not stand still.)
+template <int kC, int kN, typename At>
+__device__ __forceinline__ void await(Link<kC> (&links)[kN], int n, const unsigned long long* from, long long stride, int end, const At& steps)
 {
-    Link<kC> link;
-    unsigned long long word[kC];
-    const auto there = [&](int j) {
-        const unsigned hi = (unsigned)(word[j] >> 32);
-        return end ? hi == 0 : hi != kNothing;
+    unsigned long long word[kN][kC];
+    const auto there = [&](int k, int j) {
+        const unsigned hi = (unsigned)(word[k][j] >> 32);
+        return min(k, n - 1) == end ? hi == 0 : hi != kNothing;
     };
     int tries = 1 << 22;
     for (;;) {
         bool all = true;
 #pragma unroll
-        for (int j = 0; j < kC; j++) {
-            word[j] = steps.has(j) ? __hip_atomic_load(from + steps.at + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
-            all &= there(j);
-        }
+        for (int k = 0; k < kN; k++)
+#pragma unroll
+            for (int j = 0; j < kC; j++)
+                word[k][j] = __hip_atomic_load(from + min(k, n - 1) * stride + steps.at + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int k = 0; k < kN; k++)
+#pragma unroll
+            for (int j = 0; j < kC; j++) all &= there(k, j);
         if (__all(all) || --tries == 0) break;
         __builtin_amdgcn_s_sleep(1);
     }
 #pragma unroll
-    for (int j = 0; j < kC; j++) {
-        link.p[j] = there(j) ? __uint_as_float((unsigned)(word[j] >> 32)) : 0.0f;
-        link.e[j] = there(j) ? __uint_as_float((unsigned)word[j]) : __builtin_nanf("");
-    }
-    return link;
+    for (int k = 0; k < kN; k++)
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            links[k].p[j] = there(k, j) ? __uint_as_float((unsigned)(word[k][j] >> 32)) : 0.0f;
+            links[k].e[j] = there(k, j) ? __uint_as_float((unsigned)word[k][j]) : __builtin_nanf("");
+        }
 }
+// Chains (the channels of a wave, of one sequence) are handed out from one queue or from eight, each a run of neighbouring ones for the
+// workgroups of one XCD (and, when that is empty, for the others): the first chain of queue q.  (A launch has fewer than 2^26 chains.)
+constexpr unsigned kXcds = 8;
+__device__ __forceinline__ unsigned queue_of(unsigned chains, unsigned q, unsigned queues) { return queues == 1 ? q * chains : q * chains / kXcds; }
 // Before the pieces: nothing is there but what enters the first one.  (The state that enters is read here only: it may be the one that the
 // last piece replaces.)
 __global__ __launch_bounds__(256) void recur_clear_kernel(const RecurArgs r)
 {
     const long long n = (long long)r.pieces * r.d, i = blockIdx.x * 256ll + threadIdx.x;
     const int b = blockIdx.y;
-    if (i == 0 && b == 0) *r.ticket = 0;
+    if (i < kXcds && b == 0) r.ticket[i] = 0;
     if (i >= n) return;
     r.slots[b * n + i] = i < r.d ? (r.enter ? __float_as_uint(r.enter[(long long)b * r.d + i]) : 0) : ~0ull;
 }
 
 // What a workgroup's waves share.
-constexpr int kMostLooked = 8;
-template <int kC, int kW>
+template <int kC, int kT, int kW>
 struct PieceShared {
-    Link<kC> part[kW][64], seen[kMostLooked][64];
-    float before[kW][kC][64];   // (gradients)
-    unsigned ticket;
+    static constexpr bool kOnly = kT * kW <= 32;        // (short sequences: there is one piece)
+    static constexpr int kMostLooked = kW < 8 ? 8 : kW;   // pieces before its own that a workgroup looks at
+    Link<kC> part[kW][64], seen[kOnly ? 1 : kMostLooked][64];
+    float before[kW][kC][64];                      // (gradients)
+    int turn;
+    unsigned chain;
 };
 // Which piece it is, of how many channels and where.
 struct PieceOf {
@@ -209,28 +215,47 @@ struct PieceOf {
     template <typename Shared>
     __device__ __forceinline__ PieceOf(const RecurArgs& r, int channels, Shared& sh)
     {
-        unsigned n = blockIdx.x;
-        if (r.pieces > 1) {
-            if (threadIdx.x == 0) sh.ticket = atomicAdd(r.ticket, 1u);
-            __syncthreads();
-            n = __builtin_amdgcn_readfirstlane(sh.ticket);
-        }
         const unsigned tiles = (r.d + channels - 1) / channels, chains = tiles * r.batch;
-        turn = n / chains;
-        b = n % chains / tiles;
-        first = n % tiles * channels;
+        unsigned chain = blockIdx.x;
+        turn = 0;
+        if (!Shared::kOnly && r.pieces > 1) {
+            if (threadIdx.x == 0) {
+                // (there are as many pieces as workgroups, and each takes one: a queue that is not empty is found)
+                constexpr int kXccId = 20 | 3 << 11;   // (hardware register XCC_ID, four bits)
+                unsigned q = r.queues > 1 ? __builtin_amdgcn_s_getreg(kXccId) % kXcds : 0, n, of;
+                for (;; q = q + 1 == (unsigned)r.queues ? 0 : q + 1) {
+                    of = queue_of(chains, q + 1, r.queues) - queue_of(chains, q, r.queues);
+                    n = atomicAdd(r.ticket + q, 1u);
+                    if (n < of * r.pieces) break;
+                }
+                sh.turn = n / of;
+                sh.chain = queue_of(chains, q, r.queues) + n % of;
+            }
+            __syncthreads();
+            turn = __builtin_amdgcn_readfirstlane(sh.turn), chain = __builtin_amdgcn_readfirstlane(sh.chain);
+        }
+        b = chain / tiles;
+        first = chain % tiles * channels;
     }
 };
 // What enters the piece: the state that the r.look-th piece before it leaves, and the links of those between, folded in the order of the walk.
 // The state that a piece leaves is this same fold, one link further, so its bits do not depend on how far back the look went or on
 // which of the words were there.  A sequence of one piece has read what enters it beside its tokens, before a barrier: the same memory may
 // be written at its end.
-template <int kC, int kW, typename At>
-__device__ __forceinline__ void look_back(float (&carry)[kC], const At& steps, const RecurArgs& r, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
+template <int kC, int kT, int kW, typename At>
+__device__ __forceinline__ void look_back(float (&carry)[kC], const At& steps, const RecurArgs& r, const PieceOf& piece, int w, int lane, PieceShared<kC, kT, kW>& sh)
 {
     const unsigned long long* const slots = r.slots + (long long)piece.b * r.pieces * r.d;
     const int look = min(r.look, piece.turn + 1);   // (slot `turn` is what the piece before this one leaves, slot 0 what enters the first one)
-    for (int k = w; k < look; k += kW) sh.seen[k][lane] = await<kC>(slots + (long long)(piece.turn - k) * r.d, steps, k == look - 1);
+    constexpr int kN = PieceShared<kC, kT, kW>::kMostLooked / kW;   // of one wave
+    const int n = (look - w + kW - 1) / kW;
+    if (n > 0) {
+        Link<kC> links[kN];
+        await<kC, kN>(links, n, slots + (long long)(piece.turn - w) * r.d, -(long long)kW * r.d, (look - 1) % kW == w ? n - 1 : -1, steps);
+#pragma unroll
+        for (int k = 0; k < kN; k++)
+            if (k < n) sh.seen[w + k * kW][lane] = links[k];
+    }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kC; j++) carry[j] = sh.seen[look - 1][lane].e[j];
@@ -268,36 +293,40 @@ __device__ __forceinline__ void announce(const Link<kC>& all, const At& steps, c
 }
 
 template <typename IO, int kGate, int kC, int kT, int kW, bool kPast, bool kWhole>
-__device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
+__device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kT, kW>& sh)
 {
     const int s0 = (piece.turn * kW + w) * kT;
     const Steps<IO, kC, kT, kPast, kWhole> steps(places, piece.b, s0, r.L, piece.first, lane, r.d);
     Piece<IO, kC> x[kT], g[kT], add[kT];
-    steps.load(x, r.x);
-    steps.load(g, r.g);
     float bias[kC], a[kT][kC], u[kT][kC], h[kC];
-    steps.load_params(bias, r.bias);
     if (r.pieces == 1) steps.load_params(h, r.enter ? r.enter + (long long)piece.b * r.d : nullptr);
-    if (r.add.p) {
-        steps.load(add, r.add);
-    } else {
 #pragma unroll
-        for (int i = 0; i < kT; i++) add[i] = Piece<IO, kC>{};
-    }
+    for (int i = 0; i < kT; i++) add[i] = Piece<IO, kC>{};
     Link<kC> mine;
 #pragma unroll
     for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = 0.0f;
+    if (steps.idle()) {
 #pragma unroll
-    for (int i = 0; i < kT; i++)
+        for (int i = 0; i < kT; i++)
 #pragma unroll
-        for (int j = 0; j < kC; j++) {
-            float q;
-            gate_of<kGate>(g[i][j], bias[j], a[i][j], q);
-            u[i][j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
-            if (!steps.inside(i)) a[i][j] = 1.0f, u[i][j] = 0.0f;
-            mine.e[j] = a[i][j] * mine.e[j] + u[i][j];
-            mine.p[j] *= a[i][j];
-        }
+            for (int j = 0; j < kC; j++) a[i][j] = 1.0f, u[i][j] = 0.0f;
+    } else {
+        steps.load(x, r.x);
+        steps.load(g, r.g);
+        steps.load_params(bias, r.bias);
+        if (r.add.p) steps.load(add, r.add);
+#pragma unroll
+        for (int i = 0; i < kT; i++)
+#pragma unroll
+            for (int j = 0; j < kC; j++) {
+                float q;
+                gate_of<kGate>(g[i][j], bias[j], a[i][j], q);
+                u[i][j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
+                if (!steps.inside(i)) a[i][j] = 1.0f, u[i][j] = 0.0f;
+                mine.e[j] = a[i][j] * mine.e[j] + u[i][j];
+                mine.p[j] *= a[i][j];
+            }
+    }
     Link<kC> all = mine, before;
     if constexpr (kW > 1) {
         sh.part[w][lane] = mine;
@@ -318,8 +347,8 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
 #pragma unroll
         for (int j = 0; j < kC; j++) before.p[j] = 1.0f, before.e[j] = 0.0f;
     }
-    if (w == 0) announce(all, steps, r, piece);
-    if (r.pieces > 1) look_back<kC, kW>(h, steps, r, piece, w, lane, sh);
+    if (!PieceShared<kC, kT, kW>::kOnly && w == 0) announce(all, steps, r, piece);
+    if (!PieceShared<kC, kT, kW>::kOnly && r.pieces > 1) look_back<kC, kT, kW>(h, steps, r, piece, w, lane, sh);
     if (w == 0) leave(all, h, steps, r, piece);
 #pragma unroll
     for (int j = 0; j < kC; j++) h[j] = before.p[j] * h[j] + before.e[j];
@@ -336,9 +365,9 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
     }
 }
 template <typename IO, int kGate, int kC, int kT, int kW, bool kPast>
-__global__ __launch_bounds__(64 * kW, 4) void recur_kernel(const RecurArgs r)
+__global__ __launch_bounds__(64 * kW, kT * kW > 32 ? 4 : 1) void recur_kernel(const RecurArgs r)
 {
-    __shared__ PieceShared<kC, kW> sh;
+    __shared__ PieceShared<kC, kT, kW> sh;
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const PieceOf piece(r, 64 * kC, sh);
     const Places places(r, piece.b);
@@ -352,35 +381,44 @@ __global__ __launch_bounds__(64 * kW, 4) void recur_kernel(const RecurArgs r)
 // and dg are of dh, and dy as it was read, not the states.  dbias is summed by lane over the wave's tokens, then over the waves and the
 // pieces in a fixed order.
 template <typename IO, int kGate, int kC, int kT, int kW, bool kPast, bool kWhole>
-__device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kW>& sh)
+__device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places& places, const PieceOf& piece, int w, int lane, PieceShared<kC, kT, kW>& sh)
 {
     const int seg = r.pieces - 1 - piece.turn, base = seg * kW * kT, s0 = base + w * kT, kept = (r.L + kKeep - 1) / kKeep, first = min(s0 / kKeep, kept - 1);
     const Steps<IO, kC, kT, kPast, kWhole> steps(places, piece.b, s0, r.L, piece.first, lane, r.d);
     Piece<IO, kC> x[kT], g[kT], dy[kT];
-    steps.load(x, r.x);
-    steps.load(g, r.g);
-    steps.load(dy, r.dy);
     float bias[kC], dbias[kC], h[kC], dh[kC], a[kT][kC], q[kT][kC];
-    steps.load_params(bias, r.bias);
     steps.load_params(h, r.states + ((long long)piece.b * kept + first) * r.d);
     if (r.pieces == 1) steps.load_params(dh, r.enter ? r.enter + (long long)piece.b * r.d : nullptr);
     Link<kC> mine;   // (P, Q)
     float e[kC];
 #pragma unroll
     for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = e[j] = dbias[j] = 0.0f;
+    if (steps.idle()) {
 #pragma unroll
-    for (int i = 0; i < kT; i++)
+        for (int i = 0; i < kT; i++) {
+            x[i] = dy[i] = Piece<IO, kC>{};
 #pragma unroll
-        for (int j = 0; j < kC; j++) {
-            gate_of<kGate>(g[i][j], bias[j], a[i][j], q[i][j]);
-            if (!steps.inside(i)) a[i][j] = 1.0f, q[i][j] = 0.0f, x[i].v[j] = dy[i].v[j] = 0;
-            e[j] = a[i][j] * e[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
-            mine.p[j] *= a[i][j];
+            for (int j = 0; j < kC; j++) a[i][j] = 1.0f, q[i][j] = 0.0f;
         }
+    } else {
+        steps.load(x, r.x);
+        steps.load(g, r.g);
+        steps.load(dy, r.dy);
+        steps.load_params(bias, r.bias);
 #pragma unroll
-    for (int i = kT - 1; i >= 0; i--)
+        for (int i = 0; i < kT; i++)
 #pragma unroll
-        for (int j = 0; j < kC; j++) mine.e[j] = a[i][j] * (dy[i][j] + mine.e[j]);
+            for (int j = 0; j < kC; j++) {
+                gate_of<kGate>(g[i][j], bias[j], a[i][j], q[i][j]);
+                if (!steps.inside(i)) a[i][j] = 1.0f, q[i][j] = 0.0f, x[i].v[j] = dy[i].v[j] = 0;
+                e[j] = a[i][j] * e[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
+                mine.p[j] *= a[i][j];
+            }
+#pragma unroll
+        for (int i = kT - 1; i >= 0; i--)
+#pragma unroll
+            for (int j = 0; j < kC; j++) mine.e[j] = a[i][j] * (dy[i][j] + mine.e[j]);
+    }
     Link<kC> all = mine, behind;
 #pragma unroll
     for (int j = 0; j < kC; j++) behind.p[j] = 1.0f, behind.e[j] = 0.0f;
@@ -409,7 +447,7 @@ __device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places
             }
         }
     }
-    if (w == 0) announce(all, steps, r, piece);
+    if (!PieceShared<kC, kT, kW>::kOnly && w == 0) announce(all, steps, r, piece);
     float c[kT][kC];
 #pragma unroll
     for (int i = 0; i < kT; i++) {
@@ -421,7 +459,7 @@ __device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places
             h[j] = a[i][j] * h[j] + (kGate == kSigmoid ? q[i][j] * v : v);
         }
     }
-    if (r.pieces > 1) look_back<kC, kW>(dh, steps, r, piece, w, lane, sh);
+    if (!PieceShared<kC, kT, kW>::kOnly && r.pieces > 1) look_back<kC, kT, kW>(dh, steps, r, piece, w, lane, sh);
     if (w == 0) leave(all, dh, steps, r, piece);
 #pragma unroll
     for (int j = 0; j < kC; j++) dh[j] = behind.p[j] * dh[j] + behind.e[j];
@@ -459,7 +497,7 @@ __device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places
 template <typename IO, int kGate, int kC, int kT, int kW, bool kPast>
 __global__ __launch_bounds__(64 * kW) void recur_bwd_kernel(const RecurArgs r)
 {
-    __shared__ PieceShared<kC, kW> sh;
+    __shared__ PieceShared<kC, kT, kW> sh;
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const PieceOf piece(r, 64 * kC, sh);
     const Places places(r, piece.b);
@@ -483,35 +521,42 @@ int check_recurrence(const bimamba_recurrence_desc* d)
     return d->seqlen > 64 && pieces >= 1ll << 23 ? BIMAMBA_ERR_UNSUPPORTED : BIMAMBA_OK;
 }
 
-// Tokens of a wave in a piece, waves of one.  Short sequences go in one piece of as few registers as hold it, since its time is that of one
-// load after the other (512 x 32 tokens of 4096 channels: 8 x 4 4.6 us, 16 x 8 11.0).  Long ones: 16 x 8 forward, 8 x 65536 tokens of 4096
-// channels 388 us (16 x 4 465, 8 x 8 467, 16 x 16 485).  The gradients hold half as much again, so two workgroups of eight waves no
-// longer fit a CU: 16 x 4 476 us (16 x 8 643, 8 x 8 475) where there are more pieces than the chip holds at once, 16 x 8 below (4096 tokens
-// of 2048 channels 26 us, 16 x 4 33: half the pieces to look back at).
+// Tokens of a wave in a piece, waves of one, channels of a lane.  Short sequences go in one piece of as few registers as hold it, since its
+// time is that of one load after the other (512 x 32 tokens of 4096 channels: 8 x 4 4.6 us, 16 x 8 11.0).  Where there is little to do
+// altogether a lane has one channel and a workgroup sixteen waves: half the work of a wave, half the pieces to look back at (2 x 4096 tokens
+// of 512 channels 15.2 us, with two channels and eight waves 17.9; 2 x 128 5.0 and 6.2).  Else two channels: 16 x 8 forward, 8 x 65536
+// tokens of 4096 channels 383 us (16 x 4 465, 8 x 8 467, 16 x 16 485), in one piece of 16 x 16 up to 256 tokens (16 x 256 of 2048: 14.7 us,
+// two pieces 21.0).  The gradients hold half as much again, so two workgroups of eight waves no longer fit a CU: 16 x 4 477 us
+// (16 x 8 643, 8 x 8 475) where there are more pieces than the chip holds at once, 16 x 8 below (4096 tokens of 2048 channels 28 us, 16 x 4
+// 37).
 struct RecurPlan {
     int tokens, waves, pieces;
-    int channels;   // a lane
+    int channels;
     unsigned tiles;
 };
 RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
 {
     RecurPlan p{};
-    p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 1 ? 2 : 1;
-    p.tiles = (d->d_inner + 64 * p.channels - 1) / (64 * p.channels);
     const int L = d->seqlen;
     const auto pieces = [&](int steps) { return (L + steps - 1) / steps; };
+    const auto tiles = [&](int channels) { return (d->d_inner + 64 * channels - 1) / (64 * channels); };
+    const bool little = L > 64 && (L <= 256 || L > 1024) && (long long)tiles(1) * d->batch * pieces(256) <= cu_count();
+    p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 64 && !little ? 2 : 1;
+    p.tiles = tiles(p.channels);
     if (L == 1 && !back) p.tokens = 1, p.waves = 1;
     else if (L <= 4) p.tokens = 4, p.waves = 1;
     else if (L <= 32) p.tokens = 8, p.waves = 4;
-    else if (L <= 64 || (back && (long long)p.tiles * d->batch * pieces(128) > 2 * cu_count())) p.tokens = 16, p.waves = 4;
-    else p.tokens = 16, p.waves = 8;
+    else if (L <= 64) p.tokens = 16, p.waves = 4;
+    else if (little) p.tokens = L <= 128 ? 8 : 16, p.waves = 16;
+    else if (back) p.tokens = 16, p.waves = (long long)p.tiles * d->batch * pieces(128) <= 2 * cu_count() ? 8 : 4;
+    else p.tokens = 16, p.waves = L > 128 && L <= 256 ? 16 : 8;
     p.pieces = pieces(p.tokens * p.waves);
     return p;
 }
 
-size_t slots_bytes(const bimamba_recurrence_desc* d, const RecurPlan& p)   // (and the ticket)
+size_t slots_bytes(const bimamba_recurrence_desc* d, const RecurPlan& p)   // (and the tickets)
 {
-    return p.pieces > 1 ? (size_t)d->batch * p.pieces * d->d_inner * 8 + 16 : 0;
+    return p.pieces > 1 ? (size_t)d->batch * p.pieces * d->d_inner * 8 + kXcds * 4 : 0;
 }
 
 template <typename IO, int kGate, int kC, bool kPast>
@@ -521,34 +566,60 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     // meanwhile, the more the fewer sequences and channels there are; each piece looked at costs words to read.  65536 tokens of 2048
     // channels: 8 pieces 188 us, 4 199, 2 266; 8 x 8192 of 4096: 1 piece 381 us, 8 395.
     const int look = (int)(cu_count() / (2u * p.tiles * (unsigned)a.batch));
-    a.look = look < 1 ? 1 : look > kMostLooked ? kMostLooked : look;
+    const int most = p.waves < 8 ? 8 : p.waves;
+    a.look = look < 1 ? 1 : look > most ? most : look;
     if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 255) / 256), a.batch), dim3(256), 0, st, a);
     const dim3 grid(p.tiles * (unsigned)a.batch * p.pieces), wg(64 * p.waves);
-    if (back) {
-        if (p.tokens == 4) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 4, 1, kPast>), grid, wg, 0, st, a);
-        else if (p.tokens == 8) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 8, 4, kPast>), grid, wg, 0, st, a);
-        else if (p.waves == 4) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 16, 4, kPast>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, 16, 8, false>), grid, wg, 0, st, a);   // (a few pieces: within the caches)
-    } else {
-        if (p.tokens == 1) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 1, 1, kPast>), grid, wg, 0, st, a);
-        else if (p.tokens == 4) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 4, 1, kPast>), grid, wg, 0, st, a);
-        else if (p.tokens == 8) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 8, 4, kPast>), grid, wg, 0, st, a);
-        else if (p.waves == 4) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 16, 4, kPast>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, 16, 8, kPast>), grid, wg, 0, st, a);
-    }
+    const auto form = [&](auto tokens, auto waves, auto beyond) {
+        constexpr int kT = decltype(tokens)::value, kW = decltype(waves)::value;
+        constexpr bool kBeyond = kPast && decltype(beyond)::value;   // (the others never move more than the caches hold, or are not compiled for it)
+        if (p.tokens != kT || p.waves != kW) return;
+        if (back) {
+            if constexpr (kT > 1 && (kC == 1 || kW < 16)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kBeyond>), grid, wg, 0, st, a);
+        } else {
+            hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kBeyond>), grid, wg, 0, st, a);
+        }
+    };
+    using std::integral_constant;
+    const integral_constant<bool, true> yes{};
+    const integral_constant<bool, false> no{};
+    const integral_constant<int, 1> n1{};
+    const integral_constant<int, 4> n4{};
+    const integral_constant<int, 8> n8{};
+    const integral_constant<int, 16> n16{};
+    form(n1, n1, yes);
+    form(n4, n1, yes);
+    form(n8, n4, yes);
+    form(n16, n4, yes);
+    form(n16, n8, yes);
+    if constexpr (kC == 1) form(n8, n16, no);
+    form(n16, n16, yes);
 }
 template <typename IO, int kC>
-void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool back, hipStream_t st)
+void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool on_lines, bool back, hipStream_t st)
 {
-    const bool past = past_caches((back ? 5.0 : 3.0) * d->batch * d->seqlen * d->d_inner * sizeof(typename IO::T));
+    const bool past = a.queues == 1 && on_lines && past_caches((back ? 5.0 : 3.0) * d->batch * d->seqlen * d->d_inner * sizeof(typename IO::T));
     if (d->gate == BIMAMBA_GATE_SIGMOID) past ? launch_pieces<IO, kSigmoid, kC, true>(p, a, back, st) : launch_pieces<IO, kSigmoid, kC, false>(p, a, back, st);
     else past ? launch_pieces<IO, kLog, kC, true>(p, a, back, st) : launch_pieces<IO, kLog, kC, false>(p, a, back, st);
 }
-void launch(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool back, hipStream_t st)
+// Where rows do not start at cache lines the pieces of neighbouring channels share lines: they are read and written through the caches, and, with
+// more chains than workgroups in hand, by workgroups of one XCD, which share a cache.  29 x 2478 tokens of 2248 channels, past the
+// caches 312 us, through them 272, and with a queue for each XCD 257, gradients 544, 456, 392.  (With few chains the queues only
+// keep them apart: one sequence of 65536 x 2040 245 us, with eight queues 339; and rows that start at lines have nothing to share:
+// 65536 x 2048 201 and 255.)
+bool on_lines(const RowView& v, size_t elem)
 {
-    if (d->io_dtype == BIMAMBA_F32) launch_gate<IoF32, 1>(d, p, a, back, st);
-    else if (p.channels == 2) launch_gate<IoBF16, 2>(d, p, a, back, st);
-    else launch_gate<IoBF16, 1>(d, p, a, back, st);
+    return !v.p || (reinterpret_cast<uintptr_t>(v.p) % 128 == 0 && v.sb * (long long)elem % 128 == 0 && v.st * (long long)elem % 128 == 0);
+}
+void launch(const bimamba_recurrence_desc* d, const RecurPlan& p, RecurArgs& a, bool back, hipStream_t st)
+{
+    const size_t elem = dtype_bytes(d->io_dtype);
+    bool lines = true;
+    for (const RowView* v : {&a.x, &a.g, &a.add, &a.y, &a.dy, &a.dx, &a.dg}) lines = lines && on_lines(*v, elem);
+    a.queues = !lines && p.tiles * (unsigned)a.batch >= (unsigned)cu_count() ? kXcds : 1;
+    if (d->io_dtype == BIMAMBA_F32) launch_gate<IoF32, 1>(d, p, a, lines, back, st);
+    else if (p.channels == 2) launch_gate<IoBF16, 2>(d, p, a, lines, back, st);
+    else launch_gate<IoBF16, 1>(d, p, a, lines, back, st);
 }
 
 // An fp32 or int64 array, none if p is null.
@@ -612,7 +683,7 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
     a.x = row_view(x), a.g = row_view(g), a.y = row_view(y);
     if (add) a.add = row_view(add);
     a.bias = bias, a.lengths = lengths, a.enter = h_in, a.leave = h_out, a.states = states;
-    a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 2;
+    a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 4;
     a.L = L, a.d = D, a.pieces = p.pieces, a.reverse = d->reverse, a.batch = Bt;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
@@ -684,7 +755,7 @@ int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tenso
         RecurArgs a{};
         a.x = row_view(x), a.g = row_view(g), a.dy = row_view(dy), a.dx = row_view(dx), a.dg = row_view(dg);
         a.bias = bias, a.lengths = lengths, a.enter = dh_out, a.leave = dh_in, a.states = const_cast<float*>(states);
-        a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 2;
+        a.ticket = static_cast<unsigned*>(workspace), a.slots = static_cast<unsigned long long*>(workspace) + 4;
         float* const sums = static_cast<float*>(workspace) + slots_bytes(d, p) / sizeof(float);
         a.dbias = dbias ? slots > 1 ? sums : dbias : nullptr;
         a.L = L, a.d = D, a.pieces = p.pieces, a.reverse = d->reverse, a.batch = Bt;
