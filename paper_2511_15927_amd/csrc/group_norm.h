@@ -11,14 +11,15 @@ struct GroupNormArgs {
     float *mean, *rstd;           // [rows][G]; forward: null, not wanted
     float *dw, *db;               // sums of a row group, null: not wanted
     long long slot;               // from one row group's to the next one's
-    unsigned L, rows, per_wave;   // rows that a wave takes, or the waves that share a group together
+    unsigned L, rows, per_wave;   // steps that a wave takes, or the waves that share a group together
+    int at_once;                  // rows of a step: several where a row's groups leave lanes free
     int G, n, d, lanes;           // groups, channels of one; lanes of a wave that hold one
     int centred;
     float eps;
 };
 // Which waves hold a group, in how many pieces a lane, how many waves a workgroup has, and the launch.
 struct GroupPlan {
-    int waves, pieces, lanes, team;
+    int waves, pieces, lanes, at_once, team;
     unsigned tiles, row_groups, per_wave;
 };
 template <int kAct>

@@ -34,12 +34,14 @@ GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
     while (p.lanes < 64 && p.lanes < pieces) p.lanes *= 2;
     p.pieces = 1;
     while (p.pieces * p.lanes * p.waves < pieces) p.pieces *= 2;
-    const int runs = 64 / p.lanes;
+    int runs = 64 / p.lanes;   // groups of a row that a wave holds; where there are not that many it holds those of several rows
+    p.at_once = 1;
+    while (p.waves == 1 && runs > 1 && runs / 2 >= d->groups) runs /= 2, p.at_once *= 2;
     p.tiles = (d->groups + runs - 1) / runs;
-    p.team = p.waves > 1 ? p.waves : bwd && p.pieces == 1 ? 8 : 4;
+    p.team = p.waves > 1 ? p.waves : bwd && p.pieces == 1 && p.at_once == 1 ? 8 : 4;
     // Rows: as many as are in hand at once go to one wave each, up to four where there are more (sixteen for the gradients of shared groups, which
     // otherwise leave a slot as long as two rows for every few of them).
-    const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = p.waves == 1 ? p.team : 1;
+    const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = (p.waves == 1 ? p.team : 1) * p.at_once;
     const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 8u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 16 : 4;
     p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);
     // (a grid's second axis ends at 65535)
@@ -53,7 +55,7 @@ GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
 void launch(const bimamba_group_norm_desc* d, const GroupPlan& p, GroupNormArgs& a, bool bwd, hipStream_t st)
 {
     a.L = d->seqlen, a.rows = (unsigned)((long long)d->batch * d->seqlen), a.per_wave = p.per_wave;
-    a.G = d->groups, a.n = d->d_inner / d->groups, a.d = d->d_inner, a.lanes = p.lanes, a.centred = d->centred, a.eps = d->eps;
+    a.G = d->groups, a.n = d->d_inner / d->groups, a.d = d->d_inner, a.lanes = p.lanes, a.at_once = p.at_once, a.centred = d->centred, a.eps = d->eps;
     const bool bf16 = d->io_dtype == BIMAMBA_BF16, past = past_caches((bwd ? 3.0 : 2.0) * a.rows * a.d * dtype_bytes(d->io_dtype));
     switch (d->act) {
         case BIMAMBA_ACT_NONE: launch_group_norm<BIMAMBA_ACT_NONE>(p, a, bf16, past, bwd, st); break;

@@ -59,48 +59,68 @@ struct GroupSum {
 };
 
 // Where a lane's elements lie and which rows its wave takes.
-template <int kWaves, int kPieces, int kPiece, int kTeam, bool kPast>
+template <int kWaves, int kPieces, int kPiece, int kTeam, bool kPast, bool kMany>
 struct GroupPlace {
     int g, in, n, stride;
     bool real, whole;   // whether the lane's group exists; (wave-uniform) every piece of every lane lies within its group
-    unsigned r0, r1;
+    bool in_group;      // (wave-uniform) every piece lies within its group, whether or not there is one for each lane
+    unsigned run, r0, r1;   // the lane's row among those that the wave takes at once; the first of them, the end
     __device__ __forceinline__ GroupPlace(const GroupNormArgs& a, int lane, int wave) : n(a.n)
     {
-        const int runs = 64 / a.lanes, first = blockIdx.x * runs;
-        g = first + lane / a.lanes;
+        const int runs = 64 / a.lanes / (kMany ? a.at_once : 1), first = blockIdx.x * runs, k = lane / a.lanes;   // (groups of a row)
+        run = kMany ? k / runs : 0;
+        g = first + (kMany ? k % runs : k);
         real = g < a.G;
         g = min(g, a.G - 1);
         in = (lane % a.lanes + (kWaves > 1 ? wave * kPieces * 64 : 0)) * kPiece;
         stride = a.lanes * kPiece;
-        whole = first + runs <= a.G && a.n == kWaves * kPieces * stride;
+        whole = !kMany && first + runs <= a.G && a.n == kWaves * kPieces * stride;
+        in_group = a.n == kWaves * kPieces * stride;
         const unsigned group = kWaves == 1 ? blockIdx.y * kTeam + wave : blockIdx.y;
-        r0 = min(group * a.per_wave, a.rows);
-        r1 = min(r0 + a.per_wave, a.rows);
+        const unsigned step = a.per_wave * at_once(a);
+        r0 = (unsigned)min((unsigned long long)a.rows, (unsigned long long)group * step);
+        r1 = min(r0 + step, a.rows);
+    }
+    static __device__ __forceinline__ unsigned at_once(const GroupNormArgs& a) { return kMany ? a.at_once : 1; }
+    // The row that a lane takes of those from r on: beyond the last one that one, and then it stores nothing.
+    struct Row {
+        unsigned r, b, t;
+        bool real;
+    };
+    __device__ __forceinline__ Row row(const GroupNormArgs& a, unsigned r) const
+    {
+        if constexpr (kMany) r += run;   // (else the same in all lanes)
+        Row x;
+        x.real = real && r < r1;
+        x.r = min(r, r1 - 1);
+        x.b = x.r / a.L;
+        x.t = x.r - x.b * a.L;
+        return x;
     }
     __device__ __forceinline__ int at(int k) const { return in + k * stride; }
     __device__ __forceinline__ int channel() const { return g * n; }
     template <typename IO>
-    __device__ __forceinline__ void load(Piece<IO, kPiece> (&p)[kPieces], const RowView& v, unsigned b, unsigned t) const
+    __device__ __forceinline__ void load(Piece<IO, kPiece> (&p)[kPieces], const RowView& v, const Row& x) const
     {
-        const typename IO::T* const row = static_cast<const typename IO::T*>(v.p) + row_offset(v, b, t) + channel();
+        const typename IO::T* const row = static_cast<const typename IO::T*>(v.p) + row_offset(v, x.b, x.t) + channel();
 #pragma unroll
         for (int k = 0; k < kPieces; k++) p[k] = load_clamped<IO, kPiece, kPast>(row, at(k), n);
     }
     template <typename IO>
     __device__ __forceinline__ void settled(Piece<IO, kPiece> (&p)[kPieces]) const
     {
-        if (whole) return;
+        if (in_group) return;
 #pragma unroll
         for (int k = 0; k < kPieces; k++) settle(p[k], at(k), n, typename IO::T(0));
     }
     template <typename IO>
-    __device__ __forceinline__ void store(const RowView& v, unsigned b, unsigned t, const float (&f)[kPieces][kPiece]) const
+    __device__ __forceinline__ void store(const RowView& v, const Row& x, const float (&f)[kPieces][kPiece]) const
     {
-        typename IO::T* const row = static_cast<typename IO::T*>(v.p) + row_offset(v, b, t) + channel();
+        typename IO::T* const row = static_cast<typename IO::T*>(v.p) + row_offset(v, x.b, x.t) + channel();
 #pragma unroll
         for (int k = 0; k < kPieces; k++) {
             if (whole) store_piece<IO, kPast>(row + at(k), f[k]);
-            else if (real) store_piece_of<IO, kPast>(row, at(k), n, f[k]);
+            else if (x.real) store_piece_of<IO, kPast>(row, at(k), n, f[k]);
         }
     }
     __device__ __forceinline__ void params(float (&f)[kPieces][kPiece], const float* p, float missing) const
@@ -115,23 +135,23 @@ struct GroupPlace {
     }
 };
 
-template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast>
+template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast, bool kMany>
 __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
 {
     __shared__ GroupSum<kWaves> sum;
     constexpr bool kGated = kAct == kBefore || kAct == kAfter;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast> place(a, lane, wave);
+    const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast, kMany> place(a, lane, wave);
     if (place.r0 >= place.r1) return;   // (with several waves to a group: the whole workgroup)
     float w[kPieces][kPiece], c[kPieces][kPiece];
     place.params(w, a.weight, 1.0f);
     place.params(c, a.bias, 0.0f);
     const float inv = 1.0f / a.n;
-    unsigned b = place.r0 / a.L, t = place.r0 - b * a.L;
     Piece<IO, kPiece> px[kPieces], pz[kPieces];
-    place.template load<IO>(px, a.x, b, t);
-    if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
-    for (unsigned r = place.r0; r < place.r1; r++) {
+    auto next = place.row(a, place.r0);
+    place.template load<IO>(px, a.x, next);
+    if constexpr (kGated) place.template load<IO>(pz, a.z, next);
+    for (unsigned r = place.r0; r < place.r1; r += place.at_once(a)) {
         float u[kPieces][kPiece], gate[kPieces][kPiece], s0 = 0.0f, s1 = 0.0f;
         place.template settled<IO>(px);
         if constexpr (kGated) place.template settled<IO>(pz);
@@ -145,11 +165,11 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
                 s0 += u[k][i];
                 s1 += u[k][i] * u[k][i];
             }
-        const unsigned b0 = b, t0 = t;
-        if (++t == a.L) t = 0, b++;
-        if (r + 1 < place.r1) {
-            place.template load<IO>(px, a.x, b, t);
-            if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
+        const auto row = next;
+        if (place.r1 - r > place.at_once(a)) {
+            next = place.row(a, r + place.at_once(a));
+            place.template load<IO>(px, a.x, next);
+            if constexpr (kGated) place.template load<IO>(pz, a.z, next);
         }
         sum(s0, s1, a.lanes, wave, 0);
         float mean = 0.0f;
@@ -161,7 +181,7 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
 #pragma unroll
                 for (int i = 0; i < kPiece; i++) {
                     u[k][i] -= mean;
-                    s1 += place.whole || place.at(k) + i < a.n ? u[k][i] * u[k][i] : 0.0f;
+                    s1 += place.in_group || place.at(k) + i < a.n ? u[k][i] * u[k][i] : 0.0f;
                 }
             sum(s0, s1, a.lanes, wave, 1);
         } else if constexpr (kWaves > 1) {
@@ -175,21 +195,21 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
                 const float v = u[k][i] * rstd * w[k][i] + c[k][i];
                 u[k][i] = kAct == kSilu ? v * sigmoid_of(v) : kAct == kAfter ? v * gate[k][i] : v;
             }
-        place.template store<IO>(a.y, b0, t0, u);
-        if (place.real && lane % a.lanes == 0 && (kWaves == 1 || wave == 0)) {
-            if (a.mean) a.mean[(long long)r * a.G + place.g] = mean;
-            if (a.rstd) a.rstd[(long long)r * a.G + place.g] = rstd;
+        place.template store<IO>(a.y, row, u);
+        if (row.real && lane % a.lanes == 0 && (kWaves == 1 || wave == 0)) {
+            if (a.mean) a.mean[(long long)row.r * a.G + place.g] = mean;
+            if (a.rstd) a.rstd[(long long)row.r * a.G + place.g] = rstd;
         }
     }
 }
 
-template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast>
+template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast, bool kMany>
 __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
 {
     __shared__ GroupSum<kWaves> sum;
     constexpr bool kGated = kAct == kBefore || kAct == kAfter;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast> place(a, lane, wave);   // (r0 >= r1: a wave without rows, which leaves zeros)
+    const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast, kMany> place(a, lane, wave);   // (r0 >= r1: a wave without rows, which leaves zeros)
     float w[kPieces][kPiece], c[kPieces][kPiece], dw[kPieces][kPiece], db[kPieces][kPiece];
     place.params(w, a.weight, 1.0f);
     if constexpr (kAct == kSilu || kAct == kAfter) place.params(c, a.bias, 0.0f);
@@ -198,13 +218,14 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
 #pragma unroll
         for (int i = 0; i < kPiece; i++) dw[k][i] = db[k][i] = 0.0f;
     const float inv = 1.0f / a.n;
-    unsigned b = place.r0 / a.L, t = place.r0 - b * a.L;
-    for (unsigned r = place.r0; r < place.r1; r++) {
+    int turn = 0;
+    for (unsigned r = place.r0; r < place.r1; r += place.at_once(a), turn ^= 1) {
+        const auto row = place.row(a, r);
         Piece<IO, kPiece> px[kPieces], pz[kPieces], pd[kPieces];
-        place.template load<IO>(px, a.x, b, t);
-        if constexpr (kGated) place.template load<IO>(pz, a.z, b, t);
-        place.template load<IO>(pd, a.dy, b, t);
-        const float mean = a.centred ? a.mean[(long long)r * a.G + place.g] : 0.0f, rstd = a.rstd[(long long)r * a.G + place.g];
+        place.template load<IO>(px, a.x, row);
+        if constexpr (kGated) place.template load<IO>(pz, a.z, row);
+        place.template load<IO>(pd, a.dy, row);
+        const float mean = a.centred ? a.mean[(long long)row.r * a.G + place.g] : 0.0f, rstd = a.rstd[(long long)row.r * a.G + place.g];
         place.template settled<IO>(px);
         if constexpr (kGated) place.template settled<IO>(pz);
         place.template settled<IO>(pd);
@@ -232,13 +253,13 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
                         dv *= gate[k][i];
                     }
                 }
-                dw[k][i] += dv * xh[k][i];
-                db[k][i] += dv;
+                dw[k][i] += !kMany || row.real ? dv * xh[k][i] : 0.0f;
+                db[k][i] += !kMany || row.real ? dv : 0.0f;
                 g[k][i] = dv * w[k][i];
                 s0 += g[k][i];
                 s1 += g[k][i] * xh[k][i];
             }
-        sum(s0, s1, a.lanes, wave, (r - place.r0) & 1);
+        sum(s0, s1, a.lanes, wave, turn);
         const float c0 = a.centred ? s0 * inv : 0.0f, c1 = s1 * inv;
 #pragma unroll
         for (int k = 0; k < kPieces; k++)
@@ -252,9 +273,16 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
                     g[k][i] = du;
                 }
             }
-        place.template store<IO>(a.dx, b, t, g);
-        if constexpr (kGated) place.template store<IO>(a.dz, b, t, dz);
-        if (++t == a.L) t = 0, b++;
+        place.template store<IO>(a.dx, row, g);
+        if constexpr (kGated) place.template store<IO>(a.dz, row, dz);
+    }
+    if constexpr (kMany) {   // the rows that a wave took at once
+        for (int x = 64 / a.at_once; x < 64; x *= 2)
+#pragma unroll
+            for (int i = 0; i < kPiece; i++) {
+                dw[0][i] += __shfl_xor(dw[0][i], x);
+                db[0][i] += __shfl_xor(db[0][i], x);
+            }
     }
     const long long slot = (long long)blockIdx.y * a.slot + place.channel();
     if constexpr (kWaves > 1) {
@@ -275,16 +303,15 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
 #pragma unroll
                 for (int i = 0; i < kPiece; i++) all[wave][k * kPiece + i][lane] = which ? db[k][i] : dw[k][i];
             __syncthreads();
-            if (wave != 0 || !place.real) continue;
+            if (wave != 0 || !place.real || place.run != 0) continue;
 #pragma unroll
             for (int k = 0; k < kPieces; k++) {
                 float f[kPiece];
 #pragma unroll
                 for (int i = 0; i < kPiece; i++) {
-                    const int e = k * kPiece + i;
-                    f[i] = all[0][e][lane];
+                    f[i] = all[0][k * kPiece + i][lane];
 #pragma unroll
-                    for (int m = 1; m < kTeam; m++) f[i] += all[m][e][lane];
+                    for (int m = 1; m < kTeam; m++) f[i] += all[m][k * kPiece + i][lane];
                 }
                 store_piece_of<IoF32>(to + slot, place.at(k), a.n, f);
             }
@@ -292,31 +319,31 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
     }
 }
 
-template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast>
+template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast, bool kMany>
 __global__ __launch_bounds__(64 * kTeam) void group_norm_kernel(const GroupNormArgs a)
 {
     if constexpr (kWaves == 1 && kPieces == 1) {   // (groups smaller than a piece: an element a lane)
-        if (a.n < kPieceOf<IO>) return group_norm_rows<IO, kAct, 1, 1, 1, kTeam, kPast>(a);
+        if (a.n < kPieceOf<IO>) return group_norm_rows<IO, kAct, 1, 1, 1, kTeam, kPast, kMany>(a);
     }
-    group_norm_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>, kTeam, kPast>(a);
+    group_norm_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>, kTeam, kPast, kMany>(a);
 }
-template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast>
+template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast, bool kMany>
 __global__ __launch_bounds__(64 * kTeam) void group_norm_bwd_kernel(const GroupNormArgs a)
 {
     if constexpr (kWaves == 1 && kPieces == 1) {
-        if (a.n < kPieceOf<IO>) return group_norm_bwd_rows<IO, kAct, 1, 1, 1, kTeam, kPast>(a);
+        if (a.n < kPieceOf<IO>) return group_norm_bwd_rows<IO, kAct, 1, 1, 1, kTeam, kPast, kMany>(a);
     }
-    group_norm_bwd_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>, kTeam, kPast>(a);
+    group_norm_bwd_rows<IO, kAct, kWaves, kPieces, kPieceOf<IO>, kTeam, kPast, kMany>(a);
 }
 
 namespace {
 
-template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast>
+template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast, bool kMany = false>
 void launch_form(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
 {
     const dim3 grid(p.tiles, p.row_groups), wg(64 * kTeam);
-    if (bwd) hipLaunchKernelGGL((group_norm_bwd_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast>), grid, wg, 0, st, a);
-    else hipLaunchKernelGGL((group_norm_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast>), grid, wg, 0, st, a);
+    if (bwd) hipLaunchKernelGGL((group_norm_bwd_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((group_norm_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
 }
 template <typename IO, int kAct, bool kPast>
 void launch_io(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
@@ -328,7 +355,8 @@ void launch_io(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t
     } else if (p.waves == 4) {
         launch_form<IO, kAct, 4, kWide, 4, kPast>(p, a, bwd, st);
     } else if (p.pieces == 1) {
-        if (p.team == 8) launch_form<IO, kAct, 1, 1, 8, kPast>(p, a, bwd, st);
+        if (p.at_once > 1) launch_form<IO, kAct, 1, 1, 4, kPast, true>(p, a, bwd, st);
+        else if (p.team == 8) launch_form<IO, kAct, 1, 1, 8, kPast>(p, a, bwd, st);
         else launch_form<IO, kAct, 1, 1, 4, kPast>(p, a, bwd, st);
     } else if (p.pieces == 2) {
         launch_form<IO, kAct, 1, 2, 4, kPast>(p, a, bwd, st);
