@@ -185,7 +185,7 @@ DropPlan plan_dropout(const bimamba_dropout_desc* d, bool per_batch, bool sums)
     p.rows = per_batch ? d->seqlen : (unsigned)((long long)d->batch * d->seqlen);
     // Rows: as many as are in hand at once go to one wave each, a few more where there are more of them.
     const unsigned together = kTeam * (64 / p.lanes), most = sums ? 8 : 2;
-    const unsigned long long fair = (unsigned long long)p.rows * p.tiles * p.vectors / (together * 16u * cu_count());
+    const unsigned long long fair = (unsigned long long)p.rows * p.tiles * p.vectors / (together * (sums ? 6u : 16u) * cu_count());
     p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);
     // (a grid's second axis ends at 65535)
     const unsigned long long least = (p.rows + 65535ull * together - 1) / (65535ull * together);

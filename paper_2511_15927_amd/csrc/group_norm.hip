@@ -42,7 +42,7 @@ GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
     // Rows: as many as are in hand at once go to one wave each, up to four where there are more (sixteen for the gradients of shared groups, which
     // otherwise leave a slot as long as two rows for every few of them).
     const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = (p.waves == 1 ? p.team : 1) * p.at_once;
-    const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 8u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 16 : 4;
+    const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 3u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 16 : 4;
     p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);
     // (a grid's second axis ends at 65535)
     const unsigned long long least = (rows + 65535ull * together - 1) / (65535ull * together);
