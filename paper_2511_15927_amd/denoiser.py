@@ -2,12 +2,13 @@
 
     logits = head(norm(B_N(... B_1(E(tokens), tau) ..., tau))),   B(x, tau) = x + out_proj(Mixer(in_proj(AdaLN(x; tau))))
 
-(the paper's eqs. 7-10 without the MLP).  The token table, the norms, the mixers, the log probabilities and the clipping are calls of
-the library, forward and backward; the projections are plain matrix products of torch.  embed(), layer_norm(), mixer() and
-log_probs() take part in autograd and can be used on their own; they have first derivatives only, and a gradient through them that is
-itself differentiated is an error.
+(the paper's eqs. 7-10 without the MLP).  With mixer="recurrence" the mixer is a gated linear recurrence in both directions, its sum gated
+and normalised by groups of channels, and comes back as x + gate(tau) * dropout(out_proj(...)).  The token table, the norms, the mixers,
+dropout, the log probabilities and the clipping are calls of the library, forward and backward; the projections are plain matrix
+products of torch.  embed(), layer_norm(), mixer(), recurrence(), group_norm(), dropout_add() and log_probs() take part in autograd and
+can be used on their own; they have first derivatives only, and a gradient through them that is itself differentiated is an error.
 
-    python -m paper_2511_15927_amd.denoiser [--steps 200] [--width 256] [--layers 4] [--io bf16]
+    python -m paper_2511_15927_amd.denoiser [--steps 200] [--width 256] [--layers 4] [--io bf16] [--mixer recurrence --dropout 0.1]
 
 trains on synthetic sequences (runs of consecutive ids), then fills a masked sequence, the most confident places first.
 """
@@ -39,7 +40,7 @@ class _FirstOrder(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("embed, layer_norm, mixer and log_probs have no second derivatives")
+        raise RuntimeError("the library's functions have no second derivatives")
 
 
 def _first_order(grads, *sources):
@@ -133,6 +134,95 @@ def mixer(cfg, x, z, dt, B, C, pf, pb):
     return _Mixer.apply(cfg, x, z, dt, B, C, *(p[k] for p in (pf, pb) for k in PARAMS))
 
 
+class _Recurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, g, bias, add, h_in, lengths, gate, reverse, want_state):
+        Bt, L, D = x.shape
+        ctx.desc, ctx.has = bd.make_recurrence_desc(Bt, L, D, io=NAME[x.dtype], gate=gate, reverse=int(reverse)), (add is not None, h_in is not None, want_state)
+        y, states = torch.empty(Bt, L, D, dtype=x.dtype, device=x.device), torch.empty(Bt, -(-L // bd.RECURRENCE_KEEP), D, device=x.device)
+        h_out = torch.empty(Bt, D, device=x.device) if want_state else None
+        ws = _bytes(bd.bimamba_recurrence_workspace_bytes(ctx.desc), x)
+        bd.bimamba_recurrence(ctx.desc, x, g, bias, y, add=add, lengths=lengths, h_in=h_in, h_out=h_out, states=states, workspace=ws)
+        ctx.save_for_backward(x, g, bias, lengths, states)
+        return (y, h_out) if want_state else y
+
+    @staticmethod
+    def backward(ctx, dy, dh_out=None):
+        x, g, bias, lengths, states = ctx.saved_tensors
+        add, h_in, want_state = ctx.has
+        dx, dg = (torch.empty_like(x, memory_format=torch.contiguous_format) for _ in range(2))
+        dbias = None if bias is None else torch.empty_like(bias)
+        dh_in = torch.empty(x.shape[0], x.shape[2], device=x.device) if h_in else None
+        ws = _bytes(bd.bimamba_recurrence_bwd_workspace_bytes(ctx.desc), x)
+        bd.bimamba_recurrence_bwd(ctx.desc, x, g, bias, states, _rows(dy), dx, dg, dbias=dbias, lengths=lengths,
+                                  dh_out=dh_out.contiguous() if want_state else None, dh_in=dh_in, workspace=ws)
+        dadd = None
+        if add:
+            dadd = dy if lengths is None else torch.where(torch.arange(dy.shape[1], device=dy.device)[:, None] < lengths[:, None, None], dy, 0)
+        grads = _first_order((dx, dg, dbias, dadd, dh_in), x, g, bias, states, dy, dh_out)
+        return grads + (None,) * 4
+
+
+def recurrence(x, g, bias=None, add=None, h_in=None, lengths=None, gate="sigmoid", reverse=False, want_state=False):
+    """h = a h + u along the sequence, y = h + add: x, g, add [batch, L, d]; gate "sigmoid" (a = sigmoid(g + bias), u = (1 - a) x) or "log"
+    (a = exp(min(g, 0)), u = x).  h_in float32 [batch, d], the state before the first step; with want_state (y, the state after the
+    last); lengths int64 [batch]: y is 0 behind them."""
+    return _Recurrence.apply(x, g, bias, add, h_in, lengths, gate, reverse, want_state)
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, z, weight, bias, groups, act, centred, eps):
+        Bt, L, D = x.shape
+        ctx.desc = bd.make_group_norm_desc(Bt, L, D, groups, io=NAME[x.dtype], act=act, centred=int(centred), eps=eps)
+        y, rstd = torch.empty(Bt, L, D, dtype=x.dtype, device=x.device), torch.empty(Bt, L, groups, device=x.device)
+        mean = torch.empty_like(rstd) if centred else None
+        bd.bimamba_group_norm(ctx.desc, x, z, weight, bias, y, mean, rstd)
+        ctx.save_for_backward(x, z, weight, bias, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, z, weight, bias, mean, rstd = ctx.saved_tensors
+        dx, dz = (None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format) for t in (x, z))
+        dweight, dbias = (None if t is None else torch.empty_like(t) for t in (weight, bias))
+        ws = _bytes(bd.bimamba_group_norm_bwd_workspace_bytes(ctx.desc), x)
+        bd.bimamba_group_norm_bwd(ctx.desc, x, z, weight, bias, mean, rstd, _rows(dy), dx, dz, dweight, dbias, ws)
+        return _first_order((dx, dz, dweight, dbias), x, z, weight, bias, rstd, dy) + (None,) * 4
+
+
+def group_norm(x, z, weight, bias, groups, act="gate_before", centred=False, eps=1e-5):
+    """The norm of every token's `groups` groups of channels; act: "none", "silu", "gate_before" (of x SiLU(z)) or "gate_after" (times SiLU(z));
+    z: None without a gate; weight, bias float32 [d] or None."""
+    return _GroupNorm.apply(x, z, weight, bias, groups, act, centred, eps)
+
+
+class _DropoutAdd(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, residual, key, p, site):
+        Bt, L, D = x.shape
+        ctx.desc, ctx.has = bd.make_dropout_desc(Bt, L, D, io=NAME[x.dtype], p=p, site=site), residual is not None
+        out = torch.empty(Bt, L, D, dtype=x.dtype, device=x.device)
+        bd.bimamba_dropout_add(ctx.desc, key, x, gate, residual, out)
+        ctx.save_for_backward(None if gate is None else x, gate, key)   # (no mask)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        x, gate, key = ctx.saved_tensors
+        dx = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+        dgate = None if gate is None else torch.empty(gate.shape, device=dout.device)
+        ws = None if gate is None else _bytes(bd.bimamba_dropout_add_bwd_workspace_bytes(ctx.desc, gate.dim() == 2), dout)
+        bd.bimamba_dropout_add_bwd(ctx.desc, key, x, gate, _rows(dout), dx, dgate, ws)
+        return _first_order((dx, dgate, dout if ctx.has else None), x, gate, dout) + (None,) * 3
+
+
+def dropout_add(x, gate, residual, key, p, site=0):
+    """residual + gate * dropout(x), its mask made from key (int64 [2] on the device: seed, offset) and site, forward and backward; gate float32
+    [d], [batch, d] or None; residual like x, or None."""
+    return _DropoutAdd.apply(x, gate, residual, key, p, site)
+
+
 class _LogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, want_entropy):
@@ -162,13 +252,24 @@ class Denoiser:
     """Parameters are float32 tensors in a dict; activations are of the type `io`.  The last id of the vocabulary is the mask."""
     FEATURES = 64   # of the noise level
 
-    def __init__(self, vocab, width, layers, d_state=16, io="bf16", seed=0, device="cuda"):
+    def __init__(self, vocab, width, layers, d_state=16, io="bf16", seed=0, device="cuda", mixer="mamba", dropout=0.0):
+        """mixer: "mamba" (the selective scan, d_state states a channel) or "recurrence"; dropout: the share that training drops of what a
+        block adds to its input, with masks from `key`, whose offset every step moves."""
+        assert mixer in ("mamba", "recurrence"), mixer
         self.vocab, self.width, self.layers, self.d_state, self.io, self.mask = vocab, width, layers, d_state, TYPE[io], vocab - 1
+        self.mixer, self.dropout, self.key = mixer, dropout, torch.tensor([seed, 0], device=device)
         gen = torch.Generator().manual_seed(seed)
         D, Dn, N = width, 2 * width, d_state
         normal = lambda *s, scale: scale * torch.randn(*s, generator=gen)  # noqa: E731
         p = dict(table=normal(vocab, D, scale=D ** -0.5), norm_w=torch.ones(D), norm_b=torch.zeros(D), head=normal(vocab, D, scale=D ** -0.5))
-        for l in range(layers):
+        for l in range(layers if mixer == "recurrence" else 0):
+            p["%d.cond" % l] = normal(3 * D, self.FEATURES, scale=0.02)
+            p["%d.in" % l] = normal(4 * Dn, D, scale=D ** -0.5)               # x | z | gates of the two directions
+            p["%d.out" % l] = normal(D, Dn, scale=0.5 * Dn ** -0.5)
+            p["%d.norm" % l] = torch.ones(Dn)
+            for s in "fb":   # (channels that remember 1 to 100 tokens)
+                p["%d.%s.bias" % (l, s)] = math.log(100.0) * torch.rand(Dn, generator=gen)
+        for l in range(layers if mixer == "mamba" else 0):
             p["%d.cond" % l] = normal(2 * D, self.FEATURES, scale=0.02)
             p["%d.in" % l] = normal(2 * Dn, D, scale=D ** -0.5)               # x | z
             p["%d.ssm" % l] = normal(Dn + 2 * N, D, scale=D ** -0.5)          # dt | B | C
@@ -186,8 +287,20 @@ class Denoiser:
         w = self.params[name].to(self.io)
         return (x.reshape(-1, x.shape[-1]) @ w.t()).view(*x.shape[:-1], w.shape[0])
 
-    def logits(self, tokens, level):
-        """Logits [batch, L, vocab] of tokens [batch, L] (the mask's is -inf) at noise levels [batch] in (0, 1]."""
+    def _block(self, x, cond, l, p_drop):
+        """A block with the gated recurrence: its input plus what the noise level's gate leaves of it."""
+        p, D, Dn = self.params, self.width, 2 * self.width
+        still = cond.new_ones(3 * D)
+        still[D:2 * D].fill_(0.0)
+        gain, shift, gate = (cond + still).split(D, 1)   # column slices of one projection
+        xs, z, gf, gb = self._linear(layer_norm(x, gain, shift), "%d.in" % l).split(Dn, 2)
+        h = recurrence(xs, gf, p["%d.f.bias" % l])
+        h = recurrence(xs, gb, p["%d.b.bias" % l], add=h, reverse=True)
+        y = group_norm(h, z, p["%d.norm" % l], None, Dn // 64 if Dn % 64 == 0 else 1)
+        return dropout_add(self._linear(y, "%d.out" % l), gate, x, self.key, p_drop, site=l)
+
+    def logits(self, tokens, level, train=False):
+        """Logits [batch, L, vocab] of tokens [batch, L] (the mask's is -inf) at noise levels [batch] in (0, 1]; train: with dropout."""
         p, D, Dn, N = self.params, self.width, 2 * self.width, self.d_state
         Bt, L = tokens.shape
         cfg = dict(batch=Bt, seqlen=L, d_inner=Dn, d_state=N, n_heads=Dn, n_groups=1, d_conv=4, io=NAME[self.io], a_kind=bd.A_PER_HEAD_STATE,
@@ -197,16 +310,21 @@ class Denoiser:
         x = embed(p["table"], tokens, math.sqrt(D), self.io)
         for l in range(self.layers):
             cond = feature @ p["%d.cond" % l].t()
+            p_drop = self.dropout if train else 0.0
+            if self.mixer == "recurrence":
+                x = self._block(x, cond, l, p_drop)
+                continue
             gain, shift = (cond + torch.cat([torch.ones(D), torch.zeros(D)]).to(cond)).split(D, 1)   # column slices of one projection
             y = layer_norm(x, gain, shift)
             xs, z = self._linear(y, "%d.in" % l).split(Dn, 2)
             dt, B, C = self._linear(y, "%d.ssm" % l).split([Dn, N, N], 2)
             side = [dict(conv_w=p["%d.%s.conv_w" % (l, s)], conv_b=p["%d.%s.conv_b" % (l, s)], A=-torch.exp(p["%d.%s.A_log" % (l, s)]),
                          D=p["%d.%s.D" % (l, s)], dt_bias=p["%d.%s.dt_bias" % (l, s)]) for s in "fb"]
-            x = x + self._linear(mixer(cfg, xs, z, dt, B, C, *side), "%d.out" % l)
+            y = self._linear(mixer(cfg, xs, z, dt, B, C, *side), "%d.out" % l)
+            x = x + y if p_drop == 0.0 else dropout_add(y, None, x, self.key, p_drop, site=l)
         logits = self._linear(layer_norm(x, p["norm_w"], p["norm_b"]), "head")
         never = torch.zeros(self.vocab, dtype=self.io, device=logits.device)
-        never[self.mask] = -math.inf
+        never[self.mask:].fill_(-math.inf)   # (a kernel, no copy from the host: a step can be captured)
         return logits + never
 
     def noised(self, tokens, gen):
@@ -217,7 +335,7 @@ class Denoiser:
 
     def loss(self, noised, targets, level):
         """The masked-diffusion bound per token: -log p of the masked tokens, each weighted by 1 / level."""
-        logp, _ = log_probs(self.logits(noised, level), targets)
+        logp, _ = log_probs(self.logits(noised, level, train=True), targets)
         return -(logp / level[:, None]).sum() / noised.numel()
 
     def train_step(self, tokens, gen, lr=0.05, max_norm=1.0):
@@ -233,6 +351,7 @@ class Denoiser:
         for p, g in zip(params, table.grads):
             p.grad = g   # (what the program has made of it since: freed it, put another in its place)
         torch._foreach_zero_(table.grads)
+        self.key[1] += 1
         loss = self.loss(*self.noised(tokens, gen))
         loss.backward()
         for (name, p), g in zip(self.params.items(), table.grads):
@@ -279,8 +398,10 @@ def main(argv=None):
     ap.add_argument("--width", type=int, default=256)
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--io", choices=("f32", "bf16"), default="bf16")
+    ap.add_argument("--mixer", choices=("mamba", "recurrence"), default="mamba")
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args(argv)
-    model = Denoiser(a.vocab, a.width, a.layers, io=a.io)
+    model = Denoiser(a.vocab, a.width, a.layers, io=a.io, mixer=a.mixer, dropout=a.dropout)
     gen = torch.Generator(device="cuda").manual_seed(1)
     for step in range(a.steps):
         loss, norm = model.train_step(synthetic_tokens(a.batch, a.seqlen, a.vocab, gen), gen)
