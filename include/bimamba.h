@@ -452,7 +452,7 @@ enum bimamba_gate {
 typedef struct bimamba_recurrence_desc {
     uint32_t struct_size;   /* sizeof(bimamba_recurrence_desc), checked */
     int32_t batch;          /* >= 0, <= 65535 */
-    int32_t seqlen;         /* >= 0 */
+    int32_t seqlen;         /* >= 0; above 4 tokens batch * ceil(seqlen / 64) * ceil(d_inner / 64) < 2^23 (BIMAMBA_ERR_UNSUPPORTED) */
     int32_t d_inner;        /* <= 65536 */
     int32_t io_dtype;       /* bimamba_dtype of x, g, add, y and of dy, dx, dg */
     int32_t gate;           /* bimamba_gate */
@@ -473,7 +473,8 @@ typedef struct bimamba_recurrence_desc {
  *   states    fp32 [batch, ceil(seqlen / 64), d_inner] or NULL: the state before every 64th step (BIMAMBA_RECURRENCE_KEEP), counted in
  *             the order of the walk; the gradients take them.  Behind a sequence's end: its last state.
  *   workspace at least bimamba_recurrence_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL if that is 0.
- * A value that is not finite makes everything not finite that its channel's walk reaches after it.
+ * A value that is not finite makes everything not finite that its channel's walk reaches after it, up to factors whose product is 0 (a
+ * factor of 0, or one that underflows): whether it reaches past those is left open.
  */
 int bimamba_recurrence(const bimamba_recurrence_desc* desc, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
                        const bimamba_tensor* add, const int64_t* lengths, const float* h_in, const bimamba_tensor* y, float* h_out,

@@ -82,6 +82,17 @@ def test_recurrence_workspace():
         assert recurrence(**dict(one, ws=AT[at])) == ALIAS, at
 
 
+@pytest.mark.parametrize("batch, seqlen, d", [(8192, 64, 65536), (64, 8192, 65536), (1 << 15, 5, 16384), (1, 1 << 29, 64)])
+def test_recurrence_of_more_pieces_than_a_grid_holds(batch, seqlen, d):
+    """2^23 times 64 steps of 64 channels, and a step less."""
+    for call in (recurrence, recurrence_bwd):
+        assert call(batch=batch, seqlen=seqlen, d_inner=d) == UNSUPPORTED
+    assert bd.bimamba_recurrence_bwd_workspace_bytes(bd.make_recurrence_desc(batch, seqlen, d)) == 0
+    fewer = (batch - 1, seqlen) if batch > 1 else (batch, seqlen - 64)
+    assert bd.bimamba_recurrence_bwd_workspace_bytes(bd.make_recurrence_desc(*fewer, d)) > 0
+    assert bd.bimamba_recurrence_bwd_workspace_bytes(bd.make_recurrence_desc(65535, 4, 65536)) > 0
+
+
 def recurrence_bwd(**kw):
     d, kw = made(bd.make_recurrence_desc, dict(batch=2, seqlen=10, d_inner=64), kw)
     a = dict(x=view(AT[1]), g=view(AT[2]), bias=AT[3], lengths=AT[4], states=AT[5], dy=view(AT[6]), dh_out=AT[7], dx=view(AT[8]), dg=view(AT[9]),
