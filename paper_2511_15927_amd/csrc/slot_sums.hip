@@ -2,10 +2,11 @@
 
 namespace bm {
 
-// Many slots are added in two steps, few in the second alone.  First: 64 lanes of four channels, four waves of eight slots each, all of them asked
-// for together; the sum goes to the first of the 32 slots, which no other workgroup reads.  (2048 slots of 2 x 4096: both steps 17 us, one
-// step alone 60.)
-constexpr int kSlots = 32, kWide = 256;
+// More than 2048 slots are added in two steps, others in the second alone, whose time is that of one row of threads' loads.  First: 64 lanes of
+// four channels, four waves of eight slots each, all of them asked for together; the sum goes to the first of the 32 slots, which no other
+// workgroup reads.  (Just written, of 2 x 256 channels: 512 slots both steps 5.1 us, one 2.4; 2048 5.2, 5.5; 16384 18.9, 38.9; of 2 x 4096:
+// 512 12.0, 8.4; 4096 28.9, 26.2; of 2 x 4: 65536 12.5, 122.)
+constexpr int kSlots = 32, kWide = 256, kOneStep = 2048;
 __global__ __launch_bounds__(256) void slot_merge_kernel(const SlotSumArgs a, int arrays)
 {
     const int which = blockIdx.z % arrays, vector = blockIdx.z / arrays;
@@ -65,7 +66,7 @@ void launch_slot_sum(SlotSumArgs a, int vectors, hipStream_t st)
 {
     const int arrays = a.out[1] ? 2 : 1;
     const long long per_vector = a.count * a.pitch;
-    if (a.count > 2 * kSlots && a.count <= 65535ll * kSlots && vectors * arrays <= 65535) {
+    if (a.count > kOneStep && a.count <= 65535ll * kSlots && vectors * arrays <= 65535) {
         const long long heads = (a.count + kSlots - 1) / kSlots;
         hipLaunchKernelGGL(slot_merge_kernel, dim3((a.d + kWide - 1) / kWide, (unsigned)heads, vectors * arrays), dim3(256), 0, st, a, arrays);
         a.count = heads, a.pitch *= kSlots;

@@ -400,3 +400,45 @@ def test_masks_go_by_key_and_site_and_not_by_layout(bd):
         seen.append(out.clone())
     made([1, 2], 0, 2, 60)   # (rows are counted through the batch)
     assert torch.equal(out, seen[0])
+
+
+@pytest.mark.parametrize("D", [3, 130])
+def test_sums_over_thousands_of_workgroups(bd, D):
+    """More than 2048 slots, whose sums are made in two steps: dbias, dweight and dgate are the sums of what the calls give for each token.  No value
+    passes 300 additions on its way, each off by 2^-24 of the magnitudes; a slot left out would be off by 1 / 2400."""
+    def near(got, terms):
+        terms = terms.double().flatten(0, 1)
+        assert bool(((got.double() - terms.sum(0)).abs() <= 300 * 2.0 ** -24 * terms.abs().sum(0)).all())
+
+    def r(*s, seed=3):
+        return torch.randn(*s, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+    room = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")  # noqa: E731
+    B, L = 2100, 3
+    desc = bd.make_recurrence_desc(B, L, D, io="f32")
+    x, g, dy, bias = r(B, L, D), r(B, L, D, seed=4), r(B, L, D, seed=5), r(D)
+    y, dx, dg, states, dbias = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty(B, 1, D, device="cuda"), torch.empty(D, device="cuda")
+    bd.bimamba_recurrence(desc, x, g, bias, y, states=states, workspace=room(bd.bimamba_recurrence_workspace_bytes(desc)))
+    bd.bimamba_recurrence_bwd(desc, x, g, bias, states, dy, dx, dg, dbias=dbias, workspace=room(bd.bimamba_recurrence_bwd_workspace_bytes(desc)))
+    near(dbias, dg)
+
+    B, L = 2, 300000 if D == 3 else 36000
+    desc = bd.make_group_norm_desc(B, L, D, 1, io="f32", act="none")
+    need = bd.bimamba_group_norm_bwd_workspace_bytes(desc)
+    assert need >= 2048 * 2 * D * 4
+    x, dy, w = r(B, L, D), r(B, L, D, seed=4), r(D)
+    y, dx, rstd, dweight, dbias = torch.empty_like(x), torch.empty_like(x), torch.empty(B, L, 1, device="cuda"), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    bd.bimamba_group_norm(desc, x, None, w, None, y, None, rstd)
+    bd.bimamba_group_norm_bwd(desc, x, None, w, None, None, rstd, dy, dx, None, dweight, dbias, room(need))
+    near(dbias, dy)
+    near(dweight, dy.double() * x.double() * rstd.double())
+
+    B, L = 1, 1100000 if D == 3 else 70000
+    desc = bd.make_dropout_desc(B, L, D, io="f32", p=0.25)
+    need = bd.bimamba_dropout_add_bwd_workspace_bytes(desc, False)
+    assert need >= 2048 * D * 4
+    key, gate = torch.tensor([5, 6], device="cuda"), torch.ones(D, device="cuda")
+    x, dout = r(B, L, D), r(B, L, D, seed=4)
+    kept, dx, dgate = torch.empty_like(x), torch.empty_like(x), torch.empty(D, device="cuda")
+    bd.bimamba_dropout_add(desc, key, x, None, None, kept)
+    bd.bimamba_dropout_add_bwd(desc, key, x, gate, dout, dx, dgate, room(need))
+    near(dgate, kept.double() * dout.double())
