@@ -16,44 +16,58 @@ enum Act { kPlain = BIMAMBA_ACT_NONE, kSilu = BIMAMBA_ACT_SILU, kBefore = BIMAMB
 
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
 
-// Two values summed over each run of `lanes` lanes, the same in all of a run.
-__device__ __forceinline__ void run_sum(float& u, float& v, int lanes)
+// Values summed over each run of `lanes` lanes, the same in all of a run.
+template <int kN>
+__device__ __forceinline__ void run_sum(float (&v)[kN], int lanes)
 {
-#define BM_DPP(x, ctrl) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xf, 0xf, true))
+#define BM_DPP(ctrl) \
+    for (int i = 0; i < kN; i++) v[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[i]), ctrl, 0xf, 0xf, true))
     if (lanes < 2) return;
-    u += BM_DPP(u, 0xB1), v += BM_DPP(v, 0xB1);     // quad_perm 1 0 3 2
+#pragma unroll
+    BM_DPP(0xB1);    // quad_perm 1 0 3 2
     if (lanes < 4) return;
-    u += BM_DPP(u, 0x4E), v += BM_DPP(v, 0x4E);     // quad_perm 2 3 0 1
+#pragma unroll
+    BM_DPP(0x4E);    // quad_perm 2 3 0 1
     if (lanes < 8) return;
-    u += BM_DPP(u, 0x141), v += BM_DPP(v, 0x141);   // row_half_mirror
+#pragma unroll
+    BM_DPP(0x141);   // row_half_mirror
     if (lanes < 16) return;
-    u += BM_DPP(u, 0x140), v += BM_DPP(v, 0x140);   // row_mirror
+#pragma unroll
+    BM_DPP(0x140);   // row_mirror
 #undef BM_DPP
     if (lanes < 32) return;
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(u), false, false);
-    u = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+#pragma unroll
+    for (int i = 0; i < kN; i++) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     if (lanes < 64) return;
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(u), __float_as_uint(u), false, false);
-    u = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+#pragma unroll
+    for (int i = 0; i < kN; i++) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
 }
 
-// The sums of a group from those of its lanes, and over its waves; there is a barrier between two uses of the same turn.
-template <int kWaves>
+// The sums of a group from those of its lanes, and over its waves.  (Two turns: a part is written again only after the barrier of the sum
+// between, which no wave passes before it has read this one's.)
+template <int kWaves, int kN>
 struct GroupSum {
-    float2 part[2][kWaves];
-    __device__ __forceinline__ void operator()(float& u, float& v, int lanes, int wave, int turn)
+    float part[2][kWaves][kN];
+    __device__ __forceinline__ void operator()(float (&v)[kN], int lanes, int wave, int& turn)
     {
-        run_sum(u, v, lanes);
+        run_sum(v, lanes);
         if constexpr (kWaves > 1) {
-            part[turn][wave] = make_float2(u, v);
-            __syncthreads();
-            u = part[turn][0].x, v = part[turn][0].y;
 #pragma unroll
-            for (int k = 1; k < kWaves; k++) u += part[turn][k].x, v += part[turn][k].y;
+            for (int i = 0; i < kN; i++) part[turn][wave][i] = v[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kN; i++) {
+                v[i] = part[turn][0][i];
+#pragma unroll
+                for (int k = 1; k < kWaves; k++) v[i] += part[turn][k][i];
+            }
+            turn ^= 1;
         }
     }
 };
@@ -138,7 +152,7 @@ struct GroupPlace {
 template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast, bool kMany>
 __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
 {
-    __shared__ GroupSum<kWaves> sum;
+    __shared__ GroupSum<kWaves, 1> sum;
     constexpr bool kGated = kAct == kBefore || kAct == kAfter;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast, kMany> place(a, lane, wave);
@@ -151,8 +165,9 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
     auto next = place.row(a, place.r0);
     place.template load<IO>(px, a.x, next);
     if constexpr (kGated) place.template load<IO>(pz, a.z, next);
+    int turn = 0;
     for (unsigned r = place.r0; r < place.r1; r += place.at_once(a)) {
-        float u[kPieces][kPiece], gate[kPieces][kPiece], s0 = 0.0f, s1 = 0.0f;
+        float u[kPieces][kPiece], gate[kPieces][kPiece], total[1] = {0.0f}, mean = 0.0f;
         place.template settled<IO>(px);
         if constexpr (kGated) place.template settled<IO>(pz);
 #pragma unroll
@@ -162,8 +177,6 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
                 u[k][i] = px[k][i];
                 if constexpr (kGated) gate[k][i] = pz[k][i] * sigmoid_of(pz[k][i]);
                 if constexpr (kAct == kBefore) u[k][i] *= gate[k][i];
-                s0 += u[k][i];
-                s1 += u[k][i] * u[k][i];
             }
         const auto row = next;
         if (place.r1 - r > place.at_once(a)) {
@@ -171,23 +184,30 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
             place.template load<IO>(px, a.x, next);
             if constexpr (kGated) place.template load<IO>(pz, a.z, next);
         }
-        sum(s0, s1, a.lanes, wave, 0);
-        float mean = 0.0f;
         if (a.centred) {
-            mean = s0 * inv;
-            s0 = s1 = 0.0f;
 #pragma unroll
             for (int k = 0; k < kPieces; k++)
 #pragma unroll
-                for (int i = 0; i < kPiece; i++) {
-                    u[k][i] -= mean;
-                    s1 += place.in_group || place.at(k) + i < a.n ? u[k][i] * u[k][i] : 0.0f;
-                }
-            sum(s0, s1, a.lanes, wave, 1);
-        } else if constexpr (kWaves > 1) {
-            __syncthreads();
+                for (int i = 0; i < kPiece; i++) total[0] += u[k][i];
+            sum(total, a.lanes, wave, turn);
+            mean = total[0] * inv;
+            total[0] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kPieces; k++)
+#pragma unroll
+                for (int i = 0; i < kPiece; i++) u[k][i] -= mean;
+            if (!place.in_group)
+#pragma unroll
+                for (int k = 0; k < kPieces; k++)
+#pragma unroll
+                    for (int i = 0; i < kPiece; i++) u[k][i] = place.at(k) + i < a.n ? u[k][i] : 0.0f;
         }
-        const float rstd = 1.0f / sqrtf(s1 * inv + a.eps);
+#pragma unroll
+        for (int k = 0; k < kPieces; k++)
+#pragma unroll
+            for (int i = 0; i < kPiece; i++) total[0] += u[k][i] * u[k][i];
+        sum(total, a.lanes, wave, turn);
+        const float rstd = 1.0f / sqrtf(total[0] * inv + a.eps);
 #pragma unroll
         for (int k = 0; k < kPieces; k++)
 #pragma unroll
@@ -206,7 +226,7 @@ __device__ __forceinline__ void group_norm_rows(const GroupNormArgs& a)
 template <typename IO, int kAct, int kWaves, int kPieces, int kPiece, int kTeam, bool kPast, bool kMany>
 __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
 {
-    __shared__ GroupSum<kWaves> sum;
+    __shared__ GroupSum<kWaves, 2> sum;
     constexpr bool kGated = kAct == kBefore || kAct == kAfter;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const GroupPlace<kWaves, kPieces, kPiece, kTeam, kPast, kMany> place(a, lane, wave);   // (r0 >= r1: a wave without rows, which leaves zeros)
@@ -219,7 +239,7 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
         for (int i = 0; i < kPiece; i++) dw[k][i] = db[k][i] = 0.0f;
     const float inv = 1.0f / a.n;
     int turn = 0;
-    for (unsigned r = place.r0; r < place.r1; r += place.at_once(a), turn ^= 1) {
+    for (unsigned r = place.r0; r < place.r1; r += place.at_once(a)) {
         const auto row = place.row(a, r);
         Piece<IO, kPiece> px[kPieces], pz[kPieces], pd[kPieces];
         place.template load<IO>(px, a.x, row);
@@ -230,7 +250,7 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
         if constexpr (kGated) place.template settled<IO>(pz);
         place.template settled<IO>(pd);
         // xh, and k = dv * weight; what dz needs beside them
-        float xh[kPieces][kPiece], g[kPieces][kPiece], dz[kPieces][kPiece], gate[kPieces][kPiece], s0 = 0.0f, s1 = 0.0f;
+        float xh[kPieces][kPiece], g[kPieces][kPiece], dz[kPieces][kPiece], gate[kPieces][kPiece], total[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < kPieces; k++)
 #pragma unroll
@@ -256,11 +276,11 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
                 dw[k][i] += !kMany || row.real ? dv * xh[k][i] : 0.0f;
                 db[k][i] += !kMany || row.real ? dv : 0.0f;
                 g[k][i] = dv * w[k][i];
-                s0 += g[k][i];
-                s1 += g[k][i] * xh[k][i];
+                total[0] += g[k][i];
+                total[1] += g[k][i] * xh[k][i];
             }
-        sum(s0, s1, a.lanes, wave, turn);
-        const float c0 = a.centred ? s0 * inv : 0.0f, c1 = s1 * inv;
+        sum(total, a.lanes, wave, turn);
+        const float c0 = a.centred ? total[0] * inv : 0.0f, c1 = total[1] * inv;
 #pragma unroll
         for (int k = 0; k < kPieces; k++)
 #pragma unroll
