@@ -239,13 +239,27 @@ __device__ __forceinline__ void group_norm_bwd_rows(const GroupNormArgs& a)
         for (int i = 0; i < kPiece; i++) dw[k][i] = db[k][i] = 0.0f;
     const float inv = 1.0f / a.n;
     int turn = 0;
+    struct Read {
+        Piece<IO, kPiece> x[kPieces], z[kPieces], d[kPieces];
+        float mean, rstd;
+    };
+    const auto read = [&](const auto& row) {
+        Read p;
+        place.template load<IO>(p.x, a.x, row);
+        if constexpr (kGated) place.template load<IO>(p.z, a.z, row);
+        place.template load<IO>(p.d, a.dy, row);
+        p.mean = a.centred ? a.mean[(long long)row.r * a.G + place.g] : 0.0f;
+        p.rstd = a.rstd[(long long)row.r * a.G + place.g];
+        return p;
+    };
+    Read ahead;
+    if (kWaves > 1 && place.r0 < place.r1) ahead = read(place.row(a, place.r0));
     for (unsigned r = place.r0; r < place.r1; r += place.at_once(a)) {
         const auto row = place.row(a, r);
-        Piece<IO, kPiece> px[kPieces], pz[kPieces], pd[kPieces];
-        place.template load<IO>(px, a.x, row);
-        if constexpr (kGated) place.template load<IO>(pz, a.z, row);
-        place.template load<IO>(pd, a.dy, row);
-        const float mean = a.centred ? a.mean[(long long)row.r * a.G + place.g] : 0.0f, rstd = a.rstd[(long long)row.r * a.G + place.g];
+        Read now = kWaves > 1 ? ahead : read(row);
+        if (kWaves > 1 && place.r1 - r > place.at_once(a)) ahead = read(place.row(a, r + place.at_once(a)));
+        auto &px = now.x, &pz = now.z, &pd = now.d;
+        const float mean = now.mean, rstd = now.rstd;
         place.template settled<IO>(px);
         if constexpr (kGated) place.template settled<IO>(pz);
         place.template settled<IO>(pd);
