@@ -28,7 +28,8 @@ GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
     const int n = d->d_inner / d->groups, piece = d->io_dtype == BIMAMBA_BF16 ? 8 : 4;
     const int pieces = n < piece ? n : (n + piece - 1) / piece;   // (of one element in small groups)
     // 16 elements a lane at most: 32 of them and the gradients' sums take the registers of half the waves (32768 x 2 groups of 2048, gated: four
-    // waves to a group 130 us, one 139; gradients 234, 265; groups of 8192: eight waves 279, four 296; gradients 496, 605)
+    // waves to a group 127 us, one 138; gradients 241, 262; groups of 8192: eight waves 286, four 293; gradients 501, 502; of 4096: 256,
+    // 263; 478, 507)
     p.waves = n <= 1024 ? 1 : n <= 2048 ? 4 : 8;
     p.lanes = 1;
     while (p.lanes < 64 && p.lanes < pieces) p.lanes *= 2;
@@ -39,10 +40,10 @@ GroupPlan plan_group_norm(const bimamba_group_norm_desc* d, bool bwd)
     while (p.waves == 1 && runs > 1 && runs / 2 >= d->groups) runs /= 2, p.at_once *= 2;
     p.tiles = (d->groups + runs - 1) / runs;
     p.team = p.waves > 1 ? p.waves : bwd && p.pieces == 1 && p.at_once == 1 ? 8 : 4;
-    // Rows: as many as are in hand at once go to one wave each, up to four where there are more (sixteen for the gradients of shared groups, which
-    // otherwise leave a slot as long as two rows for every few of them).
+    // Rows: as many as are in hand at once go to one wave each, up to four where there are more (four to each wave for the gradients of shared
+    // groups, which otherwise leave a slot as long as two rows for every few of them: 65536 groups of 4096 32 rows 492 us, 16 512, 8 527).
     const unsigned rows = (unsigned)((long long)d->batch * d->seqlen), together = (p.waves == 1 ? p.team : 1) * p.at_once;
-    const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 3u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 16 : 4;
+    const unsigned long long fair = (unsigned long long)rows * p.tiles / (together * (bwd ? 3u : 16u) * cu_count()), most = bwd && p.waves > 1 ? 4 * p.waves : 4;
     p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);
     // (a grid's second axis ends at 65535)
     const unsigned long long least = (rows + 65535ull * together - 1) / (65535ull * together);

@@ -10,8 +10,10 @@ namespace bm {
 // each output is rounded once.
 //
 // What bounds it are the bytes, and in which order the memory sees them: a wave takes four rows and goes, so that all waves in hand
-// work on neighbouring rows.  65536 rows of 4096 in groups of 64, gated, past the caches: 4 rows 251 us (6.4 TB/s; a large copy
-// reaches 6.1), 1 row 280, 8 rows 274; through the caches 284; gradients 426 us (6.3 TB/s) in workgroups of eight waves.
+// work on neighbouring rows.  65536 rows of 4096 in groups of 64, gated, past the caches: 4 rows 250 us (6.45 TB/s; two tensors added to a
+// third reach 6.0, past the caches 6.55), 1 row 284, 8 rows 274; through the caches 280; gradients 433 us (6.2 TB/s), 2 rows 461, 8 rows 463,
+// through the caches 478.  Groups that waves share wait at a barrier in each row: their gradients read a row ahead (65536 groups of
+// 4096 511 us, 541 without).
 enum Act { kPlain = BIMAMBA_ACT_NONE, kSilu = BIMAMBA_ACT_SILU, kBefore = BIMAMBA_ACT_GATE_BEFORE, kAfter = BIMAMBA_ACT_GATE_AFTER };
 
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
