@@ -522,13 +522,18 @@ int check_recurrence(const bimamba_recurrence_desc* d)
 }
 
 // Tokens of a wave in a piece, waves of one, channels of a lane.  Short sequences go in one piece of as few registers as hold it, since its
-// time is that of one load after the other (512 x 32 tokens of 4096 channels: 8 x 4 4.6 us, 16 x 8 11.0).  Where there is little to do
-// altogether a lane has one channel and a workgroup sixteen waves: half the work of a wave, half the pieces to look back at (2 x 4096 tokens
-// of 512 channels 15.2 us, with two channels and eight waves 17.9; 2 x 128 5.0 and 6.2).  Else two channels: 16 x 8 forward, 8 x 65536
-// tokens of 4096 channels 383 us (16 x 4 465, 8 x 8 467, 16 x 16 485), in one piece of 16 x 16 up to 256 tokens (16 x 256 of 2048: 14.7 us,
-// two pieces 21.0).  The gradients hold half as much again, so two workgroups of eight waves no longer fit a CU: 16 x 4 477 us
-// (16 x 8 643, 8 x 8 475) where there are more pieces than the chip holds at once, 16 x 8 below (4096 tokens of 2048 channels 28 us, 16 x 4
-// 37).
+// time is that of one load after the other (16 x 32 tokens of 4096 channels: 8 x 4 4.4 us, 16 x 8 9.2).  Two channels a lane take fewer
+// instructions for a byte, one spreads the work over twice the waves.  What there is to spread is the number n of pieces of 128 tokens of 64
+// channels, what has to follow one another a chain's pieces.
+//   Forward (bf16, us, one channel and two): 64 x 128 tokens of 2048 channels (n = 2048) 21.3, 22.5; 128 x 128 of 4096 (8192) 83, 75.
+// Up to 256 tokens in one piece of 16 x 16: 4 x 200 of 4096 (512) 10.5, 14.5; 8 x 200 (1024) 18.6, 15.5; 64 x 256 (8192) 108, in two pieces
+// 97.  Longer ones with one channel in pieces of 16 x 16 and of 16 x 8, and with two of 16 x 8: 700 of 512 (48) 11.7, 8.6, 11.3; 2048 of 2048
+// (512) 13.4, 17.5, 15.0; 8192 of 2048 (2048) 34.2, 39.4, 37.6; 8192 of 4096 (4096) 58.1, 64.2, 53.7; 8 x 2048 of 4096 (8192) 116, 119, 102;
+// but in few chains, 65536 of 512 (4096) 62.7, -, 117.
+//   The gradients hold half as much again, so with two channels two workgroups of eight waves no longer fit a CU.  One channel 16 x 16 and 16 x 8,
+// two channels 16 x 8 and 16 x 4: 700 of 512 15.3, 10.0, 13.2, 12.5; 2048 of 2048 16.7, 20.0, 17.9, 22.4; 8192 of 2048 46.9, 45.1, 48.4, 51.6;
+// 8 x 2048 of 4096 170, 160, 161, 150; in few chains, 65536 of 512 98, 99, 116, 192, of 256 51, 77, 110, 179.  fp32 has one channel a lane:
+// 4 x 8192 of 4096 16 x 16 544, 16 x 8 503, 16 x 4 506; forward 321, 302, 430.
 struct RecurPlan {
     int tokens, waves, pieces;
     int channels;
@@ -540,16 +545,18 @@ RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
     const int L = d->seqlen;
     const auto pieces = [&](int steps) { return (L + steps - 1) / steps; };
     const auto tiles = [&](int channels) { return (d->d_inner + 64 * channels - 1) / (64 * channels); };
-    const bool little = L > 64 && (L <= 256 || L > 1024) && (long long)tiles(1) * d->batch * pieces(256) <= cu_count();
-    p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 64 && !little ? 2 : 1;
+    const long long cus = cu_count(), chains = (long long)tiles(1) * d->batch, n = chains * pieces(128);
+    const bool some = n <= 8 * cus, one = back ? some || chains <= cus / 4 : L <= 128 ? some : L <= 256 ? n <= 2 * cus : some || chains <= cus / 16;
+    p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 64 && (L <= 64 || !one) ? 2 : 1;
     p.tiles = tiles(p.channels);
     if (L == 1 && !back) p.tokens = 1, p.waves = 1;
     else if (L <= 4) p.tokens = 4, p.waves = 1;
     else if (L <= 32) p.tokens = 8, p.waves = 4;
-    else if (L <= 64) p.tokens = 16, p.waves = 4;
-    else if (little) p.tokens = L <= 128 ? 8 : 16, p.waves = 16;
-    else if (back) p.tokens = 16, p.waves = (long long)p.tiles * d->batch * pieces(128) <= 2 * cu_count() ? 8 : 4;
-    else p.tokens = 16, p.waves = L > 128 && L <= 256 ? 16 : 8;
+    else if (L <= 64 || (back && p.channels == 2)) p.tokens = 16, p.waves = 4;
+    else if (L <= 128) p.tokens = 16, p.waves = 8;
+    else if (back) p.tokens = 16, p.waves = n > cus && (n <= 4 * cus || chains <= cus / 32) ? 16 : 8;
+    else if (L <= 256) p.tokens = 16, p.waves = some ? 16 : 8;
+    else p.tokens = 16, p.waves = p.channels == 1 && n > cus && (some || chains <= cus / 16) ? 16 : 8;
     p.pieces = pieces(p.tokens * p.waves);
     return p;
 }
@@ -570,30 +577,26 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     a.look = look < 1 ? 1 : look > most ? most : look;
     if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 255) / 256), a.batch), dim3(256), 0, st, a);
     const dim3 grid(p.tiles * (unsigned)a.batch * p.pieces), wg(64 * p.waves);
-    const auto form = [&](auto tokens, auto waves, auto beyond) {
+    const auto form = [&](auto tokens, auto waves) {
         constexpr int kT = decltype(tokens)::value, kW = decltype(waves)::value;
-        constexpr bool kBeyond = kPast && decltype(beyond)::value;   // (the others never move more than the caches hold, or are not compiled for it)
         if (p.tokens != kT || p.waves != kW) return;
         if (back) {
-            if constexpr (kT > 1 && (kC == 1 || kW < 16)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kBeyond>), grid, wg, 0, st, a);
+            if constexpr (kT > 1 && (kC == 1 || kT * kW <= 64)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
         } else {
-            hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kBeyond>), grid, wg, 0, st, a);
+            hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
         }
     };
     using std::integral_constant;
-    const integral_constant<bool, true> yes{};
-    const integral_constant<bool, false> no{};
     const integral_constant<int, 1> n1{};
     const integral_constant<int, 4> n4{};
     const integral_constant<int, 8> n8{};
     const integral_constant<int, 16> n16{};
-    form(n1, n1, yes);
-    form(n4, n1, yes);
-    form(n8, n4, yes);
-    form(n16, n4, yes);
-    form(n16, n8, yes);
-    if constexpr (kC == 1) form(n8, n16, no);
-    form(n16, n16, yes);
+    form(n1, n1);
+    form(n4, n1);
+    form(n8, n4);
+    form(n16, n4);
+    form(n16, n8);
+    form(n16, n16);
 }
 template <typename IO, int kC>
 void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool on_lines, bool back, hipStream_t st)
