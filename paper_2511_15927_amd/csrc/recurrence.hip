@@ -13,7 +13,8 @@ namespace bm {
 // handed out before its own only, by workgroups that run, so every wait ends.
 //
 // Everything is in fp32: a, u, the states; y is rounded once.  1 - a is formed beside a from the same exponential, not as a difference, so
-// that neither loses digits where the other is near 1: with e = exp(-|v|), sigmoid(|v|) = 1 - e / (1 + e) and sigmoid(-|v|) = e / (1 + e).
+// that it loses no digits where a is near 1: with e = exp(-v), a = 1 / (1 + e) and 1 - a = e a; e is cut at 2^126, where a is 2^-126 for
+// what is less.  (Both from exp(-|v|), with selections for the sign of v: 8 x 8192 tokens of 4096 channels 356 us, so 332.)
 constexpr int kKeep = BIMAMBA_RECURRENCE_KEEP;   // steps between two kept states
 
 enum Gate { kLog, kSigmoid };
@@ -117,9 +118,9 @@ template <int kGate>
 __device__ __forceinline__ void gate_of(float g, float bias, float& a, float& q)
 {
     if constexpr (kGate == kSigmoid) {
-        const float v = g + bias, e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), low = e * __builtin_amdgcn_rcpf(1.0f + e), high = 1.0f - low;
-        a = v > 0.0f ? high : low;
-        q = v > 0.0f ? low : high;
+        const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-kLog2e * (g + bias), 126.0f));   // (a NaN stays one)
+        a = __builtin_amdgcn_rcpf(1.0f + e);
+        q = e * a;
     } else {
         a = __builtin_amdgcn_exp2f(kLog2e * (g > 0.0f ? 0.0f : g));   // (a NaN stays one)
         q = g > 0.0f ? 0.0f : a;
