@@ -191,13 +191,17 @@ constexpr unsigned kXcds = 8;
 __device__ __forceinline__ unsigned queue_of(unsigned chains, unsigned q, unsigned queues) { return queues == 1 ? q * chains : q * chains / kXcds; }
 // Before the pieces: nothing is there but what enters the first one.  (The state that enters is read here only: it may be the one that the
 // last piece replaces.)
+constexpr int kCleared = 8;   // words of a thread
 __global__ __launch_bounds__(256) void recur_clear_kernel(const RecurArgs r)
 {
-    const long long n = (long long)r.pieces * r.d, i = blockIdx.x * 256ll + threadIdx.x;
+    const long long n = (long long)r.pieces * r.d, first = blockIdx.x * (256ll * kCleared) + threadIdx.x;
     const int b = blockIdx.y;
-    if (i < kXcds && b == 0) r.ticket[i] = 0;
-    if (i >= n) return;
-    r.slots[b * n + i] = i < r.d ? (r.enter ? __float_as_uint(r.enter[(long long)b * r.d + i]) : 0) : ~0ull;
+    if (first < kXcds && b == 0) r.ticket[first] = 0;
+#pragma unroll
+    for (int k = 0; k < kCleared; k++) {
+        const long long i = first + k * 256;
+        if (i < n) r.slots[b * n + i] = i < r.d ? (r.enter ? __float_as_uint(r.enter[(long long)b * r.d + i]) : 0) : ~0ull;
+    }
 }
 
 // What a workgroup's waves share.
@@ -576,7 +580,7 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     const int look = (int)(cu_count() / (2u * p.tiles * (unsigned)a.batch));
     const int most = p.waves < 8 ? 8 : p.waves;
     a.look = look < 1 ? 1 : look > most ? most : look;
-    if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 255) / 256), a.batch), dim3(256), 0, st, a);
+    if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 256 * kCleared - 1) / (256 * kCleared)), a.batch), dim3(256), 0, st, a);
     const dim3 grid(p.tiles * (unsigned)a.batch * p.pieces), wg(64 * p.waves);
     const auto form = [&](auto tokens, auto waves) {
         constexpr int kT = decltype(tokens)::value, kW = decltype(waves)::value;

@@ -7,6 +7,8 @@ and normalised by groups of channels, and comes back as x + gate(tau) * dropout(
 dropout, the log probabilities and the clipping are calls of the library, forward and backward; the projections are plain matrix
 products of torch.  embed(), layer_norm(), mixer(), recurrence(), group_norm(), dropout_add() and log_probs() take part in autograd and
 can be used on their own; they have first derivatives only, and a gradient through them that is itself differentiated is an error.
+They can be captured into a graph; a captured step takes its gradients with torch.autograd.grad, or runs backward() while no graph of the
+same parameters that was made outside the capture is alive.
 
     python -m paper_2511_15927_amd.denoiser [--steps 200] [--width 256] [--layers 4] [--io bf16] [--mixer recurrence --dropout 0.1]
 
