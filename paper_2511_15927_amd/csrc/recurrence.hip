@@ -6,7 +6,8 @@ namespace bm {
 // The sequence is cut into pieces of kW waves times kT tokens, a workgroup each for the channels of one wave, whose tokens stay in
 // registers.  A wave first runs its tokens from a state of zero, which gives the state E that they add and the factor P that they put
 // on what enters; the pairs are exchanged through shared memory, folded onto the state that enters the piece, and the tokens run again
-// from there: the activations are read once.  What enters a piece comes from those before it.  A workgroup publishes its piece's (P, E),
+// from there: the activations are read once.  (32 tokens of a wave stay as they were read, and their gates are formed twice: what they take in
+// registers is half.)  What enters a piece comes from those before it.  A workgroup publishes its piece's (P, E),
 // looks back, and then publishes what leaves the piece as (0, h).  A pair is one word of 64
 // bits, written and read whole, so that no fence is needed; a word of ones says that nothing is there yet.  Pieces are handed out by a
 // counter in the order of the walk, all channels and sequences of a step before the next step: a workgroup waits for pieces that were
@@ -303,7 +304,17 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
     const int s0 = (piece.turn * kW + w) * kT;
     const Steps<IO, kC, kT, kPast, kWhole> steps(places, piece.b, s0, r.L, piece.first, lane, r.d);
     Piece<IO, kC> x[kT], g[kT], add[kT];
-    float bias[kC], a[kT][kC], u[kT][kC], h[kC];
+    constexpr bool kAgain = kT > 16;
+    float bias[kC] = {}, a[kAgain ? 1 : kT][kC], u[kAgain ? 1 : kT][kC], h[kC];
+    const auto gates = [&](int i, float (&at)[kC], float (&ut)[kC]) {
+#pragma unroll
+        for (int j = 0; j < kC; j++) {
+            float q;
+            gate_of<kGate>(g[i][j], bias[j], at[j], q);
+            ut[j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
+            if (!steps.inside(i)) at[j] = 1.0f, ut[j] = 0.0f;
+        }
+    };
     if (r.pieces == 1) steps.load_params(h, r.enter ? r.enter + (long long)piece.b * r.d : nullptr);
 #pragma unroll
     for (int i = 0; i < kT; i++) add[i] = Piece<IO, kC>{};
@@ -312,25 +323,29 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
     for (int j = 0; j < kC; j++) mine.p[j] = 1.0f, mine.e[j] = 0.0f;
     if (steps.idle()) {
 #pragma unroll
-        for (int i = 0; i < kT; i++)
+        for (int i = 0; i < kT; i++) {
+            x[i] = g[i] = Piece<IO, kC>{};
+            if constexpr (!kAgain)
 #pragma unroll
-            for (int j = 0; j < kC; j++) a[i][j] = 1.0f, u[i][j] = 0.0f;
+                for (int j = 0; j < kC; j++) a[i][j] = 1.0f, u[i][j] = 0.0f;
+        }
     } else {
         steps.load(x, r.x);
         steps.load(g, r.g);
         steps.load_params(bias, r.bias);
-        if (r.add.p) steps.load(add, r.add);
+        if (!kAgain && r.add.p) steps.load(add, r.add);
 #pragma unroll
-        for (int i = 0; i < kT; i++)
+        for (int i = 0; i < kT; i++) {
+            float at[kC], ut[kC];
+            gates(i, at, ut);
 #pragma unroll
             for (int j = 0; j < kC; j++) {
-                float q;
-                gate_of<kGate>(g[i][j], bias[j], a[i][j], q);
-                u[i][j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
-                if (!steps.inside(i)) a[i][j] = 1.0f, u[i][j] = 0.0f;
-                mine.e[j] = a[i][j] * mine.e[j] + u[i][j];
-                mine.p[j] *= a[i][j];
+                if constexpr (!kAgain) a[i][j] = at[j], u[i][j] = ut[j];
+                mine.e[j] = at[j] * mine.e[j] + ut[j];
+                mine.p[j] *= at[j];
             }
+        }
+        if (kAgain && r.add.p) steps.load(add, r.add);
     }
     Link<kC> all = mine, before;
     if constexpr (kW > 1) {
@@ -360,10 +375,15 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
     if (r.states && s0 % kKeep == 0 && s0 < r.L) steps.store_params(r.states + ((long long)piece.b * ((r.L + kKeep - 1) / kKeep) + s0 / kKeep) * r.d, h);
 #pragma unroll
     for (int i = 0; i < kT; i++) {
-        float f[kC];
+        float f[kC], at[kC], ut[kC];
+        if constexpr (kAgain) {
+            hold(x[i]), hold(g[i]);
+            gates(i, at, ut);
+        }
 #pragma unroll
         for (int j = 0; j < kC; j++) {
-            h[j] = a[i][j] * h[j] + u[i][j];
+            if constexpr (!kAgain) at[j] = a[i][j], ut[j] = u[i][j];
+            h[j] = at[j] * h[j] + ut[j];
             f[j] = steps.inside(i) ? h[j] + add[i][j] : 0.0f;
         }
         steps.store(r.y, i, f);
@@ -531,10 +551,12 @@ int check_recurrence(const bimamba_recurrence_desc* d)
 // instructions for a byte, one spreads the work over twice the waves.  What there is to spread is the number n of pieces of 128 tokens of 64
 // channels, what has to follow one another a chain's pieces.
 //   Forward (bf16, us, one channel and two): 64 x 128 tokens of 2048 channels (n = 2048) 21.3, 22.5; 128 x 128 of 4096 (8192) 83, 75.
-// Up to 256 tokens in one piece of 16 x 16: 4 x 200 of 4096 (512) 10.5, 14.5; 8 x 200 (1024) 18.6, 15.5; 64 x 256 (8192) 108, in two pieces
-// 97.  Longer ones with one channel in pieces of 16 x 16 and of 16 x 8, and with two of 16 x 8: 700 of 512 (48) 11.7, 8.6, 11.3; 2048 of 2048
-// (512) 13.4, 17.5, 15.0; 8192 of 2048 (2048) 34.2, 39.4, 37.6; 8192 of 4096 (4096) 58.1, 64.2, 53.7; 8 x 2048 of 4096 (8192) 116, 119, 102;
-// but in few chains, 65536 of 512 (4096) 62.7, -, 117.
+// Up to 256 tokens in one piece, of 16 x 16 with one channel and of 32 x 8 with two: 4 x 200 of 4096 (512) 10.5, 14.5; 16 x 256 of 2048 (1024) 15.1,
+// 14.1; 32 x 256 (2048) 27.6, 23.2; in two of 16 x 8 64 x 256 of 4096 (8192) 97, in one 87; fp32 64 x 200 of 2048 79, 72.
+// Longer ones with one channel in pieces of 16 x 16 and of 16 x 8, and with two of 16 x 8 and 32 x 8: 700 of 512 (48) 11.7, 8.6, 11.3, -; 2048 of 2048
+// (512) 13.4, 17.5, 15.0, -; 8192 of 2048 (2048) 34.2, 39.4, 37.6, 39.0; 8 x 2048 of 4096 (8192) 116, 119, 102, 91; 8 x 4096 (16384) 216, -, 169, 172;
+// 8 x 8192 with add -, -, 373, 379; 64 x 600 of 2048 (10240), whose last piece is not filled, 172, -, 120, 130; in few chains, 65536 of 512 (4096)
+// 61, -, 117, 77; of 1024 122, -, 133, 109; of 2048 227, -, 185, 174.
 //   The gradients hold half as much again, so with two channels two workgroups of eight waves no longer fit a CU.  One channel 16 x 16 and 16 x 8,
 // two channels 16 x 8 and 16 x 4: 700 of 512 15.3, 10.0, 13.2, 12.5; 2048 of 2048 16.7, 20.0, 17.9, 22.4; 8192 of 2048 46.9, 45.1, 48.4, 51.6;
 // 8 x 2048 of 4096 170, 160, 161, 150; in few chains, 65536 of 512 98, 99, 116, 192, of 256 51, 77, 110, 179.  fp32 has one channel a lane:
@@ -551,17 +573,20 @@ RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
     const auto pieces = [&](int steps) { return (L + steps - 1) / steps; };
     const auto tiles = [&](int channels) { return (d->d_inner + 64 * channels - 1) / (64 * channels); };
     const long long cus = cu_count(), chains = (long long)tiles(1) * d->batch, n = chains * pieces(128);
-    const bool some = n <= 8 * cus, one = back ? some || chains <= cus / 4 : L <= 128 ? some : L <= 256 ? n <= 2 * cus : some || chains <= cus / 16;
+    const bool some = n <= 8 * cus, one = back ? some || chains <= cus / 4 : L <= 128 ? some : L <= 256 ? n <= 2 * cus : some || chains <= cus / 32;
     p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 64 && (L <= 64 || !one) ? 2 : 1;
     p.tiles = tiles(p.channels);
+    const bool words = p.channels == 2 || d->io_dtype == BIMAMBA_F32;   // (of 32 bits, as 32 tokens take it)
+    p.tokens = 16, p.waves = 8;
     if (L == 1 && !back) p.tokens = 1, p.waves = 1;
     else if (L <= 4) p.tokens = 4, p.waves = 1;
     else if (L <= 32) p.tokens = 8, p.waves = 4;
-    else if (L <= 64 || (back && p.channels == 2)) p.tokens = 16, p.waves = 4;
-    else if (L <= 128) p.tokens = 16, p.waves = 8;
-    else if (back) p.tokens = 16, p.waves = n > cus && (n <= 4 * cus || chains <= cus / 32) ? 16 : 8;
-    else if (L <= 256) p.tokens = 16, p.waves = some ? 16 : 8;
-    else p.tokens = 16, p.waves = p.channels == 1 && n > cus && (some || chains <= cus / 16) ? 16 : 8;
+    else if (L <= 64 || (back && p.channels == 2)) p.waves = 4;
+    else if (L <= 128) p.waves = 8;
+    else if (back) p.waves = n > cus && (n <= 4 * cus || chains <= cus / 32) ? 16 : 8;
+    else if (L <= 256) one || !words ? p.waves = 16 : p.tokens = 32;
+    else if (p.channels == 1) p.waves = n > cus && one ? 16 : 8;
+    else if (16 * pieces(256) <= 9 * pieces(128) && (n <= 32 * cus || chains <= cus / 2)) p.tokens = 32;
     p.pieces = pieces(p.tokens * p.waves);
     return p;
 }
@@ -586,7 +611,7 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
         constexpr int kT = decltype(tokens)::value, kW = decltype(waves)::value;
         if (p.tokens != kT || p.waves != kW) return;
         if (back) {
-            if constexpr (kT > 1 && (kC == 1 || kT * kW <= 64)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
+            if constexpr (kT > 1 && (kC == 1 ? kT < 32 : kT * kW <= 64)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
         } else {
             hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
         }
@@ -596,12 +621,14 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     const integral_constant<int, 4> n4{};
     const integral_constant<int, 8> n8{};
     const integral_constant<int, 16> n16{};
+    const integral_constant<int, 32> n32{};
     form(n1, n1);
     form(n4, n1);
     form(n8, n4);
     form(n16, n4);
     form(n16, n8);
-    form(n16, n16);
+    if constexpr (kC == 1) form(n16, n16);
+    if constexpr (sizeof(Piece<IO, kC>) == 4) form(n32, n8);
 }
 template <typename IO, int kC>
 void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool on_lines, bool back, hipStream_t st)
