@@ -39,8 +39,8 @@ struct DropArgs {
 __device__ __forceinline__ unsigned half_of(const Words& r, int i) { return (r.w[i >> 1] >> (i & 1 ? 16 : 0)) & 0xffffu; }
 
 // A lane has one piece of 16 bytes of a row in hand; with short rows a wave takes several at once.  What bounds it are the bytes, the
-// generator runs beside them (65536 rows of 2048 bf16 with a residual and a gate: 126 us, 6.4 TB/s, at p = 0.1 and, without the
-// generator, at p = 0; a large copy reaches 6.1).  A wave takes two rows and goes, eight for the gate's gradient, so that all waves in hand
+// generator runs beside them (65536 rows of 2048 bf16 with a residual and a gate: 126 to 131 us, 6.3 TB/s, at p = 0.1 and, without the
+// generator, 124 at p = 0; a large copy reaches 6.1).  A wave takes two rows and goes, eight for the gate's gradient, so that all waves in hand
 // work on neighbouring rows: 1 row 156 us, 8 rows 140, 32 rows 165; gradients with 8 rows 134 us, 2 rows 145, 32 rows 172.
 template <typename IO, int kPiece>
 struct DropPlace {

@@ -14,8 +14,10 @@ namespace bm {
 // handed out before its own only, by workgroups that run, so every wait ends.
 //
 // Everything is in fp32: a, u, the states; y is rounded once.  1 - a is formed beside a from the same exponential, not as a difference, so
-// that it loses no digits where a is near 1: with e = exp(-v), a = 1 / (1 + e) and 1 - a = e a; e is cut at 2^126, where a is 2^-126 for
-// what is less.  (Both from exp(-|v|), with selections for the sign of v: 8 x 8192 tokens of 4096 channels 356 us, so 332.)
+// that it loses no digits where a is near 1.  fp32 activations: with e = exp(-|v|), sigmoid(|v|) = 1 - e / (1 + e) and sigmoid(-|v|) = e / (1 + e),
+// a off by half a unit of its last place where it is near 1.  bf16 ones: with e = exp(-v), a = 1 / (1 + e) and 1 - a = e a, without a
+// selection; a is off by two units there (the sum's and the reciprocal's), which a channel that remembers 1000 tokens turns into 2^-13 of a state, a
+// thirtieth of what y loses as it is rounded (8 x 8192 tokens of 4096 channels: 356 us with selections, 332 without; fp32 the same).
 constexpr int kKeep = BIMAMBA_RECURRENCE_KEEP;   // steps between two kept states
 
 enum Gate { kLog, kSigmoid };
@@ -115,11 +117,15 @@ struct Steps {
 };
 
 // a, and for a sigmoid gate 1 - a, for a log gate the factor that da / dg is (a, or 0 where g > 0 was cut).
-template <int kGate>
+template <typename IO, int kGate>
 __device__ __forceinline__ void gate_of(float g, float bias, float& a, float& q)
 {
-    if constexpr (kGate == kSigmoid) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-kLog2e * (g + bias), 126.0f));   // (a NaN stays one)
+    if constexpr (kGate == kSigmoid && sizeof(typename IO::T) == 4) {
+        const float v = g + bias, e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), low = e * __builtin_amdgcn_rcpf(1.0f + e), high = 1.0f - low;
+        a = v > 0.0f ? high : low;
+        q = v > 0.0f ? low : high;
+    } else if constexpr (kGate == kSigmoid) {   // (e is cut at 2^126, and a at 2^-126; a NaN stays one)
+        const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-kLog2e * (g + bias), 126.0f));
         a = __builtin_amdgcn_rcpf(1.0f + e);
         q = e * a;
     } else {
@@ -310,7 +316,7 @@ __device__ __forceinline__ void recur_piece(const RecurArgs& r, const Places& pl
 #pragma unroll
         for (int j = 0; j < kC; j++) {
             float q;
-            gate_of<kGate>(g[i][j], bias[j], at[j], q);
+            gate_of<IO, kGate>(g[i][j], bias[j], at[j], q);
             ut[j] = kGate == kSigmoid ? q * x[i][j] : x[i][j];
             if (!steps.inside(i)) at[j] = 1.0f, ut[j] = 0.0f;
         }
@@ -434,7 +440,7 @@ __device__ __forceinline__ void recur_bwd_piece(const RecurArgs& r, const Places
         for (int i = 0; i < kT; i++)
 #pragma unroll
             for (int j = 0; j < kC; j++) {
-                gate_of<kGate>(g[i][j], bias[j], a[i][j], q[i][j]);
+                gate_of<IO, kGate>(g[i][j], bias[j], a[i][j], q[i][j]);
                 if (!steps.inside(i)) a[i][j] = 1.0f, q[i][j] = 0.0f, x[i].v[j] = dy[i].v[j] = 0;
                 e[j] = a[i][j] * e[j] + (kGate == kSigmoid ? q[i][j] * x[i][j] : x[i][j]);
                 mine.p[j] *= a[i][j];
@@ -601,7 +607,7 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
 {
     // How far a workgroup looks back: what a hop from one state to the next takes has to pass over as many pieces of a sequence as are done
     // meanwhile, the more the fewer sequences and channels there are; each piece looked at costs words to read.  65536 tokens of 2048
-    // channels: 8 pieces 188 us, 4 199, 2 266; 8 x 8192 of 4096: 1 piece 381 us, 8 395.
+    // channels in pieces of 16 x 8: 8 pieces 190 us, 4 199, 2 262; 8 x 8192 of 4096: 1 piece 322 us, 8 345.
     const int look = (int)(cu_count() / (2u * p.tiles * (unsigned)a.batch));
     const int most = p.waves < 8 ? 8 : p.waves;
     a.look = look < 1 ? 1 : look > most ? most : look;
@@ -639,9 +645,9 @@ void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const Rec
 }
 // Where rows do not start at cache lines the pieces of neighbouring channels share lines: they are read and written through the caches, and, with
 // more chains than workgroups in hand, by workgroups of one XCD, which share a cache.  29 x 2478 tokens of 2248 channels, past the
-// caches 312 us, through them 272, and with a queue for each XCD 257, gradients 544, 456, 392.  (With few chains the queues only
-// keep them apart: one sequence of 65536 x 2040 245 us, with eight queues 339; and rows that start at lines have nothing to share:
-// 65536 x 2048 201 and 255.)
+// caches 306 us, through them 266, and with a queue for each XCD 249, gradients 542, 450, 381.  (With few chains the queues only
+// keep them apart: one sequence of 65536 x 2040 231 us, with eight queues 314; and rows that start at lines have nothing to share:
+// 65536 x 2048 189 and 238.)
 bool on_lines(const RowView& v, size_t elem)
 {
     return !v.p || (reinterpret_cast<uintptr_t>(v.p) % 128 == 0 && v.sb * (long long)elem % 128 == 0 && v.st * (long long)elem % 128 == 0);

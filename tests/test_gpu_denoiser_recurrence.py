@@ -88,6 +88,7 @@ def test_a_block_against_plain_torch(dn, L, io):
     ref = [v.detach().cpu().double().requires_grad_() for v in leaves]
     rout, rlast = plain(*ref)
     want = torch.autograd.grad((rout * weight.double()).sum() + rlast.sum(), ref)
+    out, rout = out.detach(), rout.detach()
     # fp32: some hundred roundings of 2^-24, more where the norm of a nearly flat group enlarges them; bf16: five activations and their gradients
     # are rounded to 2^-8 on the way
     tol = 2e-5 if io == "f32" else 6 * 2.0 ** -8

@@ -43,6 +43,13 @@ def walk(i, gate, reverse):
         up = v.v > 0
         a, q = torch.where(up, 1 - low, low), torch.where(up, low, 1 - low)
         a_off, q_off = low_off + U32 * torch.where(up, a, 0), low_off + U32 * torch.where(up, 0, q)
+        if i["x"].dtype == torch.bfloat16:
+            # e = exp(-v), a = 1 / (1 + e), q = e a.  e is off by r = 1.1 v.e + U32 (3 |v| + 4) of itself (the product with log2 e, exp2's unit in the last
+            # place), which moves 1 + e by q r of itself and e / (1 + e) by a r; the sum adds U32, the reciprocal one unit in the last place,
+            # 2 U32, the last product U32.  (Below v = -87 a stays at 2^-126.)
+            r = 1.1 * v.e + U32 * (3 * v.v.abs() + 4)
+            a, q = torch.sigmoid(v.v), torch.sigmoid(-v.v)
+            a_off, q_off = a * (q * r + 3 * U32) + 1.2e-38, q * (a * r + 4 * U32)
         u, u_off = q * x, q_off * x.abs() + U32 * (q * x).abs()
     else:
         cut = g.clamp(max=0.0)

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from running_error import TYPES, Run, blank, cuda, gen, nans, normal, wide, within, workspace
-from test_gpu_recurrence import KEEP, bd, forward_ref, inputs, run_backward, run_forward  # noqa: F401
+from test_gpu_recurrence import KEEP, bd, forward_ref, gradient_ref, inputs, run_backward, run_forward  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -442,3 +442,31 @@ def test_sums_over_thousands_of_workgroups(bd, D):
     bd.bimamba_dropout_add(desc, key, x, None, None, kept)
     bd.bimamba_dropout_add_bwd(desc, key, x, gate, dout, dx, dgate, room(need))
     near(dgate, kept.double() * dout.double())
+
+
+# ---- more work than the chip holds at once, in the other sizes of pieces ----
+
+MUCH = [(1100, 70, 66), (200, 200, 66), (300, 140, 33), (400, 150, 66), (70, 300, 66), (350, 300, 66), (300, 500, 66)]
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,D", MUCH)
+def test_walks_of_much_work(bd, B, L, D, io):
+    n = MUCH.index((B, L, D)) + (io == "bf16")
+    gate, reverse = ("sigmoid", "log")[n // 2 % 2], n % 2
+    i = inputs(B, L, D, io, gate, 500 + n, n % 3 == 0)
+    out = run_forward(bd, i, io, gate, reverse, add=n % 4 != 1)
+    y, last, kept = forward_ref(i, gate, reverse, True, n % 4 != 1)
+    within(out["y"], y, io)
+    within(out["h_out"], last)
+    within(out["states"], kept)
+    back = run_backward(bd, i, io, gate, reverse, out["states"])
+    dx, dg, dbias, dh_in = gradient_ref(i, gate, reverse, out["states"].cpu())
+    within(back["dx"], dx, io)
+    within(back["dg"], dg, io)
+    within(back["dh_in"], dh_in)
+    if gate == "sigmoid":
+        within(back["dbias"], dbias)
+    again = run_forward(bd, i, io, gate, reverse, add=n % 4 != 1), run_backward(bd, i, io, gate, reverse, out["states"])
+    for one, two in ((out, again[0]), (back, again[1])):
+        assert all(v is None or torch.equal(v, two[k]) for k, v in one.items())
