@@ -562,7 +562,8 @@ int check_recurrence(const bimamba_recurrence_desc* d)
 // Longer ones with one channel in pieces of 16 x 16 and of 16 x 8, and with two of 16 x 8 and 32 x 8: 700 of 512 (48) 11.7, 8.6, 11.3, -; 2048 of 2048
 // (512) 13.4, 17.5, 15.0, -; 8192 of 2048 (2048) 34.2, 39.4, 37.6, 39.0; 8 x 2048 of 4096 (8192) 116, 119, 102, 91; 8 x 4096 (16384) 216, -, 169, 172;
 // 8 x 8192 with add -, -, 373, 379; 64 x 600 of 2048 (10240), whose last piece is not filled, 172, -, 120, 130; in few chains, 65536 of 512 (4096)
-// 61, -, 117, 77; of 1024 122, -, 133, 109; of 2048 227, -, 185, 174.
+// 61, -, 117, 77; of 1024 122, -, 133, 109; of 2048 227, -, 185, 174; where a chain's pieces are most of it, 8192 of 64 (64) 13.5, 14.8; 4096 of 512
+// (256) 11.9, 12.5; 2048 of 512 (128) 10.5, 9.3.
 //   The gradients hold half as much again, so with two channels two workgroups of eight waves no longer fit a CU.  One channel 16 x 16 and 16 x 8,
 // two channels 16 x 8 and 16 x 4: 700 of 512 15.3, 10.0, 13.2, 12.5; 2048 of 2048 16.7, 20.0, 17.9, 22.4; 8192 of 2048 46.9, 45.1, 48.4, 51.6;
 // 8 x 2048 of 4096 170, 160, 161, 150; in few chains, 65536 of 512 98, 99, 116, 192, of 256 51, 77, 110, 179.  fp32 has one channel a lane:
@@ -582,6 +583,7 @@ RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
     const bool some = n <= 8 * cus, one = back ? some || chains <= cus / 4 : L <= 128 ? some : L <= 256 ? n <= 2 * cus : some || chains <= cus / 32;
     p.channels = d->io_dtype == BIMAMBA_BF16 && d->d_inner > 64 && (L <= 64 || !one) ? 2 : 1;
     p.tiles = tiles(p.channels);
+    const bool far = n > cus || pieces(128) >= 32;
     const bool words = p.channels == 2 || d->io_dtype == BIMAMBA_F32;   // (of 32 bits, as 32 tokens take it)
     p.tokens = 16, p.waves = 8;
     if (L == 1 && !back) p.tokens = 1, p.waves = 1;
@@ -589,9 +591,9 @@ RecurPlan plan_recurrence(const bimamba_recurrence_desc* d, bool back)
     else if (L <= 32) p.tokens = 8, p.waves = 4;
     else if (L <= 64 || (back && p.channels == 2)) p.waves = 4;
     else if (L <= 128) p.waves = 8;
-    else if (back) p.waves = n > cus && (n <= 4 * cus || chains <= cus / 32) ? 16 : 8;
+    else if (back) p.waves = far && (n <= 4 * cus || chains <= cus / 32) ? 16 : 8;
     else if (L <= 256) one || !words ? p.waves = 16 : p.tokens = 32;
-    else if (p.channels == 1) p.waves = n > cus && one ? 16 : 8;
+    else if (p.channels == 1) p.waves = far && one ? 16 : 8;
     else if (16 * pieces(256) <= 9 * pieces(128) && (n <= 32 * cus || chains <= cus / 2)) p.tokens = 32;
     p.pieces = pieces(p.tokens * p.waves);
     return p;
