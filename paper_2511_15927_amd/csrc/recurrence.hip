@@ -610,7 +610,8 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     // How far a workgroup looks back: what a hop from one state to the next takes has to pass over as many pieces of a sequence as are done
     // meanwhile, the more the fewer sequences and channels there are; each piece looked at costs words to read.  65536 tokens of 2048
     // channels in pieces of 16 x 8: 8 pieces 190 us, 4 199, 2 262; 8 x 8192 of 4096: 1 piece 322 us, 8 345.
-    const int look = (int)(cu_count() / (2u * p.tiles * (unsigned)a.batch));
+    // (Of the gradients' pieces of four waves there are twice as many: 2 x 16384 of 4096, 2 pieces 273 us, 4 264.)
+    const int look = (int)((p.waves <= 4 ? 2u : 1u) * cu_count() / (2u * p.tiles * (unsigned)a.batch));
     const int most = p.waves < 8 ? 8 : p.waves;
     a.look = look < 1 ? 1 : look > most ? most : look;
     if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 256 * kCleared - 1) / (256 * kCleared)), a.batch), dim3(256), 0, st, a);
