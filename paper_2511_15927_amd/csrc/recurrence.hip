@@ -548,7 +548,7 @@ int check_recurrence(const bimamba_recurrence_desc* d)
     if (!known_dtype(d->io_dtype) || (d->gate != BIMAMBA_GATE_LOG && d->gate != BIMAMBA_GATE_SIGMOID)) return BIMAMBA_ERR_UNSUPPORTED;
     if (d->batch > 65535 || d->d_inner > kMaxWidth) return BIMAMBA_ERR_UNSUPPORTED;
     // (a grid holds 2^32 threads: up to four tokens are one wave's, else a piece has four waves for each 64 steps at most)
-    const long long pieces = ((d->seqlen + 63) / 64) * (long long)d->batch * ((d->d_inner + 63) / 64);
+    const long long pieces = ((d->seqlen + 63ll) / 64) * d->batch * ((d->d_inner + 63) / 64);
     return d->seqlen > 4 && pieces >= 1ll << 23 ? BIMAMBA_ERR_UNSUPPORTED : BIMAMBA_OK;
 }
 

@@ -299,7 +299,7 @@ PyObject* recurrence(PyObject* const* a)   // desc, x, g, bias, add, lengths, h_
 {
     Reader r;
     const auto d = r.desc<bimamba_recurrence_desc>(a[0]);
-    const int64_t D = d.d_inner, kept = (d.seqlen + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
+    const int64_t D = d.d_inner, kept = (int64_t(d.seqlen) + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
     const auto x = r.rows(a[1], "x", d.io_dtype, d.batch, d.seqlen, D), g = r.rows(a[2], "g", d.io_dtype, d.batch, d.seqlen, D);
     const float* const bias = r.flat(a[3], "bias", {D});
     const auto add = maybe_rows(r, a[4], "add", d, D);
@@ -316,7 +316,7 @@ PyObject* recurrence_bwd(PyObject* const* a)   // desc, x, g, bias, lengths, sta
 {
     Reader r;
     const auto d = r.desc<bimamba_recurrence_desc>(a[0]);
-    const int64_t D = d.d_inner, kept = (d.seqlen + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
+    const int64_t D = d.d_inner, kept = (int64_t(d.seqlen) + BIMAMBA_RECURRENCE_KEEP - 1) / BIMAMBA_RECURRENCE_KEEP;
     const auto view = [&](PyObject* o, const char* what) { return r.rows(o, what, d.io_dtype, d.batch, d.seqlen, D); };
     const auto x = view(a[1], "x"), g = view(a[2], "g");
     const float* const bias = r.flat(a[3], "bias", {D});

@@ -93,6 +93,15 @@ def test_recurrence_of_more_pieces_than_a_grid_holds(batch, seqlen, d):
     assert bd.bimamba_recurrence_bwd_workspace_bytes(bd.make_recurrence_desc(65535, 4, 65536)) > 0
 
 
+def test_recurrence_of_the_longest_sequences():
+    """Lengths whose pieces do not fit 32 bits when they are rounded up."""
+    for L in ((1 << 31) - 1, (1 << 31) - 63, (1 << 31) - 64):
+        long = dict(batch=1, seqlen=L, d_inner=1)
+        assert bd.bimamba_recurrence_workspace_bytes(bd.make_recurrence_desc(1, L, 1)) == 0
+        assert recurrence(x=view(AT[1], 1, L), g=view(AT[2], 1, L), y=view(AT[7], 1, L), add=None, **long) == UNSUPPORTED
+        assert recurrence_bwd(**long) == UNSUPPORTED
+
+
 def recurrence_bwd(**kw):
     d, kw = made(bd.make_recurrence_desc, dict(batch=2, seqlen=10, d_inner=64), kw)
     a = dict(x=view(AT[1]), g=view(AT[2]), bias=AT[3], lengths=AT[4], states=AT[5], dy=view(AT[6]), dh_out=AT[7], dx=view(AT[8]), dg=view(AT[9]),
