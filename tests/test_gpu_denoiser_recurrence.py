@@ -206,3 +206,28 @@ def test_a_captured_step(dn):
         for a, b in zip(held, want):
             assert float((a - b).norm()) <= 1e-5 * float(b.norm()) + 1e-12
         assert int(model.key[1]) == offset + 1
+
+
+@pytest.mark.parametrize("B,L", [(0, 5), (2, 0), (0, 0)])
+def test_no_tokens(dn, B, L):
+    """Outputs without elements, and gradients of zero for what is shared."""
+    r = lambda *s: torch.randn(*s, device="cuda").requires_grad_()  # noqa: E731
+    D, key = 12, torch.tensor([1, 2], device="cuda")
+    x, g, bias, h_in, w, gate = r(B, L, D), r(B, L, D), r(D), r(B, D), r(D), r(D)
+    h, last = dn.recurrence(x, g, bias, h_in=h_in, want_state=True)
+    y = dn.dropout_add(dn.group_norm(h, g, w, None, 3), gate, x, key, 0.5)
+    assert y.shape == (B, L, D) and torch.equal(last, h_in)
+    grads = torch.autograd.grad(y.sum() + last.sum(), (x, g, bias, h_in, w, gate))
+    assert torch.equal(grads[3], torch.ones_like(h_in)) and all(not bool(t.any()) for t in (grads[2], grads[4], grads[5]))
+    assert grads[0].shape == grads[1].shape == (B, L, D)
+
+
+def test_broadcast_and_expanded_gradients(dn):
+    """The gradient of a sum is one number seen through strides of zero."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, g, w = (torch.randn(2, 70, 24, device="cuda", generator=gen).requires_grad_() for _ in range(3))
+    key = torch.tensor([1, 2], device="cuda")
+    for call in (lambda: dn.recurrence(x, g, add=w), lambda: dn.group_norm(x, g, None, None, 2), lambda: dn.dropout_add(x, None, w, key, 0.5)):
+        leaves = [t for t in (x, g, w) if torch.autograd.grad(call().sum(), t, allow_unused=True)[0] is not None]
+        one, two = torch.autograd.grad(call().sum(), leaves), torch.autograd.grad(call(), leaves, torch.ones(2, 70, 24, device="cuda"))
+        assert all(torch.equal(a, b) for a, b in zip(one, two))
