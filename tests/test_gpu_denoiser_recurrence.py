@@ -122,7 +122,7 @@ def test_padded_sequences_with_log_gates_and_what_they_add_to(dn, L, reverse):
         ends.append(h)
     ry, rlast = torch.stack(ys), torch.stack(ends)
     want = torch.autograd.grad((ry * weight.double()).sum() + (rlast * weight[:, 0].double()).sum(), ref)
-    for a, r in zip((y, last) + got, (ry, rlast) + want):   # fp32: some hundred roundings of 2^-24
+    for a, r in zip((y, last) + got, (ry.detach(), rlast.detach()) + want):   # fp32: some hundred roundings of 2^-24
         assert float((a.detach().cpu().double() - r).norm() / r.norm()) < 2e-5
 
 
