@@ -10,8 +10,8 @@ namespace bm {
 // registers is half.)  What enters a piece comes from those before it.  A workgroup publishes its piece's (P, E),
 // looks back, and then publishes what leaves the piece as (0, h).  A pair is one word of 64
 // bits, written and read whole, so that no fence is needed; a word of ones says that nothing is there yet.  Pieces are handed out by a
-// counter in the order of the walk, all channels and sequences of a step before the next step: a workgroup waits for pieces that were
-// handed out before its own only, by workgroups that run, so every wait ends.
+// counter in the order of the walk, all channels and sequences of a step before the next step: a workgroup waits for pieces of its own channels
+// only, which were handed out before its own to workgroups that run, so every wait ends.
 //
 // Everything is in fp32: a, u, the states; y is rounded once.  1 - a is formed beside a from the same exponential, not as a difference, so
 // that it loses no digits where a is near 1.  fp32 activations: with e = exp(-|v|), sigmoid(|v|) = 1 - e / (1 + e) and sigmoid(-|v|) = e / (1 + e),
@@ -159,15 +159,16 @@ __device__ __forceinline__ void publish(unsigned long long* to, float p, float e
 // What a link makes of the state that enters it.  (One that nothing passes ends there, so that the word (0, h) stands for the state h itself.)
 __device__ __forceinline__ float through(float p, float e, float h) { return p == 0.0f ? e : p * h + e; }
 
-// Waits for the words of pieces that lie `stride` slots apart, of `end`'s for those of the state that it leaves.  (Were they not to come, which
-// would be a mistake here, the walk would go on with a NaN, not stand still.)
+// Waits for the words of pieces that lie `stride` slots apart, of `end`'s for those of the state that it leaves, a lane for those of its own channels:
+// one that the tile before owns (a last tile of a single channel takes it along) is another chain's, which no order of the queues ties to this
+// one's pieces, and nothing is made of it.  (Were the words not to come, which would be a mistake here, the walk would go on with a NaN, not stand still.)
 template <int kC, int kN, typename At>
 __device__ __forceinline__ void await(Link<kC> (&links)[kN], int n, const unsigned long long* from, long long stride, int end, const At& steps)
 {
     unsigned long long word[kN][kC];
     const auto there = [&](int k, int j) {
         const unsigned hi = (unsigned)(word[k][j] >> 32);
-        return min(k, n - 1) == end ? hi == 0 : hi != kNothing;
+        return !steps.has(j) || (min(k, n - 1) == end ? hi == 0 : hi != kNothing);
     };
     int tries = 1 << 22;
     for (;;) {

@@ -1,0 +1,52 @@
+"""The gated recurrence in the forms that sizes choose: against the walk in 64 bits with its running error bound, made on the GPU."""
+import math
+
+import pytest
+import torch
+
+from running_error import HALF_STEP
+from test_gpu_recurrence import bd, forward_ref, gradient_ref, inputs, run_backward, run_forward  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def empty_afterwards():
+    yield
+    torch.cuda.empty_cache()
+
+
+def within(got, ref, io="f32"):
+    """got (rounded once more where io is bf16) lies within ref's bound; both on the GPU."""
+    bound = ref.e + (HALF_STEP[io] * (ref.v.abs() + ref.e) if io != "f32" else 0.0) + 1e-37
+    off = (got.double() - ref.v).abs()
+    bad = ~(off <= bound)
+    assert got.shape == ref.v.shape and not bool(bad.any()), "%d of %d beyond the bound, worst %.3g times it" % (
+        int(bad.sum()), bad.numel(), float((off / bound)[bad].nan_to_num(nan=math.inf).max()))
+
+
+def both_ways(bd, B, L, D, io, gate, reverse, seed, lengths, extra=0):  # noqa: F811
+    """A walk and its gradients, twice: within their bounds, and the same bits."""
+    i = {k: None if t is None else t.cuda() for k, t in inputs(B, L, D, io, gate, seed, lengths).items()}
+    out = run_forward(bd, i, io, gate, reverse, extra=extra)
+    back = run_backward(bd, i, io, gate, reverse, out["states"], extra)
+    with torch.device("cuda"):
+        for k, ref in zip(("y", "h_out", "states"), forward_ref(i, gate, reverse, True, True)):
+            within(out[k], ref, io if k == "y" else "f32")
+        for k, ref in zip(("dx", "dg", "dbias", "dh_in"), gradient_ref(i, gate, reverse, out["states"])):
+            if back[k] is not None:
+                within(back[k], ref, io if k in ("dx", "dg") else "f32")
+    again = run_forward(bd, i, io, gate, reverse, extra=extra), run_backward(bd, i, io, gate, reverse, out["states"], extra)
+    for one, two in ((out, again[0]), (back, again[1])):
+        assert all(v is None or torch.equal(v, two[k]) for k, v in one.items())
+
+
+@pytest.mark.parametrize("B,L,D", [(129, 700, 129), (129, 500, 257), (170, 900, 129)])
+@pytest.mark.parametrize("reverse", [0, 1])
+def test_a_last_tile_of_one_channel_waits_for_its_own_pieces(bd, B, L, D, reverse):  # noqa: F811
+    """Rows that share cache lines, two channels a lane, several pieces, a last tile of one channel, whose lanes read the channel before it as
+    well; of the eight queues some begin between the tiles of one sequence.  (The words of that channel belong to pieces of another queue: a
+    wait for them would not be in the order of the walk.  It would not show in the results.)"""
+    tiles = -(-D // 128)
+    assert tiles * B >= 256 and D % 128 == 1 and any(q * tiles * B // 8 % tiles for q in range(8))
+    both_ways(bd, B, L, D, "bf16", ("sigmoid", "log")[reverse], reverse, B + L + D, L == 700)
