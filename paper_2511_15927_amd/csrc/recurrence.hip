@@ -605,8 +605,9 @@ size_t slots_bytes(const bimamba_recurrence_desc* d, const RecurPlan& p)   // (a
     return p.pieces > 1 ? (size_t)d->batch * p.pieces * d->d_inner * 8 + kXcds * 4 : 0;
 }
 
+// False: there is no kernel for the plan's pieces.
 template <typename IO, int kGate, int kC, bool kPast>
-void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
+bool launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
 {
     // How far a workgroup looks back: what a hop from one state to the next takes has to pass over as many pieces of a sequence as are done
     // meanwhile, the more the fewer sequences and channels there are; each piece looked at costs words to read.  65536 tokens of 2048
@@ -617,14 +618,14 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     a.look = look < 1 ? 1 : look > most ? most : look;
     if (p.pieces > 1) hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)(((long long)p.pieces * a.d + 256 * kCleared - 1) / (256 * kCleared)), a.batch), dim3(256), 0, st, a);
     const dim3 grid(p.tiles * (unsigned)a.batch * p.pieces), wg(64 * p.waves);
+    bool launched = false;
     const auto form = [&](auto tokens, auto waves) {
         constexpr int kT = decltype(tokens)::value, kW = decltype(waves)::value;
-        if (p.tokens != kT || p.waves != kW) return;
-        if (back) {
-            if constexpr (kT > 1 && (kC == 1 ? kT < 32 : kT * kW <= 64)) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
-        } else {
-            hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
-        }
+        constexpr bool kBack = kT > 1 && (kC == 1 ? kT < 32 : kT * kW <= 64);   // (there are gradients of such pieces)
+        if (p.tokens != kT || p.waves != kW || (back && !kBack)) return;
+        if (!back) hipLaunchKernelGGL((recur_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
+        else if constexpr (kBack) hipLaunchKernelGGL((recur_bwd_kernel<IO, kGate, kC, kT, kW, kPast>), grid, wg, 0, st, a);
+        launched = true;
     };
     using std::integral_constant;
     const integral_constant<int, 1> n1{};
@@ -639,13 +640,14 @@ void launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     form(n16, n8);
     if constexpr (kC == 1) form(n16, n16);
     if constexpr (sizeof(Piece<IO, kC>) == 4) form(n32, n8);
+    return launched;
 }
 template <typename IO, int kC>
-void launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool on_lines, bool back, hipStream_t st)
+bool launch_gate(const bimamba_recurrence_desc* d, const RecurPlan& p, const RecurArgs& a, bool on_lines, bool back, hipStream_t st)
 {
     const bool past = a.queues == 1 && on_lines && past_caches((back ? 5.0 : 3.0) * d->batch * d->seqlen * d->d_inner * sizeof(typename IO::T));
-    if (d->gate == BIMAMBA_GATE_SIGMOID) past ? launch_pieces<IO, kSigmoid, kC, true>(p, a, back, st) : launch_pieces<IO, kSigmoid, kC, false>(p, a, back, st);
-    else past ? launch_pieces<IO, kLog, kC, true>(p, a, back, st) : launch_pieces<IO, kLog, kC, false>(p, a, back, st);
+    if (d->gate == BIMAMBA_GATE_SIGMOID) return past ? launch_pieces<IO, kSigmoid, kC, true>(p, a, back, st) : launch_pieces<IO, kSigmoid, kC, false>(p, a, back, st);
+    return past ? launch_pieces<IO, kLog, kC, true>(p, a, back, st) : launch_pieces<IO, kLog, kC, false>(p, a, back, st);
 }
 // Where rows do not start at cache lines the pieces of neighbouring channels share lines: they are read and written through the caches, and, with
 // more chains than workgroups in hand, by workgroups of one XCD, which share a cache.  29 x 2478 tokens of 2248 channels, past the
@@ -656,15 +658,14 @@ bool on_lines(const RowView& v, size_t elem)
 {
     return !v.p || (reinterpret_cast<uintptr_t>(v.p) % 128 == 0 && v.sb * (long long)elem % 128 == 0 && v.st * (long long)elem % 128 == 0);
 }
-void launch(const bimamba_recurrence_desc* d, const RecurPlan& p, RecurArgs& a, bool back, hipStream_t st)
+bool launch(const bimamba_recurrence_desc* d, const RecurPlan& p, RecurArgs& a, bool back, hipStream_t st)
 {
     const size_t elem = dtype_bytes(d->io_dtype);
     bool lines = true;
     for (const RowView* v : {&a.x, &a.g, &a.add, &a.y, &a.dy, &a.dx, &a.dg}) lines = lines && on_lines(*v, elem);
     a.queues = !lines && p.tiles * (unsigned)a.batch >= (unsigned)cu_count() ? kXcds : 1;
-    if (d->io_dtype == BIMAMBA_F32) launch_gate<IoF32, 1>(d, p, a, lines, back, st);
-    else if (p.channels == 2) launch_gate<IoBF16, 2>(d, p, a, lines, back, st);
-    else launch_gate<IoBF16, 1>(d, p, a, lines, back, st);
+    if (d->io_dtype == BIMAMBA_F32) return launch_gate<IoF32, 1>(d, p, a, lines, back, st);
+    return p.channels == 2 ? launch_gate<IoBF16, 2>(d, p, a, lines, back, st) : launch_gate<IoBF16, 1>(d, p, a, lines, back, st);
 }
 
 // An fp32 or int64 array, none if p is null.
@@ -733,7 +734,7 @@ int bimamba_recurrence(const bimamba_recurrence_desc* d, const bimamba_tensor* x
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const Launches launches;
     if (L) {
-        launch(d, p, a, false, st);
+        if (!launch(d, p, a, false, st)) return BIMAMBA_ERR_UNSUPPORTED;
     } else if (h_out && h_out != h_in) {
         // (no token: the state goes through; a sum of one slot, or of none)
         launch_slot_sum(SlotSumArgs{{const_cast<float*>(h_in), nullptr}, {h_out, nullptr}, h_in ? 1 : 0, D, D}, Bt, st);
@@ -804,7 +805,7 @@ int bimamba_recurrence_bwd(const bimamba_recurrence_desc* d, const bimamba_tenso
         float* const sums = static_cast<float*>(workspace) + slots_bytes(d, p) / sizeof(float);
         a.dbias = dbias ? slots > 1 ? sums : dbias : nullptr;
         a.L = L, a.d = D, a.pieces = p.pieces, a.reverse = d->reverse, a.batch = Bt;
-        launch(d, p, a, true, st);
+        if (!launch(d, p, a, true, st)) return BIMAMBA_ERR_UNSUPPORTED;
         if (dbias && slots > 1) launch_slot_sum(SlotSumArgs{{sums, nullptr}, {dbias, nullptr}, slots, D, D}, 1, st);
     } else {
         if (Bt && dh_in && dh_in != dh_out) launch_slot_sum(SlotSumArgs{{const_cast<float*>(dh_out), nullptr}, {dh_in, nullptr}, dh_out ? 1 : 0, D, D}, Bt, st);

@@ -50,3 +50,16 @@ def test_a_last_tile_of_one_channel_waits_for_its_own_pieces(bd, B, L, D, revers
     tiles = -(-D // 128)
     assert tiles * B >= 256 and D % 128 == 1 and any(q * tiles * B // 8 % tiles for q in range(8))
     both_ways(bd, B, L, D, "bf16", ("sigmoid", "log")[reverse], reverse, B + L + D, L == 700)
+
+
+# tokens of a wave, waves and channels a lane: what the rule of sizes gives them in bf16 (fp32: one channel), forward and for gradients
+FORMS = [(3, 1, 200), (2, 3, 50), (2, 3, 200), (3, 30, 40), (2, 32, 256), (3, 50, 40), (2, 64, 256), (2, 128, 64), (2, 200, 100), (90, 200, 256), (3, 300, 64),
+         (40, 500, 100)]
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,D", FORMS)
+def test_every_form_is_there(bd, B, L, D, io):  # noqa: F811
+    """(Outputs start as NaN: a form that is planned and not there would leave them.)"""
+    n = FORMS.index((B, L, D))
+    both_ways(bd, B, L, D, io, ("sigmoid", "log")[n % 2], n // 2 % 2, 900 + n, n % 3 == 0, extra=(0, 3)[n % 2])
