@@ -63,3 +63,16 @@ def test_every_form_is_there(bd, B, L, D, io):  # noqa: F811
     """(Outputs start as NaN: a form that is planned and not there would leave them.)"""
     n = FORMS.index((B, L, D))
     both_ways(bd, B, L, D, io, ("sigmoid", "log")[n % 2], n // 2 % 2, 900 + n, n % 3 == 0, extra=(0, 3)[n % 2])
+
+
+# two channels a lane, sequences of several pieces, tiles whose lanes all own their channels, several of them and a last one that is cut; pieces of
+# 16 x 8 and 32 x 8 and, for gradients, 16 x 4; one piece looked back at and several
+WIDE = [(350, 300, 128), (180, 300, 256), (150, 300, 257), (130, 500, 256), (90, 700, 256), (57, 1100, 256), (34, 4000, 128)]
+
+
+@pytest.mark.parametrize("gate", ["log", "sigmoid"])
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("B,L,D", WIDE)
+def test_two_channels_a_lane_in_whole_tiles(bd, B, L, D, reverse, gate):  # noqa: F811
+    n = WIDE.index((B, L, D)) + reverse + 2 * (gate == "log")
+    both_ways(bd, B, L, D, "bf16", gate, reverse, 700 + n, n % 3 == 0, extra=(0, 3)[n % 2])
