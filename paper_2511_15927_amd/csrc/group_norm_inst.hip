@@ -378,8 +378,12 @@ template <typename IO, int kAct, int kWaves, int kPieces, int kTeam, bool kPast,
 void launch_form(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
 {
     const dim3 grid(p.tiles, p.row_groups), wg(64 * kTeam);
-    if (bwd) hipLaunchKernelGGL((group_norm_bwd_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
-    else hipLaunchKernelGGL((group_norm_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
+    constexpr bool kOne = kWaves == 1 && kPieces == 1 && !kMany;   // (gradients in teams of eight, the norm in teams of four)
+    if (bwd) {
+        if constexpr (!kOne || kTeam == 8) hipLaunchKernelGGL((group_norm_bwd_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
+    } else {
+        if constexpr (!kOne || kTeam == 4) hipLaunchKernelGGL((group_norm_kernel<IO, kAct, kWaves, kPieces, kTeam, kPast, kMany>), grid, wg, 0, st, a);
+    }
 }
 template <typename IO, int kAct, bool kPast>
 void launch_io(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t st)
@@ -392,7 +396,7 @@ void launch_io(const GroupPlan& p, const GroupNormArgs& a, bool bwd, hipStream_t
         launch_form<IO, kAct, 4, kWide, 4, kPast>(p, a, bwd, st);
     } else if (p.pieces == 1) {
         if (p.at_once > 1) launch_form<IO, kAct, 1, 1, 4, kPast, true>(p, a, bwd, st);
-        else if (p.team == 8) launch_form<IO, kAct, 1, 1, 8, kPast>(p, a, bwd, st);
+        else if (bwd) launch_form<IO, kAct, 1, 1, 8, kPast>(p, a, bwd, st);
         else launch_form<IO, kAct, 1, 1, 4, kPast>(p, a, bwd, st);
     } else if (p.pieces == 2) {
         launch_form<IO, kAct, 1, 2, 4, kPast>(p, a, bwd, st);

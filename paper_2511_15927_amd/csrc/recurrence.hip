@@ -633,8 +633,10 @@ bool launch_pieces(const RecurPlan& p, RecurArgs a, bool back, hipStream_t st)
     const integral_constant<int, 8> n8{};
     const integral_constant<int, 16> n16{};
     const integral_constant<int, 32> n32{};
-    form(n1, n1);
-    form(n4, n1);
+    if constexpr (!kPast || kC == 2 || sizeof(typename IO::T) == 4) {   // (up to four tokens of 64 channels: the caches hold all that 65535 sequences move)
+        form(n1, n1);
+        form(n4, n1);
+    }
     form(n8, n4);
     form(n16, n4);
     form(n16, n8);
