@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedSumArgs a)
     if (slice >= a.slices) return;
     const int block = w - slice * a.col_blocks, lane = threadIdx.x % 64;
     if (a.d >= kPieceOf<IO>) sum_slice<IO, kPieceOf<IO>, kPast>(a, slice, block, lane);
-    else sum_slice<IO, 1, kPast>(a, slice, block, lane);
+    else sum_slice<IO, 1, false>(a, slice, block, lane);
 }
 
 // The rows of runs that span slices.  256 channels of a short run: a wave adds up its slots.  Of a long run: a workgroup, each of its

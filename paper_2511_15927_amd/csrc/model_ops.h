@@ -25,7 +25,9 @@ struct Piece {
 // lines it has to push out cost it time.  Stores, 65536 rows of 2048: layer norm 101 -> 97 us; gradient of 16384 rows of 50304 logits
 // 492 -> 407.  Loads help where little or nothing is written beside them: log probabilities of those logits 146 -> 127 us, layer norm's
 // gradients 169 -> 162; in those two 97 -> 115 and 402 -> 426, which therefore load through the caches.  (A flag at run time would not
-// do: the compiler joins the two accesses and drops the difference.)
+// do: the compiler joins the two accesses and drops the difference.)  Accesses of two bytes stay in the caches; those of four, two bf16
+// channels of the recurrence or a single fp32 one in rows of up to three, pay in the token table's rows (32M rows of 2 channels 235 -> 185 us, of
+// 3 491 -> 370), cost in the gradients of the layer norm and, of 3 channels, of the table (9440 -> 9505), which take theirs through the caches.
 template <int kBytes>
 struct PastCaches {
     typedef unsigned Bits __attribute__((ext_vector_type(kBytes / 4)));
