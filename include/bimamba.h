@@ -474,7 +474,10 @@ typedef struct bimamba_recurrence_desc {
  *             the order of the walk; the gradients take them.  Behind a sequence's end: its last state.
  *   workspace at least bimamba_recurrence_workspace_bytes(desc) bytes, 16-byte aligned; may be NULL if that is 0.
  * A value that is not finite makes everything not finite that its channel's walk reaches after it, up to factors whose product is 0 (a
- * factor of 0, or one that underflows): whether it reaches past those is left open.
+ * factor of 0, or one that underflows): whether it reaches past those, and whether into both y and h_out, is left open.
+ * All arithmetic is fp32, y is rounded once.  What a step is off by stays in the states that leave the call, and in the gradients' dh_in and dbias: its
+ * own rounding, up to 2^-24, and that of a sigmoid's factor near 1, up to 2^-25 with fp32 activations and 2^-23 with bf16 ones, of the state,
+ * as many times as the channel remembers tokens (bf16: 2^-13 at 700 of them; from some 20000 on more than a bf16 y loses as it is rounded).
  */
 int bimamba_recurrence(const bimamba_recurrence_desc* desc, const bimamba_tensor* x, const bimamba_tensor* g, const float* bias,
                        const bimamba_tensor* add, const int64_t* lengths, const float* h_in, const bimamba_tensor* y, float* h_out,

@@ -16,8 +16,10 @@ namespace bm {
 // Everything is in fp32: a, u, the states; y is rounded once.  1 - a is formed beside a from the same exponential, not as a difference, so
 // that it loses no digits where a is near 1.  fp32 activations: with e = exp(-|v|), sigmoid(|v|) = 1 - e / (1 + e) and sigmoid(-|v|) = e / (1 + e),
 // a off by half a unit of its last place where it is near 1.  bf16 ones: with e = exp(-v), a = 1 / (1 + e) and 1 - a = e a, without a
-// selection; a is off by two units there (the sum's and the reciprocal's), which a channel that remembers 1000 tokens turns into 2^-13 of a state, a
-// thirtieth of what y loses as it is rounded (8 x 8192 tokens of 4096 channels: 356 us with selections, 332 without; fp32 the same).
+// selection; a is off by two units there (the sum's and the reciprocal's, 2^-23).  With the 2^-24 that a step's own rounding may take, a channel that
+// remembers M tokens turns that into 1.5 M 2^-23 of its state at most, where half a unit of a would leave 0.75 M 2^-23: at 1000 tokens a twentieth of
+// what y loses as it is rounded, at 20000 as much; the states, dh_in and dbias are not rounded and carry it.  (8 x 8192 tokens of 4096 channels:
+// 356 us with selections, 332 without; fp32 the same.)
 constexpr int kKeep = BIMAMBA_RECURRENCE_KEEP;   // steps between two kept states
 
 enum Gate { kLog, kSigmoid };

@@ -76,3 +76,24 @@ WIDE = [(350, 300, 128), (180, 300, 256), (150, 300, 257), (130, 500, 256), (90,
 def test_two_channels_a_lane_in_whole_tiles(bd, B, L, D, reverse, gate):  # noqa: F811
     n = WIDE.index((B, L, D)) + reverse + 2 * (gate == "log")
     both_ways(bd, B, L, D, "bf16", gate, reverse, 700 + n, n % 3 == 0, extra=(0, 3)[n % 2])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,D", [(2, 4096, 70), (1, 33, 130)])
+def test_channels_that_remember_far(bd, B, L, D, io):  # noqa: F811
+    """10^4 to 10^5 tokens: what the factor is off by in every step stays in the states, which leave the call in fp32 whatever the activations' type
+    (the walk's bound: 3 units of 2^-24 a step for bf16, 1 for fp32, and 4 for the step's own rounding)."""
+    i = {k: None if t is None else t.cuda() for k, t in inputs(B, L, D, io, "sigmoid", 40 + L).items()}
+    i["bias"] = torch.linspace(math.log(1e4), math.log(1e5), D, device="cuda")
+    i["g"] = (i["g"] / 8).to(i["x"].dtype)
+    i["x"], i["h_in"] = torch.ones_like(i["x"]), torch.ones_like(i["h_in"])   # (the state stays at 1: what the factors are off by adds up)
+    out = run_forward(bd, i, io, "sigmoid", 0, add=False)
+    back = run_backward(bd, i, io, "sigmoid", 0, out["states"])
+    with torch.device("cuda"):
+        y, last, kept = forward_ref(i, "sigmoid", 0, True, False)
+        dx, dg, dbias, dh_in = gradient_ref(i, "sigmoid", 0, out["states"])
+        assert bool(((last.v - 1).abs() < 1e-12).all()) and bool((last.e <= 9 * 2.0 ** -24 * L).all())
+        for got, ref in ((out["h_out"], last), (out["states"], kept), (back["dh_in"], dh_in), (back["dbias"], dbias)):
+            within(got, ref)
+        for got, ref in ((out["y"], y), (back["dx"], dx), (back["dg"], dg)):
+            within(got, ref, io)
