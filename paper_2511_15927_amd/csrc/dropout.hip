@@ -38,9 +38,12 @@ struct DropArgs {
 };
 __device__ __forceinline__ unsigned half_of(const Words& r, int i) { return (r.w[i >> 1] >> (i & 1 ? 16 : 0)) & 0xffffu; }
 
-// A lane has one piece of 16 bytes of a row in hand; with short rows a wave takes several at once.  What bounds it are the bytes, the
-// generator runs beside them (65536 rows of 2048 bf16 with a residual and a gate: 126 to 131 us, 6.3 TB/s, at p = 0.1 and, without the
-// generator, 124 at p = 0; a large copy reaches 6.1).  A wave takes two rows and goes, eight for the gate's gradient, so that all waves in hand
+// A lane has one piece of 16 bytes of a row in hand; with short rows a wave takes several at once.  What bounds it are the bytes, with the
+// generator close behind them: where all lanes hold a piece the vector pipe is busy 88 % of the time, 82 % in the gradients (65536 rows of 2048 bf16
+// with a residual and a gate: 126 to 131 us, 6.3 TB/s, at p = 0.1 and, without the generator, 124 at p = 0; a large copy reaches 6.1).  Lanes that
+// hold nothing run the generator all the same, so at widths that are not 2^k pieces, or a little more than 64 of them, it is what
+// bounds it: 262144 rows of 512 122 us (6.6 TB/s), of 520 206 (4.0), of 640 208 (4.8), of 768 226 (5.3), of 384 116 (5.2), of 320 110 (4.6).
+// A wave takes two rows and goes, eight for the gate's gradient, so that all waves in hand
 // work on neighbouring rows: 1 row 156 us, 8 rows 140, 32 rows 165; gradients with 8 rows 134 us, 2 rows 145, 32 rows 172.
 template <typename IO, int kPiece>
 struct DropPlace {
@@ -183,7 +186,8 @@ DropPlan plan_dropout(const bimamba_dropout_desc* d, bool per_batch, bool sums)
     p.tiles = (pieces + p.lanes - 1) / p.lanes;
     p.vectors = per_batch ? d->batch : 1;
     p.rows = per_batch ? d->seqlen : (unsigned)((long long)d->batch * d->seqlen);
-    // Rows: as many as are in hand at once go to one wave each, a few more where there are more of them.
+    // Rows: as many as are in hand at once go to one wave each, a few more where there are more of them.  (Sums: divided by 6 and by 16, gradients of 4096
+    // rows of 2048 14.1 and 16.6 us, of 16384 of 512 16.8, 19.9; of 8192 of 2048 23.4, 22.6, of 16384 37.5, 36.3; from 65536 on and up to 2048 rows the same.)
     const unsigned together = kTeam * (64 / p.lanes), most = sums ? 8 : 2;
     const unsigned long long fair = (unsigned long long)p.rows * p.tiles * p.vectors / (together * (sums ? 6u : 16u) * cu_count());
     p.per_wave = (unsigned)(fair < 1 ? 1 : fair > most ? most : fair);

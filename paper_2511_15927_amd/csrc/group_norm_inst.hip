@@ -9,11 +9,14 @@ namespace bm {
 // taken over the registers, the mean before the squares around it, so that a large mean costs no digits.  All arithmetic is fp32,
 // each output is rounded once.
 //
-// What bounds it are the bytes, and in which order the memory sees them: a wave takes four rows and goes, so that all waves in hand
+// What bounds it are the bytes, with the vector pipe beside them (busy all of the time with a gate and a mean, two thirds in the gradients, where all
+// lanes hold elements), and in which order the memory sees them: a wave takes four rows and goes, so that all waves in hand
 // work on neighbouring rows.  65536 rows of 4096 in groups of 64, gated, past the caches: 4 rows 250 us (6.45 TB/s; two tensors added to a
 // third reach 6.0, past the caches 6.55), 1 row 284, 8 rows 274; through the caches 280; gradients 433 us (6.2 TB/s), 2 rows 461, 8 rows 463,
 // through the caches 478.  Groups that waves share wait at a barrier in each row: their gradients read a row ahead (65536 groups of
-// 4096 511 us, 541 without).
+// 4096 511 us, 541 without).  Lanes, pieces and waves come in powers of two: groups between them leave lanes empty, whose vector work the bytes
+// no longer hide (65536 rows, gated before: one group of 2048 133 us, 6.05 TB/s; of 1536 138, 4.4; of 2560 233, 4.3; of 5120 529, 3.8; 20 of 100 191,
+// 4.1; 55 of 37 276, 2.9; gradients 268, 223, 536, 1039, 340, 490).
 enum Act { kPlain = BIMAMBA_ACT_NONE, kSilu = BIMAMBA_ACT_SILU, kBefore = BIMAMBA_ACT_GATE_BEFORE, kAfter = BIMAMBA_ACT_GATE_AFTER };
 
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
